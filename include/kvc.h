@@ -508,6 +508,160 @@ kvc_status kvc_tiling_costs(const kvc_layout* layout, const void* kv, kvc_stride
                             int32_t width, int32_t height, void* workspace, size_t workspace_bytes, double* d_cost,
                             void* stream);
 
+/* ---- Serving on a restored cache -------------------------------------------
+ * What an engine does with the paged memory once a fetched prefix is in it
+ * (Sec. 4 item (2): the slots that restored tensors fill are the engine's; Sec.
+ * 3.3.2): many requests take up the prefix, each goes on with tokens of its
+ * own, and the pages come and go.  A "page" is a block of the paged cache in
+ * all layers, K and V: block id p of every layer's [2][num_blocks][block_size][H][D].
+ *
+ * A pool is that cache with its books: a table of pages and a length for each
+ * row (a row is a sequence; position t of row r lies in block
+ * tables[r][t / block_size], slot t % block_size), and for each page the number
+ * of table entries that hold it.  A page is free when its count is 0.  All
+ * of it is DEVICE memory of the caller's; the calls below read and write it on
+ * `stream`, so the host need not know lengths or page ids.  Entries of a row
+ * beyond ceil(lens / block_size) mean nothing and are not looked at.
+ *
+ * Pages are taken lowest id first, in the order of the list that a call is
+ * given, so the same books always become the same books.
+ *
+ * Faults that only the device can see are ORed into *d_err (KVC_FAULT_*).  A
+ * fork or grow whose list is at fault (KVC_FAULT_LIST) or lacks room
+ * (KVC_FAULT_NO_ROOM) changes nothing at all; a count of holders below 0 is
+ * taken for 0; what a single bad page id does is said at each call. */
+enum {
+  KVC_FAULT_PAGE = 1,    /* a table entry or page id outside [0, num_blocks): what it would touch is left out  */
+  KVC_FAULT_LIST = 2,    /* a list or book that contradicts itself: a row outside [0, n_rows), a length outside
+                            the row or below the tokens it should hold, a child twice or not empty, a count of holders
+                            below 0, a table that holds a free page                                     */
+  KVC_FAULT_NO_ROOM = 4  /* fewer pages are free than the call needs, or a row's table is full            */
+};
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(kvc_pool)                                     */
+  uint32_t abi_version; /* KVC_ABI_VERSION                                      */
+  int32_t num_layers, num_kv_heads, head_dim; /* head_dim a multiple of 8, else KVC_ERR_UNSUPPORTED */
+  int32_t dtype;        /* kvc_dtype                                            */
+  int64_t num_blocks;   /* pages; num_blocks * block_size below 2^32, else KVC_ERR_UNSUPPORTED      */
+  int64_t n_rows;       /* rows of the table, below 2^18, else KVC_ERR_UNSUPPORTED                  */
+  int32_t block_size;   /* tokens of a page, any number >= 1                    */
+  int32_t table_len;    /* entries of a row; table_len * block_size below 2^31, else KVC_ERR_UNSUPPORTED */
+  void* const* d_layer_cache; /* DEVICE array of num_layers DEVICE pointers, 16-byte aligned          */
+  int32_t* d_tables;    /* DEVICE int32 [n_rows][table_len]                     */
+  int32_t* d_lens;      /* DEVICE int32 [n_rows]: tokens of each row            */
+  int32_t* d_refs;      /* DEVICE int32 [num_blocks]: holders of each page; may be NULL for kvc_pages_copy,
+                           kvc_append_paged and kvc_attend_paged                */
+  uint32_t* d_err;      /* DEVICE, may be NULL                                  */
+} kvc_pool;
+
+/* Checks a pool on the host (sizes, NULL pointers, alignment). */
+kvc_status kvc_pool_validate(const kvc_pool* pool);
+
+/* Copies pages: page d_src[i] -> page d_dst[i] in all layers, K and V.
+ *   d_src, d_dst  DEVICE in: int32 [n].  No page may be copied to twice, nor be
+ *                 both copied from and copied to (the order of the copies is open)
+ * A pair with an id outside the pool is left out (KVC_FAULT_PAGE).  The books are not touched. */
+kvc_status kvc_pages_copy(const kvc_pool* pool, const int32_t* d_src, const int32_t* d_dst, int64_t n, void* stream);
+
+/* Bytes of the workspace that fork, grow and compact need (256-byte aligned
+ * DEVICE memory, contents mean nothing, one call at a time); 0 on a bad argument. */
+size_t kvc_pages_workspace(const kvc_pool* pool);
+
+/* Forks rows: row d_children[i] becomes a copy of row d_parents[i].  Whole pages
+ * are shared (their counts go up by one), the tokens of the parent's last page, where
+ * it is filled in part, are copied to a page that is taken for the child, in all
+ * layers; no token that either writes from then on is seen by the other.
+ *   d_parents, d_children  DEVICE in: int32 [n], n <= n_rows.  A child's length must be 0;
+ *                          a parent may have many children, a child may not be a
+ *                          parent or a child twice in one call
+ * A parent's entry outside the pool is copied as it is and shared with nobody
+ * (KVC_FAULT_PAGE). */
+kvc_status kvc_pages_fork(const kvc_pool* pool, const int32_t* d_parents, const int32_t* d_children, int64_t n,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Makes rows longer: lens[d_rows[i]] += d_counts[i], and takes the pages that
+ * the row's table then lacks.  Their contents are what was there before.
+ *   d_rows    DEVICE in: int32 [n], n <= n_rows, no row twice
+ *   d_counts  DEVICE in: int32 [n], >= 0; NULL: one token each
+ * KVC_FAULT_LIST too where a last page that is filled in part and would be written
+ * to is held by another row. */
+kvc_status kvc_pages_grow(const kvc_pool* pool, const int32_t* d_rows, const int32_t* d_counts, int64_t n, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Empties rows: the counts of their pages go down by one, their lengths become 0
+ * (a row twice in the list, or one that is empty, is not freed again).
+ *   d_rows  DEVICE in: int32 [n]
+ * What is wrong in one row (KVC_FAULT_PAGE, KVC_FAULT_LIST) does not keep the others from being freed. */
+kvc_status kvc_pages_free(const kvc_pool* pool, const int32_t* d_rows, int64_t n, void* stream);
+
+/* Moves the pages in use to the lowest places.  With n pages in use, the k-th
+ * page in use at a place >= n (counted from below) moves to the k-th free place < n;
+ * every other page stays.  Pages are moved in all layers; places that become free
+ * keep their contents.
+ *   d_map         DEVICE out: int32 [num_blocks], where each page went; -1 for a free one
+ *   d_tables_out  DEVICE out: int32 [n_rows][table_len], the tables with the new places (entries
+ *                 that mean nothing are copied); may be the pool's own, or apart from them
+ *   d_refs_out    DEVICE out: int32 [num_blocks], the counts at the new places; likewise
+ * A table entry outside the pool, or one that holds a free page, is copied as it is
+ * (KVC_FAULT_PAGE, KVC_FAULT_LIST); the call goes on. */
+kvc_status kvc_pages_compact(const kvc_pool* pool, int32_t* d_map, int32_t* d_tables_out, int32_t* d_refs_out, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* The tokens of a step.  Request r is row d_rows[r] of the pool, and its new tokens
+ * are its row's last ones: token i of n_r (0-based) is position lens - n_r + i. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(kvc_batch)                                    */
+  uint32_t abi_version; /* KVC_ABI_VERSION                                      */
+  int32_t n_requests;   /* >= 0                                                 */
+  int32_t most_new;     /* no request has more new tokens (a bound for the launch; later ones get no result, KVC_FAULT_LIST) */
+  int64_t n_new;        /* new tokens of all requests, below 2^31               */
+  const int32_t* d_rows;   /* DEVICE int32 [n_requests]; NULL: row r            */
+  const int32_t* d_starts; /* DEVICE int32 [n_requests + 1], ascending from 0 to n_new: request r has the tokens
+                              [starts[r], starts[r+1]); NULL: one token each (n_new == n_requests, most_new == 1) */
+} kvc_batch;
+
+/* Writes keys and values of the batch's new tokens to their slots in one layer.
+ *   k, v          DEVICE in: [n_new][H][D], 16-byte aligned, the [H][D] of a token contiguous
+ *   token_stride  elements from a token to the next, of k and of v; a multiple of 8
+ * A token whose page is outside the pool (KVC_FAULT_PAGE), or whose position is not in its
+ * row (KVC_FAULT_LIST), is left out. */
+kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_t layer, const void* k, const void* v,
+                            int64_t token_stride, void* stream);
+
+/* Attention of the batch's new tokens over their rows, in one layer.  The query
+ * of a token at position p sees the positions 0 .. p of its row (p < 0: none):
+ *   out = sum_j softmax_j(scale * q.k_j) v_j,   lse = log sum_j exp(scale * q.k_j)
+ * and out = 0, lse = -inf where it sees none.  Query head h reads KV head
+ * h / (num_q_heads / H).  The rows share their first prefix_tokens positions, which are
+ * read through row prefix_row's table, once for all queries.
+ * Arithmetic: products of 16-bit values summed in fp32, softmax and sums in fp32,
+ * probabilities rounded to the cache's type before they meet V, one rounding at the end. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(kvc_attention)                                */
+  uint32_t abi_version; /* KVC_ABI_VERSION                                      */
+  int32_t num_q_heads;  /* a multiple of H                                      */
+  float scale;          /* > 0, finite                                          */
+  int64_t most_tokens;  /* no row of the batch is longer (a bound for the launch; what lies beyond is not seen, KVC_FAULT_LIST) */
+  int64_t prefix_tokens; /* 0: nothing is shared.  Any number up to most_tokens; rows may be shorter */
+  int64_t prefix_row;   /* row whose first prefix_tokens positions every row of the batch has, as far as it goes */
+  int64_t q_token_stride, q_head_stride;     /* elements, multiples of 8       */
+  int64_t out_token_stride, out_head_stride; /* elements, multiples of 8       */
+} kvc_attention;
+
+/* Bytes of the workspace of a call (0 is an answer too); (size_t)-1 on a bad argument. */
+size_t kvc_attention_workspace(const kvc_pool* pool, const kvc_batch* batch, const kvc_attention* attention);
+
+/*   q          DEVICE in : [n_new][num_q_heads][D] by its strides, 16-byte aligned
+ *   out        DEVICE out: likewise, every element written
+ *   lse        DEVICE out: fp32 [n_new][num_q_heads], may be NULL
+ *   workspace  DEVICE, 256-byte aligned, contents mean nothing, one call at a time
+ * head_dim up to 256, else KVC_ERR_UNSUPPORTED.  A position whose page is outside the
+ * pool is not seen (KVC_FAULT_PAGE).  The launch is fixed by the host's arguments: it may be
+ * captured into a graph and replayed while lengths, tables and rows change within the bounds. */
+kvc_status kvc_attend_paged(const kvc_pool* pool, const kvc_batch* batch, const kvc_attention* attention, int32_t layer,
+                            const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, not a step of the paper's path: a streaming copy with the byte
  * ratio of restore (8 bytes read and 16 written per lane).  The benchmark runs it
  * to show what the part delivers for sequential output and for output cut into

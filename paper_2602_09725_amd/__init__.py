@@ -10,4 +10,6 @@ from .kvc import (  # noqa: F401
     layout_set_resolution, meta_staging_size, pack_form, pack_plan, build_id, select_resolution, kvc_fetch_pipeline, kvc_fetch_pipeline_frames, kvc_pack, kvc_restore, kvc_restore_paged,
     kvc_restore_paged_frame, kvc_restore_paged_frames, layout_validate, lib_path, load, status_str, N_RESIDUALS, residual_histograms_size,
     kvc_residual_histograms, kvc_proxy_costs, proxy_cost_bits, tile_candidates, kvc_tiling_costs, tiling_costs_workspace, tile_arrays, kvc_probe_expand, PROBE_ONE_XCD_PER_PIECE, PROBE_LINE_READS,
+    Attention, Batch, KVC_FAULT_LIST, KVC_FAULT_NO_ROOM, KVC_FAULT_PAGE, Pool, attention_workspace, kvc_append_paged, kvc_attend_paged,
+    kvc_pages_compact, kvc_pages_copy, kvc_pages_fork, kvc_pages_free, kvc_pages_grow, pages_workspace, pool_validate,
 )

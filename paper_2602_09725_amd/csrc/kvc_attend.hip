@@ -1,0 +1,595 @@
+// Attention of a batch over paged rows that share their first tokens (kvc_attend_paged).
+//
+// Of a query row (a token and one of the G query heads of a KV head) with s_j = q . k_j, the result is
+//   out = sum_j w_j v_j / sum_j w_j,  w_j = exp2(scale_log2 * (s_j - m)),  m any number near the largest s_j,
+// and results over disjoint sets of tokens join by their m and sums.  So the work is cut into pieces: the shared prefix is
+// one sequence for the rows of all requests (read once for 32 or 128 of them), each row's own tokens another for the rows
+// of its request, and both are cut along the tokens until the chip is full.  A second, small launch joins the pieces.
+//
+// A wave holds 32 rows.  It computes S^T = K Q^T and O^T += V^T W^T with 32x32x16 matrix instructions, so that a lane has
+// one row (lane % 32) in all of its registers: the softmax needs one exchange between the halves of a wave for a
+// maximum, and W^T leaves the first product in the order that the second one takes, if V's tokens are taken in
+// the same order: lanes 0-31 hold tokens {0..3, 8..11}, lanes 32-63 {4..7, 12..15} of 16.  V^T comes from V's rows in LDS by
+// transposing reads.
+#include <hip/hip_runtime.h>
+
+#include "kvc_device.h"
+#include "kvc_serve.h"
+
+namespace kvc {
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define KVC_LDS __attribute__((address_space(3)))
+
+template <int DT>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (DT == KVC_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ void fault(const AttendParams& p, uint32_t bits) {
+  if (p.pool.err && bits) atomicOr(p.pool.err, bits);
+}
+
+// Values of a lane and of its partner 32 lanes away.
+__device__ __forceinline__ float half_max(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+constexpr float kNone = -__builtin_inff();
+
+// exp2(a - b) where a is -inf if b is: 0 then.
+__device__ __forceinline__ float weight(float a, float b) { return a == kNone ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
+
+// ---- who sees what --------------------------------------------------------------------------------------------------------
+
+struct Request {
+  uint32_t row, first, n, len;  // row of the table; first new token, new tokens; tokens (the true length)
+  uint32_t faults;
+};
+
+__device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r) {
+  Request q;
+  q.faults = 0;
+  q.first = r;
+  q.n = 1;
+  if (p.batch.starts) {
+    const uint32_t a = (uint32_t)p.batch.starts[r], b = (uint32_t)p.batch.starts[r + 1];
+    q.first = a < p.batch.n_new ? a : p.batch.n_new;
+    const uint32_t end = b < p.batch.n_new ? b : p.batch.n_new;
+    q.n = end > q.first ? end - q.first : 0;
+    if (a > b || b > p.batch.n_new || q.n > p.batch.most_new) q.faults |= KVC_FAULT_LIST;
+  }
+  q.row = p.batch.rows ? (uint32_t)p.batch.rows[r] : r;
+  q.len = 0;
+  if (q.row < p.pool.n_rows) q.len = (uint32_t)p.pool.lens[q.row];
+  else q.faults |= KVC_FAULT_LIST, q.row = 0;
+  if (q.len > p.most_tokens) {
+    q.faults |= KVC_FAULT_LIST;
+    if (q.len > 0x7fffffffu) q.len = 0;
+  }
+  return q;
+}
+
+// Positions that new token t of a request sees: those below this.
+__device__ __forceinline__ uint32_t limit_of(const AttendParams& p, const Request& q, uint32_t t) {
+  const int64_t seen = (int64_t)q.len - q.n + (t - q.first) + 1;
+  return seen < 0 ? 0 : seen < (int64_t)p.most_tokens ? (uint32_t)seen : p.most_tokens;
+}
+
+// Request of new token t.
+__device__ __forceinline__ uint32_t request_of(const BatchView& b, uint32_t t) {
+  if (!b.starts) return t;
+  uint32_t low = 0, high = b.n_requests;
+  while (low + 1 < high) {
+    const uint32_t mid = (low + high) / 2;
+    if ((uint32_t)b.starts[mid] <= t) low = mid;
+    else high = mid;
+  }
+  return low;
+}
+
+// Tokens of the shared prefix that there are.
+__device__ __forceinline__ uint32_t prefix_there(const AttendParams& p) {
+  if (p.prefix == 0) return 0;
+  const uint32_t len = (uint32_t)as_const(p.pool.lens)[p.prefix_row];
+  return len > p.pool.capacity ? 0 : len < p.prefix ? len : p.prefix;
+}
+
+// ---- tiles ----------------------------------------------------------------------------------------------------------------
+
+// What a load of a token that is not there reads.
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// Where the 16-byte vector `chunk` of a token's row lies in the row in LDS.  Reads of K take one chunk of 32 tokens that follow one
+// another, transposing reads of V two of four: both find them in different banks.
+template <int CH>
+__device__ __forceinline__ uint32_t place(uint32_t token, uint32_t chunk) {
+  constexpr uint32_t B = CH >= 16 ? 16 : CH, LOG = B == 16 ? 4 : 3;
+  return chunk ^ (((token << 1) & (B - 1)) | ((token >> (LOG - 1)) & 1u));
+}
+
+template <int DT>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  const uint32_t e = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
+  return (w & e) == e || ((w >> 16) & e) == e;
+}
+
+// The two values of a word, 0 in the place of those that are not finite.
+template <int DT>
+__device__ __forceinline__ uint32_t only_finite(uint32_t w) {
+  const uint32_t e = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
+  if ((w & e) == e) w &= 0xffff0000u;
+  if (((w >> 16) & e) == e) w &= 0xffffu;
+  return w;
+}
+
+// Sizes of a body: R waves side by side along the rows; tokens of a tile; LDS of a tile's K (and V).
+template <int DP, int R>
+struct Shape {
+  static constexpr int CH = DP / 8;                          // vectors of a token's row
+  static constexpr int TT = R == 1 || DP > 128 ? 32 : 64;    // tokens of a tile
+  static constexpr int GROUPS = 4 / R;                       // waves along the tokens, each with tiles of its own
+  static constexpr int BUFFERS = R == 1 ? 1 : 2;
+  static constexpr int LOADS = TT * CH / (R * 64);           // vectors of K (and of V) that a thread loads
+  static constexpr int STEP = R * 64 / CH;                   // tokens from one of them to the next
+  static constexpr int TILE = TT * CH;                       // vectors of a tile
+  static constexpr int LDS = GROUPS * BUFFERS * 2 * TILE;    // vectors in all
+};
+
+template <int DP>
+constexpr int lds_vectors() {
+  constexpr int a = Shape<DP, 1>::LDS, b = Shape<DP, 4>::LDS, c = 4 * 32 * DP / 4;  // the last: the sums at the end
+  return a > b ? (a > c ? a : c) : (b > c ? b : c);
+}
+
+struct Tops {
+  float m[4][32], l[4][32];
+  uint32_t most[4];
+};
+
+// One workgroup's unit: rows x head x piece of the tokens.
+template <int DT, int DP, int R>
+__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, u32x4* lds, Tops& tops) {
+  using S = Shape<DP, R>;
+  constexpr int CH = S::CH, TT = S::TT, KK = DP / 16, DD = DP / 32, NS = TT / 32;
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u, half = lane >> 5;
+
+  uint32_t rest, block, split, head, request = 0;
+  fd_divmod(part.drows, unit, rest, block);
+  fd_divmod(part.dsplits, rest, rest, split);
+  head = rest;
+  if (!shared) fd_divmod(part.drequests, rest, head, request);
+  const uint32_t heads = p.H * p.G;
+
+  // The lane's row: its token, query head, and how far it sees.
+  const uint32_t base_row = (block * R + (R == 1 ? 0 : wave)) * 32;
+  Request q{};
+  if (!shared) {
+    q = request_at(p, request);
+    if (threadIdx.x == 0) fault(p, q.faults);
+  }
+  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
+  uint32_t token, g, limit = 0;
+  bool there;
+  {
+    uint32_t t;
+    fd_divmod(p.dG, base_row + col, t, g);
+    there = t < new_tokens;
+    token = there ? t : 0;
+    if (shared) {
+      if (there) {
+        q = request_at(p, request_of(p.batch, token));
+        if (split == 0 && head == 0 && half == 0) fault(p, q.faults);
+        limit = limit_of(p, q, token);
+      }
+    } else if (there) {
+      token += q.first;
+      limit = limit_of(p, q, token);
+    }
+  }
+  uint32_t most = limit, least = there ? limit : ~0u;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    least = min(least, (uint32_t)__shfl_xor((int)least, d));
+  }
+  least = wave_uniform(least);
+  if constexpr (R > 1) {
+    if (lane == 0) tops.most[wave] = most;
+    __syncthreads();
+    most = max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3]));
+  }
+  most = wave_uniform(most);
+
+  // The unit's tokens.
+  uint32_t t0, t1, row;
+  if (shared) {
+    t0 = split * part.tokens;
+    t1 = prefix_there(p);
+    if (t1 < p.prefix && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
+    row = p.prefix_row;
+  } else {
+    t0 = p.prefix + split * part.tokens;
+    t1 = p.most_tokens;
+    row = wave_uniform(q.row);
+  }
+  t1 = min(min(t1, t0 + part.tokens), most);
+  if (t0 >= t1) {
+    if (p.pieces > 1) return;
+    t1 = t0;
+  }
+  const int32_t* table = p.pool.tables + (uint64_t)row * p.pool.table_len;
+
+  // A page outside the pool is an error of the caller's that costs time only where it happens.
+  bool bad_pages = false;
+  if (t0 < t1) {
+    const uint32_t last = fd_div(p.pool.dbs, t1 - 1);
+    for (uint32_t b = fd_div(p.pool.dbs, t0) + threadIdx.x; b <= last; b += 256) bad_pages |= (uint32_t)table[b] >= p.pool.num_blocks;
+  }
+  bad_pages = __syncthreads_or(bad_pages);
+  if (bad_pages && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
+
+  // The rows' queries: column `col`, elements 16 k + 8 half ...
+  u32x4 query[KK];
+  {
+    const uint16_t* from = p.q + (int64_t)token * p.q_token + (int64_t)(head * p.G + g) * p.q_head;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      const uint32_t at = k * 16 + half * 8;
+      query[k] = there && at < p.D ? *(const KVC_GLOBAL u32x4*)(from + at) : u32x4{0, 0, 0, 0};
+    }
+  }
+
+  // Loads: a thread takes vector `chunk` of tokens first, first + STEP, ... of its group's tile.
+  const uint32_t group = R == 1 ? wave : 0, self = R == 1 ? lane : threadIdx.x;
+  const uint32_t first = self / CH, chunk = self % CH;
+  const uint8_t* keys = (const uint8_t*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2 + chunk * 16;
+  const uint64_t to_values = (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
+  const bool inside = chunk * 8 < p.D;
+  u32x4* const kbuf = lds + group * (S::BUFFERS * 2 * S::TILE);
+  constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a group to its next
+  const uint32_t tiles = (t1 - t0 + NEXT - 1) / NEXT;  // of the workgroup: the last may be beyond a group's tokens
+  const uint32_t start = t0 + group * TT;
+
+  uint32_t page[S::LOADS];
+  u32x4 kreg[S::LOADS], vreg[S::LOADS];
+  auto ask_pages = [&](uint32_t at) {
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      const uint32_t pos = at + first + i * S::STEP;
+      page[i] = pos < t1 ? (uint32_t)table[fd_div(p.pool.dbs, pos)] : ~0u;
+    }
+  };
+  auto ask_tile = [&](uint32_t at) {
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      const uint32_t pos = at + first + i * S::STEP;
+      const uint32_t slot = page[i] * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
+      const uint8_t* k = keys + (uint64_t)slot * p.pool.token_bytes;
+      const bool real = page[i] < p.pool.num_blocks && inside;
+      kreg[i] = *(const KVC_GLOBAL u32x4*)(real ? k : (const uint8_t*)&kZeros);
+      vreg[i] = *(const KVC_GLOBAL u32x4*)(real ? k + to_values : (const uint8_t*)&kZeros);
+    }
+  };
+  auto put_tile = [&](uint32_t buffer) {
+    u32x4* k = kbuf + buffer * (2 * S::TILE);
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      const uint32_t t = first + i * S::STEP, at = t * CH + place<CH>(t, chunk);
+      k[at] = kreg[i];
+      k[S::TILE + at] = vreg[i];
+    }
+  };
+
+  float m = kNone, l = 0.0f;  // of raw products; of this half's tokens
+  f32x16 sum[DD];
+#pragma unroll
+  for (int d = 0; d < DD; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[d][i] = 0.0f;
+
+  auto values = [&](const u32x4* v, int k, int d) {  // V^T of dims 32 d .., tokens 16 k .. in the lane's order
+    u32x4 a;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t t = k * 16 + half * 4 + ((lane & 15u) >> 2) + j * 8;
+      const uint32_t dim = d * 32 + (lane & 16u) + (lane & 3u) * 4;
+      const u32x4* at = v + t * CH + place<CH>(t, dim / 8);
+      const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KVC_LDS*)((const uint16_t*)at + (dim & 4u)));
+      const u32x2 w = __builtin_bit_cast(u32x2, r);
+      a[2 * j] = w.x;
+      a[2 * j + 1] = w.y;
+    }
+    return a;
+  };
+
+  // One tile at position `at` in `buffer`.
+  auto compute = [&](uint32_t at, uint32_t buffer) {
+    const u32x4* k = kbuf + buffer * (2 * S::TILE);
+    const u32x4* v = k + S::TILE;
+    f32x16 s[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < KK; ++e) {
+        const uint32_t t = n * 32 + col;
+        s[n] = mfma<DT>(k[t * CH + place<CH>(t, e * 2 + half)], query[e], s[n]);
+      }
+    }
+    const bool masked = bad_pages || at + TT > min(least, t1);
+    bool clean = false;  // V's values that are not finite are kept out of the product
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t pos = at + n * 32 + (i / 4) * 8 + half * 4 + i % 4;
+          bool seen = pos < limit && pos < t1;
+          if (bad_pages) seen = seen && (uint32_t)table[fd_div(p.pool.dbs, min(pos, t1 - 1))] < p.pool.num_blocks;
+          if (!seen) s[n][i] = kNone;
+        }
+      bool wild = false;
+      for (uint32_t i = lane; i < (uint32_t)S::TILE; i += 64) {
+        const u32x4 w = v[i];
+        wild |= not_finite<DT>(w.x) || not_finite<DT>(w.y) || not_finite<DT>(w.z) || not_finite<DT>(w.w);
+      }
+      clean = __any(wild);
+    }
+    float top = kNone;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = half_max(top);
+    if (__any(top > m)) {
+      const float now = fmaxf(m, top), keep = weight(m * p.scale_log2, now * p.scale_log2);
+      m = now;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DD; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[d][i] *= keep;
+    }
+    const float shift = m == kNone ? 0.0f : m * p.scale_log2;
+    u32x4 w[NS][2];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float a = __builtin_amdgcn_exp2f(fmaf(s[n][i], p.scale_log2, -shift));
+        const float b = __builtin_amdgcn_exp2f(fmaf(s[n][i + 1], p.scale_log2, -shift));
+        l += a + b;
+        w[n][i / 8][(i % 8) / 2] = narrow_pair<DT>(a, b);
+      }
+    if (!clean) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < DD; ++d) sum[d] = mfma<DT>(values(v, n * 2 + h, d), w[n][h], sum[d]);
+    } else {
+      // A weight of 0 does not hide an infinity: rows that see the token get it by an addition, the others not at all.
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < DD; ++d) {
+            u32x4 a = values(v, n * 2 + h, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = only_finite<DT>(a[i]);
+            sum[d] = mfma<DT>(a, w[n][h], sum[d]);
+          }
+      for (uint32_t t = 0; t < (uint32_t)TT; ++t) {
+        const bool seen = at + t < limit && at + t < t1;
+#pragma unroll
+        for (int d = 0; d < DD; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t dim = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
+            const uint32_t x = ((const uint16_t*)(v + t * CH + place<CH>(t, dim / 8)))[dim & 7u];
+            if (seen && not_finite<DT>(x)) sum[d][i] += widen_bits<DT>(x);
+          }
+      }
+    }
+  };
+
+  if (tiles) {
+    ask_pages(start);
+    ask_tile(start);
+    ask_pages(start + NEXT);
+    put_tile(0);
+    ask_tile(start + NEXT);
+    ask_pages(start + 2 * NEXT);
+    if constexpr (R > 1) __syncthreads();
+    for (uint32_t i = 0; i < tiles; ++i) {
+      const uint32_t at = start + i * NEXT;
+      if (at < t1) compute(at, S::BUFFERS == 2 ? i & 1u : 0u);
+      put_tile(S::BUFFERS == 2 ? (i + 1) & 1u : 0u);
+      ask_tile(at + 2 * NEXT);
+      ask_pages(at + 3 * NEXT);
+      if constexpr (R > 1) __syncthreads();
+    }
+  }
+
+  // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
+  __syncthreads();
+  l = half_sum(l);
+  float* const sums = (float*)lds;
+  constexpr uint32_t QD = DP / 4;  // vectors of four sums of a row
+#pragma unroll
+  for (int d = 0; d < DD; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t at = d * 8 + i * 2 + half;
+      *(f32x4*)(sums + ((wave * 32 + col) * QD + (at ^ (col & 15u))) * 4) = f32x4{sum[d][i * 4], sum[d][i * 4 + 1], sum[d][i * 4 + 2], sum[d][i * 4 + 3]};
+    }
+  if (half == 0) {
+    tops.m[wave][col] = m != kNone ? m * p.scale_log2 : l == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
+    tops.l[wave][col] = l;
+  }
+  __syncthreads();
+  constexpr uint32_t SIDE = 64 / QD == 0 ? 1 : 64 / QD;  // rows that a wave writes at a time
+  constexpr uint32_t MINE = R == 1 ? 8 : 32;             // rows that it writes in all
+  const uint32_t begin = R == 1 ? wave * 8 : 0, at = lane % QD;
+  const uint32_t piece = shared ? split : p.part[0].splits + split;
+#pragma unroll 2
+  for (uint32_t i = 0; i < MINE; i += SIDE) {
+    const uint32_t r = begin + i + lane / QD;
+    uint32_t t, gg;
+    fd_divmod(p.dG, base_row + r, t, gg);
+    if (t >= new_tokens) continue;
+    const uint32_t row_token = shared ? t : q.first + t;
+    f32x4 o = {0, 0, 0, 0};
+    float top = kNone, total = 0.0f;
+    if constexpr (R == 1) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = fmaxf(top, tops.m[k][r]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = weight(tops.m[k][r], top);
+        total += x * tops.l[k][r];
+        const f32x4 v = *(const f32x4*)(sums + ((k * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+        if (tops.m[k][r] != kNone) o += x * v;
+      }
+    } else {
+      top = tops.m[wave][r];
+      total = tops.l[wave][r];
+      o = *(const f32x4*)(sums + ((wave * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+    }
+    const uint64_t slot = ((uint64_t)piece * p.batch.n_new + row_token) * heads + head * p.G + gg;
+    if (p.pieces > 1) {
+      if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
+      if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
+    } else {
+      const float x = total == 0.0f ? 0.0f : 1.0f / total;
+      if (at * 4 < p.D) {
+        const u32x2 w = {narrow_pair<DT>(o.x * x, o.y * x), narrow_pair<DT>(o.z * x, o.w * x)};
+        *(KVC_GLOBAL u32x2*)(p.out + (int64_t)row_token * p.o_token + (int64_t)(head * p.G + gg) * p.o_head + at * 4) = w;
+      }
+      if (at == 0 && p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+    }
+  }
+}
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
+  __shared__ u32x4 lds[lds_vectors<DP>()];
+  __shared__ Tops tops;
+  // Workgroups go to the XCDs round-robin; units that follow one another (blocks of rows of the same tokens) share one.
+  const uint32_t per = gridDim.x / 8, unit = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
+  const bool shared = unit < p.part[0].units;
+  if (!shared && unit - p.part[0].units >= p.part[1].units) return;
+  const AttendPart& part = p.part[shared ? 0 : 1];
+  const uint32_t u = shared ? unit : unit - p.part[0].units;
+  if (part.waves == 1) attend_unit<DT, DP, 1>(p, part, shared, u, lds, tops);
+  else attend_unit<DT, DP, 4>(p, part, shared, u, lds, tops);
+}
+
+// Joins a row's pieces.  A row's QD lanes take four elements each; a workgroup takes 256 / QD rows.
+template <int DT, int DP>
+__global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
+  constexpr uint32_t QD = DP / 4;
+  const uint32_t heads = p.H * p.G, at = threadIdx.x % QD;
+  const uint64_t line = (uint64_t)blockIdx.x * (256 / QD) + threadIdx.x / QD;  // token and head
+  const uint64_t lines = (uint64_t)p.batch.n_new * heads;
+  if (line >= lines) return;
+  const uint32_t token = (uint32_t)(line / heads), head = (uint32_t)(line - (uint64_t)token * heads);
+  const Request q = request_at(p, request_of(p.batch, token));
+  const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
+  // pieces that hold something: those that begin below what the row sees
+  const uint32_t a = p.part[0].splits ? (prefix + p.part[0].tokens - 1) / p.part[0].tokens : 0;
+  const uint32_t n = p.part[1].splits && limit > p.prefix && token - q.first < p.batch.most_new ? (limit - p.prefix + p.part[1].tokens - 1) / p.part[1].tokens : 0;
+  float top = kNone, total = 0.0f;
+  f32x4 o = {0, 0, 0, 0};
+  for (uint32_t i = 0; i < a + n; ++i) {
+    const uint64_t slot = (uint64_t)(i < a ? i : p.part[0].splits + i - a) * lines + line;
+    const f32x2 t = *(const KVC_GLOBAL f32x2*)(p.tops + slot * 2);
+    const f32x4 v = at * 4 < p.D ? *(const KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) : f32x4{0, 0, 0, 0};
+    if (t.x == kNone) continue;
+    const float now = fmaxf(top, t.x), x = weight(top, now), y = weight(t.x, now);
+    total = total * x + t.y * y;
+    o = o * x + v * y;
+    top = now;
+  }
+  const float x = total == 0.0f ? 0.0f : 1.0f / total;
+  if (at * 4 < p.D) {
+    const u32x2 w = {narrow_pair<DT>(o.x * x, o.y * x), narrow_pair<DT>(o.z * x, o.w * x)};
+    *(KVC_GLOBAL u32x2*)(p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4) = w;
+  }
+  if (at == 0 && p.lse) p.lse[line] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
+template <int DT, int DP>
+kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
+  const uint32_t units = p.part[0].units + p.part[1].units;
+  if (units) hipLaunchKernelGGL((attend_kernel<DT, DP>), dim3((units + 7) / 8 * 8), dim3(256), 0, stream, p);
+  if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
+  if (p.pieces != 1) {  // (no piece at all: every row is empty)
+    const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = 256 / (DP / 4);
+    hipLaunchKernelGGL((join_kernel<DT, DP>), dim3((uint32_t)((lines + each - 1) / each)), dim3(256), 0, stream, p);
+  }
+  return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_RUNTIME;
+}
+
+}  // namespace
+
+kvc_status plan_attend(AttendParams& p) {
+  p.pieces = 0;
+  for (int i = 0; i < 2; ++i) {
+    AttendPart& a = p.part[i];
+    a = AttendPart{};
+    const uint64_t tokens = i == 0 ? p.prefix : p.most_tokens - p.prefix;
+    const uint64_t rows = (uint64_t)(i == 0 ? p.batch.n_new : p.batch.most_new) * p.G;
+    a.waves = rows <= 32 ? 1 : 4;
+    const uint64_t blocks = (rows + 32 * a.waves - 1) / (32 * a.waves);
+    const uint64_t whole = blocks * p.H * (i == 0 ? 1 : p.batch.n_requests);
+    a.drows = a.dsplits = a.drequests = make_fastdiv(1);
+    if (tokens == 0) continue;
+    if (whole >> 31) return KVC_ERR_UNSUPPORTED;
+    uint64_t splits = 512 / whole;
+    if (splits < 1) splits = 1;
+    uint64_t each = (tokens + splits - 1) / splits;
+    const uint64_t least = 128;
+    each = (each + least - 1) / least * least;
+    splits = (tokens + each - 1) / each;
+    if (whole * splits >> 31) return KVC_ERR_UNSUPPORTED;
+    a.row_blocks = (uint32_t)blocks;
+    a.splits = (uint32_t)splits;
+    a.tokens = (uint32_t)each;
+    a.units = (uint32_t)(whole * splits);
+    a.drows = make_fastdiv(a.row_blocks);
+    a.dsplits = make_fastdiv(a.splits);
+    a.drequests = make_fastdiv(p.batch.n_requests);
+    p.pieces += a.splits;
+  }
+  if ((uint64_t)p.part[0].units + p.part[1].units > 0x7ffffff0u) return KVC_ERR_UNSUPPORTED;
+  return KVC_OK;
+}
+
+kvc_status launch_attend(const AttendParams& p, hipStream_t stream) {
+  const bool half = p.dtype == KVC_F16;
+  if (p.D <= 64) return half ? launch_of<KVC_F16, 64>(p, stream) : launch_of<KVC_BF16, 64>(p, stream);
+  if (p.D <= 128) return half ? launch_of<KVC_F16, 128>(p, stream) : launch_of<KVC_BF16, 128>(p, stream);
+  return half ? launch_of<KVC_F16, 256>(p, stream) : launch_of<KVC_BF16, 256>(p, stream);
+}
+
+}  // namespace kvc

@@ -44,6 +44,40 @@ class HostChunk(C.Structure):
     _fields_ = [("host_blob", C.c_void_p), ("bytes", C.c_size_t), ("n_tokens", C.c_int64)]
 
 
+class Pool(C.Structure):
+    """kvc_pool.  Pointers of device memory as numbers, None for NULL."""
+    _fields_ = [("struct_size", C.c_uint32), ("abi_version", C.c_uint32)] + [
+        (n, C.c_int32) for n in ("num_layers", "num_kv_heads", "head_dim", "dtype")] + [
+        ("num_blocks", C.c_int64), ("n_rows", C.c_int64), ("block_size", C.c_int32), ("table_len", C.c_int32)] + [
+        (n, C.c_void_p) for n in ("d_layer_cache", "d_tables", "d_lens", "d_refs", "d_err")]
+
+    def __init__(self, num_layers, num_kv_heads, head_dim, dtype, num_blocks, block_size, n_rows, table_len, layer_cache_ptrs_dev,
+                 tables_ptr, lens_ptr, refs_ptr=None, err_ptr=None):
+        super().__init__(C.sizeof(Pool), KVC_ABI_VERSION, num_layers, num_kv_heads, head_dim, dtype, num_blocks, n_rows, block_size,
+                         table_len, layer_cache_ptrs_dev, tables_ptr, lens_ptr, refs_ptr, err_ptr)
+
+
+class Batch(C.Structure):
+    """kvc_batch"""
+    _fields_ = [("struct_size", C.c_uint32), ("abi_version", C.c_uint32), ("n_requests", C.c_int32), ("most_new", C.c_int32),
+                ("n_new", C.c_int64), ("d_rows", C.c_void_p), ("d_starts", C.c_void_p)]
+
+    def __init__(self, n_requests, n_new=None, most_new=1, rows_ptr=None, starts_ptr=None):
+        super().__init__(C.sizeof(Batch), KVC_ABI_VERSION, n_requests, most_new, n_requests if n_new is None else n_new, rows_ptr,
+                         starts_ptr)
+
+
+class Attention(C.Structure):
+    """kvc_attention; strides are (token, head) in elements."""
+    _fields_ = [("struct_size", C.c_uint32), ("abi_version", C.c_uint32), ("num_q_heads", C.c_int32), ("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("most_tokens", "prefix_tokens", "prefix_row", "q_token_stride", "q_head_stride", "out_token_stride",
+                                 "out_head_stride")]
+
+    def __init__(self, num_q_heads, scale, most_tokens, prefix_tokens, prefix_row, q_strides, out_strides):
+        super().__init__(C.sizeof(Attention), KVC_ABI_VERSION, num_q_heads, scale, most_tokens, prefix_tokens, prefix_row, *q_strides,
+                         *out_strides)
+
+
 def lib_path():
     return _LIB_PATH
 
@@ -109,6 +143,19 @@ def load(path=None):
     lib.kvc_tiling_costs_workspace.restype = sz
     lib.kvc_tiling_costs.argtypes = [LP, vp, Strides, i64, i32, ip, ip, ip, i32, i32, vp, sz, vp, vp]
     lib.kvc_probe_expand.argtypes = [vp, vp, sz, vp, sz, i32, i32, vp]
+    pp, bp, ap = C.POINTER(Pool), C.POINTER(Batch), C.POINTER(Attention)
+    lib.kvc_pool_validate.argtypes = [pp]
+    lib.kvc_pages_workspace.argtypes = [pp]
+    lib.kvc_pages_workspace.restype = sz
+    lib.kvc_pages_copy.argtypes = [pp, vp, vp, i64, vp]
+    lib.kvc_pages_fork.argtypes = [pp, vp, vp, i64, vp, sz, vp]
+    lib.kvc_pages_grow.argtypes = [pp, vp, vp, i64, vp, sz, vp]
+    lib.kvc_pages_free.argtypes = [pp, vp, i64, vp]
+    lib.kvc_pages_compact.argtypes = [pp, vp, vp, vp, vp, sz, vp]
+    lib.kvc_append_paged.argtypes = [pp, bp, i32, vp, vp, i64, vp]
+    lib.kvc_attention_workspace.argtypes = [pp, bp, ap]
+    lib.kvc_attention_workspace.restype = sz
+    lib.kvc_attend_paged.argtypes = [pp, bp, ap, i32, vp, vp, vp, vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -335,3 +382,60 @@ def est_bandwidth(last_chunk_size, last_transmission_delay):
 def layout_set_resolution(layout, width, height):
     """Sets the tile grid of `layout` for frames of at most width x height pixels; returns the status."""
     return load().kvc_layout_set_resolution(C.byref(layout), width, height)
+
+
+# ---- serving on a restored cache
+
+KVC_FAULT_PAGE, KVC_FAULT_LIST, KVC_FAULT_NO_ROOM = 1, 2, 4
+
+
+def pool_validate(pool):
+    return load().kvc_pool_validate(C.byref(pool))
+
+
+def pages_workspace(pool):
+    """Bytes of the workspace of fork, grow and compact."""
+    n = load().kvc_pages_workspace(C.byref(pool))
+    if n == 0:
+        raise KvcError(pool_validate(pool), "kvc_pages_workspace")
+    return n
+
+
+def kvc_pages_copy(pool, src_ptr, dst_ptr, n, stream=0):
+    _check(load().kvc_pages_copy(C.byref(pool), src_ptr, dst_ptr, n, stream), "kvc_pages_copy")
+
+
+def kvc_pages_fork(pool, parents_ptr, children_ptr, n, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().kvc_pages_fork(C.byref(pool), parents_ptr, children_ptr, n, workspace_ptr, workspace_bytes, stream), "kvc_pages_fork")
+
+
+def kvc_pages_grow(pool, rows_ptr, counts_ptr, n, workspace_ptr, workspace_bytes, stream=0):
+    """counts_ptr None: every row gets one token."""
+    _check(load().kvc_pages_grow(C.byref(pool), rows_ptr, counts_ptr, n, workspace_ptr, workspace_bytes, stream), "kvc_pages_grow")
+
+
+def kvc_pages_free(pool, rows_ptr, n, stream=0):
+    _check(load().kvc_pages_free(C.byref(pool), rows_ptr, n, stream), "kvc_pages_free")
+
+
+def kvc_pages_compact(pool, map_ptr, tables_out_ptr, refs_out_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().kvc_pages_compact(C.byref(pool), map_ptr, tables_out_ptr, refs_out_ptr, workspace_ptr, workspace_bytes, stream),
+           "kvc_pages_compact")
+
+
+def kvc_append_paged(pool, batch, layer, k_ptr, v_ptr, token_stride, stream=0):
+    _check(load().kvc_append_paged(C.byref(pool), C.byref(batch), layer, k_ptr, v_ptr, token_stride, stream), "kvc_append_paged")
+
+
+def attention_workspace(pool, batch, attention):
+    """Bytes of the workspace of one kvc_attend_paged call."""
+    n = load().kvc_attention_workspace(C.byref(pool), C.byref(batch), C.byref(attention))
+    if n == C.c_size_t(-1).value:
+        raise KvcError(1, "kvc_attention_workspace")
+    return n
+
+
+def kvc_attend_paged(pool, batch, attention, layer, q_ptr, out_ptr, lse_ptr, workspace_ptr, workspace_bytes, stream=0):
+    """lse_ptr None: the logarithms of the sums are not wanted."""
+    _check(load().kvc_attend_paged(C.byref(pool), C.byref(batch), C.byref(attention), layer, q_ptr, out_ptr, lse_ptr, workspace_ptr,
+                                   workspace_bytes, stream), "kvc_attend_paged")
