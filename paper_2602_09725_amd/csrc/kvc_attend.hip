@@ -162,11 +162,265 @@ struct Tops {
   uint32_t most[4];
 };
 
+// What a wave knows of its unit.
+struct Unit {
+  const uint8_t *keys, *values;  // of the head: slot 0
+  const int32_t* table;
+  uint32_t t0, t1, limit, least;  // tokens of the unit; those below `limit` are seen by the lane's row, below `least` by all of them
+  bool bad_pages;
+};
+
+// Running state of a lane's row: a number near the largest product so far, sum of this half's weights, sums of values.
+template <int DP>
+struct State {
+  float m, l;
+  f32x16 sum[DP / 32];
+};
+
+__device__ __forceinline__ void wait_loads(int left) {
+  // (a number in the instruction: the callers' are constants)
+  if (left == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  else if (left == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+  else if (left == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+  else if (left == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  else if (left == 9) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+  else if (left == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  else if (left == 17) asm volatile("s_waitcnt vmcnt(17)" ::: "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// Page of token `lane` (of lane % 32 in a tile of 32) of the tile at position `at`.
+template <int TT>
+__device__ __forceinline__ uint32_t page_of_lane(const AttendParams& p, const Unit& u, uint32_t at) {
+  const uint32_t pos = at + (threadIdx.x & (uint32_t)(TT - 1));
+  const uint32_t page = (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))];  // (always one load: waits count it)
+  return pos < u.t1 ? page : ~0u;
+}
+
+// Where a thread's vectors of a tile come from: offsets of K's and V's rows, ~0 for a token that is not there.
+template <int DP, int R>
+struct Sources {
+  uint64_t at[Shape<DP, R>::LOADS];
+};
+
+template <int DP, int R>
+__device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, const Unit& u, uint32_t at, uint32_t page) {
+  using S = Shape<DP, R>;
+  const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
+  const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
+  uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
+  if (page >= p.pool.num_blocks) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  Sources<DP, R> s;
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i) {
+    const uint32_t t = first + i * S::STEP, chunk = place<S::CH>(t, self % S::CH);
+    const uint32_t from = (uint32_t)__shfl((int)slot, (int)t);
+    const bool real = from != ~0u && chunk * 8 < p.D;
+    s.at[i] = real ? (uint64_t)from * p.pool.token_bytes + chunk * 16 : ~0ull;
+  }
+  return s;
+}
+
+// Loads a tile's K or V from memory straight into LDS: a wave's 64 vectors of one instruction lie side by side there.
+template <int DP, int R>
+__device__ __forceinline__ void load_tile(const uint8_t* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
+  using S = Shape<DP, R>;
+  const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i) {
+    const uint8_t* from = s.at[i] != ~0ull ? base + s.at[i] : (const uint8_t*)&kZeros;
+    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)from, (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
+  }
+}
+
+// V^T of dims 32 d .., tokens 16 k .. in the lane's order.
+template <int CH>
+__device__ __forceinline__ u32x4 values_at(const u32x4 KVC_LDS* v, int k, int d) {
+  const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
+  u32x4 a;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t t = k * 16 + half * 4 + ((lane & 15u) >> 2) + j * 8;
+    const uint32_t dim = d * 32 + (lane & 16u) + (lane & 3u) * 4;
+    const u32x4 KVC_LDS* at = v + t * CH + place<CH>(t, dim / 8);
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KVC_LDS*)((const uint16_t KVC_LDS*)at + (dim & 4u))));
+    a[2 * j] = w.x;
+    a[2 * j + 1] = w.y;
+  }
+  return a;
+}
+
+// S^T of a tile.
+template <int DT, int DP, int NS>
+__device__ __forceinline__ void products(const u32x4 KVC_LDS* k, const u32x4 (&query)[DP / 16], f32x16 (&s)[NS]) {
+  constexpr int CH = DP / 8;
+  const uint32_t lane = threadIdx.x & 63u, col = lane & 31u, half = lane >> 5;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < DP / 16; ++e) {
+      const uint32_t t = n * 32 + col;
+      s[n] = mfma<DT>(k[t * CH + place<CH>(t, e * 2 + half)], query[e], s[n]);
+    }
+  }
+}
+
+// -inf in the place of products that the lane's row does not see, in a tile at position `at`.
+template <int NS>
+__device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint32_t at, f32x16 (&s)[NS]) {
+  const uint32_t half = (threadIdx.x >> 5) & 1u;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t pos = at + n * 32 + (i / 4) * 8 + half * 4 + i % 4;
+      bool seen = pos < u.limit && pos < u.t1;
+      if (u.bad_pages) seen = seen && (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))] < p.pool.num_blocks;
+      if (!seen) s[n][i] = kNone;
+    }
+}
+
+// Weights of a tile, rounded to the type, from its products; the state is moved to them.
+template <int DT, int DP, int NS>
+__device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, const f32x16 (&s)[NS], u32x4 (&w)[NS][2]) {
+  float top = kNone;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+  top = half_max(top);
+  // The number subtracted need not be the maximum: as long as no weight exceeds 2^8, sums and types hold them as well.
+  if (__any(top > x.m + p.slack)) {
+    const float now = fmaxf(x.m, top), keep = weight(x.m * p.scale_log2, now * p.scale_log2);
+    x.m = now;
+    x.l *= keep;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x.sum[d][i] *= keep;
+  }
+  const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float a = __builtin_amdgcn_exp2f(fmaf(s[n][i], p.scale_log2, -shift));
+      const float b = __builtin_amdgcn_exp2f(fmaf(s[n][i + 1], p.scale_log2, -shift));
+      x.l += a + b;
+      w[n][i / 8][(i % 8) / 2] = narrow_pair<DT>(a, b);
+    }
+}
+
+template <int DT, int DP, int NS>
+__device__ __forceinline__ void add_values(State<DP>& x, const u32x4 KVC_LDS* v, const u32x4 (&w)[NS][2]) {
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) x.sum[d] = mfma<DT>(values_at<DP / 8>(v, n * 2 + h, d), w[n][h], x.sum[d]);
+}
+
+// The same for a tile that not all rows see all of.  A weight of 0 does not hide an infinity: values that are not finite are kept
+// out of the product, rows that see their token get them by an addition, the others not at all.
+template <int DT, int DP, int NS>
+__device__ __forceinline__ void add_seen_values(const Unit& u, uint32_t at, State<DP>& x, const u32x4 KVC_LDS* v, const u32x4 (&w)[NS][2]) {
+  constexpr int CH = DP / 8, TT = NS * 32;
+  const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
+  bool wild = false;
+  for (uint32_t i = lane; i < (uint32_t)(TT * CH); i += 64) {
+    const u32x4 y = v[i];
+    wild |= not_finite<DT>(y.x) || not_finite<DT>(y.y) || not_finite<DT>(y.z) || not_finite<DT>(y.w);
+  }
+  if (!__any(wild)) {
+    add_values<DT, DP, NS>(x, v, w);
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        u32x4 a = values_at<CH>(v, n * 2 + h, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = only_finite<DT>(a[i]);
+        x.sum[d] = mfma<DT>(a, w[n][h], x.sum[d]);
+      }
+  for (uint32_t t = 0; t < (uint32_t)TT; ++t) {
+    const bool seen = at + t < u.limit && at + t < u.t1;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t dim = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        const uint32_t y = ((const uint16_t KVC_LDS*)(v + t * CH + place<CH>(t, dim / 8)))[dim & 7u];
+        if (seen && not_finite<DT>(y)) x.sum[d][i] += widen_bits<DT>(y);
+      }
+  }
+}
+
+template <int TT>
+__device__ __forceinline__ bool is_masked(const Unit& u, uint32_t at) {
+  return u.bad_pages || at + TT > min(u.least, u.t1);
+}
+
+// One step of four waves side by side: the tile at `at` lies in (k, v), the next one goes to (k2, v2).
+template <int DT, int DP>
+__device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, uint32_t at, uint32_t& page, const u32x4 (&query)[DP / 16], State<DP>& x,
+                                             const u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
+                                             u32x4 KVC_LDS* __restrict__ k2, u32x4 KVC_LDS* __restrict__ v2) {
+  using S = Shape<DP, 4>;
+  constexpr int NS = S::TT / 32;
+  const Sources<DP, 4> from = sources_of<DP, 4>(p, u, at + S::TT, page);
+  load_tile<DP, 4>(u.keys, from, k2);
+  load_tile<DP, 4>(u.values, from, v2);
+  page = page_of_lane<S::TT>(p, u, at + 2 * S::TT);
+  f32x16 s[NS];
+  u32x4 w[NS][2];
+  products<DT, DP, NS>(k, query, s);
+  if (is_masked<S::TT>(u, at)) {
+    mask<NS>(p, u, at, s);
+    weights<DT, DP, NS>(p, x, s, w);
+    add_seen_values<DT, DP, NS>(u, at, x, v, w);
+  } else {
+    weights<DT, DP, NS>(p, x, s, w);
+    add_values<DT, DP, NS>(x, v, w);
+  }
+}
+
+// One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
+// follow them as soon as each has been read.
+template <int DT, int DP>
+__device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u, uint32_t at, uint32_t next, uint32_t& page, const u32x4 (&query)[DP / 16],
+                                            State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
+  using S = Shape<DP, 1>;
+  constexpr int N = S::LOADS;
+  f32x16 s[1];
+  u32x4 w[1][2];
+  wait_loads(N);  // K is there, V may be on its way
+  products<DT, DP, 1>(k, query, s);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at + next, page);
+  load_tile<DP, 1>(u.keys, from, k);
+  page = page_of_lane<S::TT>(p, u, at + 2 * next);
+  const bool masked = is_masked<S::TT>(u, at);
+  if (masked) mask<1>(p, u, at, s);
+  weights<DT, DP, 1>(p, x, s, w);
+  wait_loads(N + 1);  // V is there; the next K and its successor's page follow
+  if (masked) add_seen_values<DT, DP, 1>(u, at, x, v, w);
+  else add_values<DT, DP, 1>(x, v, w);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  load_tile<DP, 1>(u.values, from, v);
+}
+
 // One workgroup's unit: rows x head x piece of the tokens.
 template <int DT, int DP, int R>
-__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, u32x4* lds, Tops& tops) {
+__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, u32x4 KVC_LDS* lds, Tops& tops) {
   using S = Shape<DP, R>;
-  constexpr int CH = S::CH, TT = S::TT, KK = DP / 16, DD = DP / 32, NS = TT / 32;
+  constexpr int TT = S::TT, KK = DP / 16, DD = DP / 32;
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u, half = lane >> 5;
 
   uint32_t rest, block, split, head, request = 0;
@@ -233,16 +487,23 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     if (p.pieces > 1) return;
     t1 = t0;
   }
-  const int32_t* table = p.pool.tables + (uint64_t)row * p.pool.table_len;
+  Unit u;
+  u.table = p.pool.tables + (uint64_t)row * p.pool.table_len;
+  u.t0 = t0;
+  u.t1 = t1;
+  u.limit = limit;
+  u.least = least;
+  u.keys = (const uint8_t*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
+  u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
 
   // A page outside the pool is an error of the caller's that costs time only where it happens.
   bool bad_pages = false;
   if (t0 < t1) {
     const uint32_t last = fd_div(p.pool.dbs, t1 - 1);
-    for (uint32_t b = fd_div(p.pool.dbs, t0) + threadIdx.x; b <= last; b += 256) bad_pages |= (uint32_t)table[b] >= p.pool.num_blocks;
+    for (uint32_t b = fd_div(p.pool.dbs, t0) + threadIdx.x; b <= last; b += 256) bad_pages |= (uint32_t)u.table[b] >= p.pool.num_blocks;
   }
-  bad_pages = __syncthreads_or(bad_pages);
-  if (bad_pages && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
+  u.bad_pages = __syncthreads_or(bad_pages);
+  if (u.bad_pages && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
 
   // The rows' queries: column `col`, elements 16 k + 8 half ...
   u32x4 query[KK];
@@ -255,192 +516,60 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     }
   }
 
-  // Loads: a thread takes vector `chunk` of tokens first, first + STEP, ... of its group's tile.
-  const uint32_t group = R == 1 ? wave : 0, self = R == 1 ? lane : threadIdx.x;
-  const uint32_t first = self / CH, chunk = self % CH;
-  const uint8_t* keys = (const uint8_t*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2 + chunk * 16;
-  const uint64_t to_values = (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
-  const bool inside = chunk * 8 < p.D;
-  u32x4* const kbuf = lds + group * (S::BUFFERS * 2 * S::TILE);
-  constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a group to its next
-  const uint32_t tiles = (t1 - t0 + NEXT - 1) / NEXT;  // of the workgroup: the last may be beyond a group's tokens
-  const uint32_t start = t0 + group * TT;
-
-  uint32_t page[S::LOADS];
-  u32x4 kreg[S::LOADS], vreg[S::LOADS];
-  auto ask_pages = [&](uint32_t at) {
-#pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
-      const uint32_t pos = at + first + i * S::STEP;
-      page[i] = pos < t1 ? (uint32_t)table[fd_div(p.pool.dbs, pos)] : ~0u;
-    }
-  };
-  auto ask_tile = [&](uint32_t at) {
-#pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
-      const uint32_t pos = at + first + i * S::STEP;
-      const uint32_t slot = page[i] * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-      const uint8_t* k = keys + (uint64_t)slot * p.pool.token_bytes;
-      const bool real = page[i] < p.pool.num_blocks && inside;
-      kreg[i] = *(const KVC_GLOBAL u32x4*)(real ? k : (const uint8_t*)&kZeros);
-      vreg[i] = *(const KVC_GLOBAL u32x4*)(real ? k + to_values : (const uint8_t*)&kZeros);
-    }
-  };
-  auto put_tile = [&](uint32_t buffer) {
-    u32x4* k = kbuf + buffer * (2 * S::TILE);
-#pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
-      const uint32_t t = first + i * S::STEP, at = t * CH + place<CH>(t, chunk);
-      k[at] = kreg[i];
-      k[S::TILE + at] = vreg[i];
-    }
-  };
-
-  float m = kNone, l = 0.0f;  // of raw products; of this half's tokens
-  f32x16 sum[DD];
+  State<DP> x;
+  x.m = kNone;
+  x.l = 0.0f;
 #pragma unroll
   for (int d = 0; d < DD; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum[d][i] = 0.0f;
-
-  auto values = [&](const u32x4* v, int k, int d) {  // V^T of dims 32 d .., tokens 16 k .. in the lane's order
-    u32x4 a;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t t = k * 16 + half * 4 + ((lane & 15u) >> 2) + j * 8;
-      const uint32_t dim = d * 32 + (lane & 16u) + (lane & 3u) * 4;
-      const u32x4* at = v + t * CH + place<CH>(t, dim / 8);
-      const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KVC_LDS*)((const uint16_t*)at + (dim & 4u)));
-      const u32x2 w = __builtin_bit_cast(u32x2, r);
-      a[2 * j] = w.x;
-      a[2 * j + 1] = w.y;
+    for (int i = 0; i < 16; ++i) x.sum[d][i] = 0.0f;
+  if constexpr (R == 1) {
+    constexpr uint32_t NEXT = 4 * TT;
+    u32x4 KVC_LDS* const k = lds + wave_uniform(wave) * (2 * S::TILE);
+    u32x4 KVC_LDS* const v = k + S::TILE;
+    uint32_t at = t0 + wave_uniform(wave) * TT;
+    if (at < t1) {
+      uint32_t page = page_of_lane<TT>(p, u, at);
+      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at, page);
+      load_tile<DP, 1>(u.keys, from, k);
+      page = page_of_lane<TT>(p, u, at + NEXT);
+      load_tile<DP, 1>(u.values, from, v);
+      for (; at < t1; at += NEXT) step_of_one<DT, DP>(p, u, at, NEXT, page, query, x, k, v);
+      wait_loads(0);  // (of tiles that are not there: zeros, but they may not land on the sums)
     }
-    return a;
-  };
-
-  // One tile at position `at` in `buffer`.
-  auto compute = [&](uint32_t at, uint32_t buffer) {
-    const u32x4* k = kbuf + buffer * (2 * S::TILE);
-    const u32x4* v = k + S::TILE;
-    f32x16 s[NS];
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
-#pragma unroll
-      for (int e = 0; e < KK; ++e) {
-        const uint32_t t = n * 32 + col;
-        s[n] = mfma<DT>(k[t * CH + place<CH>(t, e * 2 + half)], query[e], s[n]);
+  } else {
+    u32x4 KVC_LDS *const k0 = lds, *const v0 = lds + S::TILE, *const k1 = lds + 2 * S::TILE, *const v1 = lds + 3 * S::TILE;
+    if (t0 < t1) {
+      uint32_t page = page_of_lane<TT>(p, u, t0);
+      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, page);
+      load_tile<DP, 4>(u.keys, from, k0);
+      load_tile<DP, 4>(u.values, from, v0);
+      page = page_of_lane<TT>(p, u, t0 + TT);
+      for (uint32_t at = t0; at < t1;) {
+        wait_loads(0);
+        __syncthreads();
+        step_of_four<DT, DP>(p, u, at, page, query, x, k0, v0, k1, v1);
+        if ((at += TT) >= t1) break;
+        wait_loads(0);
+        __syncthreads();
+        step_of_four<DT, DP>(p, u, at, page, query, x, k1, v1, k0, v0);
+        at += TT;
       }
-    }
-    const bool masked = bad_pages || at + TT > min(least, t1);
-    bool clean = false;  // V's values that are not finite are kept out of the product
-    if (masked) {
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t pos = at + n * 32 + (i / 4) * 8 + half * 4 + i % 4;
-          bool seen = pos < limit && pos < t1;
-          if (bad_pages) seen = seen && (uint32_t)table[fd_div(p.pool.dbs, min(pos, t1 - 1))] < p.pool.num_blocks;
-          if (!seen) s[n][i] = kNone;
-        }
-      bool wild = false;
-      for (uint32_t i = lane; i < (uint32_t)S::TILE; i += 64) {
-        const u32x4 w = v[i];
-        wild |= not_finite<DT>(w.x) || not_finite<DT>(w.y) || not_finite<DT>(w.z) || not_finite<DT>(w.w);
-      }
-      clean = __any(wild);
-    }
-    float top = kNone;
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-    top = half_max(top);
-    if (__any(top > m)) {
-      const float now = fmaxf(m, top), keep = weight(m * p.scale_log2, now * p.scale_log2);
-      m = now;
-      l *= keep;
-#pragma unroll
-      for (int d = 0; d < DD; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[d][i] *= keep;
-    }
-    const float shift = m == kNone ? 0.0f : m * p.scale_log2;
-    u32x4 w[NS][2];
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float a = __builtin_amdgcn_exp2f(fmaf(s[n][i], p.scale_log2, -shift));
-        const float b = __builtin_amdgcn_exp2f(fmaf(s[n][i + 1], p.scale_log2, -shift));
-        l += a + b;
-        w[n][i / 8][(i % 8) / 2] = narrow_pair<DT>(a, b);
-      }
-    if (!clean) {
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int d = 0; d < DD; ++d) sum[d] = mfma<DT>(values(v, n * 2 + h, d), w[n][h], sum[d]);
-    } else {
-      // A weight of 0 does not hide an infinity: rows that see the token get it by an addition, the others not at all.
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int d = 0; d < DD; ++d) {
-            u32x4 a = values(v, n * 2 + h, d);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = only_finite<DT>(a[i]);
-            sum[d] = mfma<DT>(a, w[n][h], sum[d]);
-          }
-      for (uint32_t t = 0; t < (uint32_t)TT; ++t) {
-        const bool seen = at + t < limit && at + t < t1;
-#pragma unroll
-        for (int d = 0; d < DD; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint32_t dim = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
-            const uint32_t x = ((const uint16_t*)(v + t * CH + place<CH>(t, dim / 8)))[dim & 7u];
-            if (seen && not_finite<DT>(x)) sum[d][i] += widen_bits<DT>(x);
-          }
-      }
-    }
-  };
-
-  if (tiles) {
-    ask_pages(start);
-    ask_tile(start);
-    ask_pages(start + NEXT);
-    put_tile(0);
-    ask_tile(start + NEXT);
-    ask_pages(start + 2 * NEXT);
-    if constexpr (R > 1) __syncthreads();
-    for (uint32_t i = 0; i < tiles; ++i) {
-      const uint32_t at = start + i * NEXT;
-      if (at < t1) compute(at, S::BUFFERS == 2 ? i & 1u : 0u);
-      put_tile(S::BUFFERS == 2 ? (i + 1) & 1u : 0u);
-      ask_tile(at + 2 * NEXT);
-      ask_pages(at + 3 * NEXT);
-      if constexpr (R > 1) __syncthreads();
+      wait_loads(0);
     }
   }
-
+  float m = x.m, l = x.l;
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   __syncthreads();
   l = half_sum(l);
-  float* const sums = (float*)lds;
+  float KVC_LDS* const sums = (float KVC_LDS*)lds;
   constexpr uint32_t QD = DP / 4;  // vectors of four sums of a row
 #pragma unroll
   for (int d = 0; d < DD; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t at = d * 8 + i * 2 + half;
-      *(f32x4*)(sums + ((wave * 32 + col) * QD + (at ^ (col & 15u))) * 4) = f32x4{sum[d][i * 4], sum[d][i * 4 + 1], sum[d][i * 4 + 2], sum[d][i * 4 + 3]};
+      *(f32x4 KVC_LDS*)(sums + ((wave * 32 + col) * QD + (at ^ (col & 15u))) * 4) = f32x4{x.sum[d][i * 4], x.sum[d][i * 4 + 1], x.sum[d][i * 4 + 2], x.sum[d][i * 4 + 3]};
     }
   if (half == 0) {
     tops.m[wave][col] = m != kNone ? m * p.scale_log2 : l == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
@@ -465,24 +594,24 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       for (int k = 0; k < 4; ++k) top = fmaxf(top, tops.m[k][r]);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float x = weight(tops.m[k][r], top);
-        total += x * tops.l[k][r];
-        const f32x4 v = *(const f32x4*)(sums + ((k * 32 + r) * QD + (at ^ (r & 15u))) * 4);
-        if (tops.m[k][r] != kNone) o += x * v;
+        const float y = weight(tops.m[k][r], top);
+        total += y * tops.l[k][r];
+        const f32x4 v = *(const f32x4 KVC_LDS*)(sums + ((k * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+        if (tops.m[k][r] != kNone) o += y * v;
       }
     } else {
       top = tops.m[wave][r];
       total = tops.l[wave][r];
-      o = *(const f32x4*)(sums + ((wave * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+      o = *(const f32x4 KVC_LDS*)(sums + ((wave * 32 + r) * QD + (at ^ (r & 15u))) * 4);
     }
     const uint64_t slot = ((uint64_t)piece * p.batch.n_new + row_token) * heads + head * p.G + gg;
     if (p.pieces > 1) {
       if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
       if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
     } else {
-      const float x = total == 0.0f ? 0.0f : 1.0f / total;
+      const float y = total == 0.0f ? 0.0f : 1.0f / total;
       if (at * 4 < p.D) {
-        const u32x2 w = {narrow_pair<DT>(o.x * x, o.y * x), narrow_pair<DT>(o.z * x, o.w * x)};
+        const u32x2 w = {narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
         *(KVC_GLOBAL u32x2*)(p.out + (int64_t)row_token * p.o_token + (int64_t)(head * p.G + gg) * p.o_head + at * 4) = w;
       }
       if (at == 0 && p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
@@ -492,8 +621,9 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
 
 template <int DT, int DP>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
-  __shared__ u32x4 lds[lds_vectors<DP>()];
+  __shared__ u32x4 store[lds_vectors<DP>()];
   __shared__ Tops tops;
+  u32x4 KVC_LDS* const lds = (u32x4 KVC_LDS*)store;
   // Workgroups go to the XCDs round-robin; units that follow one another (blocks of rows of the same tokens) share one.
   const uint32_t per = gridDim.x / 8, unit = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
   const bool shared = unit < p.part[0].units;
@@ -554,6 +684,7 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 
 kvc_status plan_attend(AttendParams& p) {
   p.pieces = 0;
+  p.slack = 8.0f / p.scale_log2 < 1e30f ? 8.0f / p.scale_log2 : 1e30f;
   for (int i = 0; i < 2; ++i) {
     AttendPart& a = p.part[i];
     a = AttendPart{};

@@ -83,6 +83,7 @@ struct AttendParams {
   FastDiv dG;
   AttendPart part[2];   // prefix, own
   float scale, scale_log2;
+  float slack;          // products that exceed the running maximum by no more than this leave it as it is
   uint32_t pieces;      // results of a row that are joined afterwards; 1: the row is written at once; 0: nobody sees anything
   float *sums, *tops;   // [pieces][n_new][heads][D] unnormalized sums, [pieces][n_new][heads][2] {maximum (log2), sum of weights}
 };
