@@ -151,20 +151,28 @@ struct Shape {
   static constexpr int LDS = GROUPS * BUFFERS * 2 * TILE;    // vectors in all
 };
 
+// LDS of a workgroup: four arrays of this many vectors, so that the compiler sees which reads a load does not touch.  Four waves
+// side by side have the K and V of two tiles in them, single waves the K of two waves in each of the first two and the V in
+// the others; in the end each wave its sums.
 template <int DP>
-constexpr int lds_vectors() {
-  constexpr int a = Shape<DP, 1>::LDS, b = Shape<DP, 4>::LDS, c = 4 * 32 * DP / 4;  // the last: the sums at the end
+constexpr int quarter() {
+  constexpr int a = Shape<DP, 4>::TILE, b = 2 * Shape<DP, 1>::TILE, c = 32 * DP / 4;
   return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
+struct Lds {
+  u32x4 KVC_LDS *a, *b, *c, *d;
+  __device__ __forceinline__ u32x4 KVC_LDS* of(uint32_t i) const { return i == 0 ? a : i == 1 ? b : i == 2 ? c : d; }
+};
+
 struct Tops {
   float m[4][32], l[4][32];
-  uint32_t most[4];
+  uint32_t most[4], least[4];
 };
 
 // What a wave knows of its unit.
 struct Unit {
-  const uint8_t *keys, *values;  // of the head: slot 0
+  const uint8_t KVC_GLOBAL *keys, *values;  // of the head: slot 0
   const int32_t* table;
   uint32_t t0, t1, limit, least;  // tokens of the unit; those below `limit` are seen by the lane's row, below `least` by all of them
   bool bad_pages;
@@ -177,59 +185,72 @@ struct State {
   f32x16 sum[DP / 32];
 };
 
-__device__ __forceinline__ void wait_loads(int left) {
-  // (a number in the instruction: the callers' are constants)
-  if (left == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  else if (left == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-  else if (left == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-  else if (left == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-  else if (left == 9) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
-  else if (left == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-  else if (left == 17) asm volatile("s_waitcnt vmcnt(17)" ::: "memory");
-  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// Waits until at most LEFT of the wave's loads are on their way.  (The builtin, which the compiler takes into account: it adds no wait
+// of its own then for loads that the wave has waited for.)
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(LEFT < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4) << 14);
+  asm volatile("" ::: "memory");
 }
 
-// Page of token `lane` (of lane % 32 in a tile of 32) of the tile at position `at`.
+// Waits until the wave's reads of LDS have come back.
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
+
+// Page of token lane % TT of the tile at position `at`, if it is there.  (Always one load: waits count it.)
 template <int TT>
 __device__ __forceinline__ uint32_t page_of_lane(const AttendParams& p, const Unit& u, uint32_t at) {
   const uint32_t pos = at + (threadIdx.x & (uint32_t)(TT - 1));
-  const uint32_t page = (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))];  // (always one load: waits count it)
-  return pos < u.t1 ? page : ~0u;
+  return (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))];
 }
 
-// Where a thread's vectors of a tile come from: offsets of K's and V's rows, ~0 for a token that is not there.
+// What has been loaded is not looked at before this point, so that no wait is put in front of it.
+__device__ __forceinline__ void from_here(uint32_t& v) { asm volatile("" : "+v"(v)); }
+
+// Where a thread's vectors of a tile come from: offsets from the first slot's key or value.
 template <int DP, int R>
 struct Sources {
   uint64_t at[Shape<DP, R>::LOADS];
+  bool real[Shape<DP, R>::LOADS];  // the token is there, and the vector within its row
 };
 
-template <int DP, int R>
+// PLAIN: all tokens of the tile are there.
+template <int DP, int R, bool PLAIN>
 __device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, const Unit& u, uint32_t at, uint32_t page) {
   using S = Shape<DP, R>;
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
   uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-  if (page >= p.pool.num_blocks) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  if (!PLAIN && (page >= p.pool.num_blocks || pos >= u.t1)) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  uint32_t from[S::LOADS];
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i) from[i] = (uint32_t)__shfl((int)slot, (int)(first + i * S::STEP));
   Sources<DP, R> s;
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
-    const uint32_t t = first + i * S::STEP, chunk = place<S::CH>(t, self % S::CH);
-    const uint32_t from = (uint32_t)__shfl((int)slot, (int)t);
-    const bool real = from != ~0u && chunk * 8 < p.D;
-    s.at[i] = real ? (uint64_t)from * p.pool.token_bytes + chunk * 16 : ~0ull;
+    const uint32_t chunk = place<S::CH>(first + i * S::STEP, self % S::CH);
+    s.at[i] = (uint64_t)from[i] * p.pool.token_bytes + chunk * 16;
+    s.real[i] = (PLAIN || from[i] != ~0u) && chunk * 8 < p.D;
   }
   return s;
 }
 
-// Loads a tile's K or V from memory straight into LDS: a wave's 64 vectors of one instruction lie side by side there.
-template <int DP, int R>
-__device__ __forceinline__ void load_tile(const uint8_t* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
+// Loads a tile's K or V from memory straight into LDS: a wave's 64 vectors of one instruction lie side by side there.  The address
+// of the zeros is told as one from the base, too: the compiler knows then that loads do not touch the tile that is being read.
+template <int DP, int R, bool WHOLE>
+__device__ __forceinline__ void load_tile(const uint8_t KVC_GLOBAL* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
   using S = Shape<DP, R>;
   const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
+  const uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
-    const uint8_t* from = s.at[i] != ~0ull ? base + s.at[i] : (const uint8_t*)&kZeros;
-    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)from, (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
+    const uint64_t from = WHOLE || s.real[i] ? s.at[i] : zeros;
+    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)(base + from), (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
   }
 }
 
@@ -362,63 +383,63 @@ __device__ __forceinline__ void add_seen_values(const Unit& u, uint32_t at, Stat
   }
 }
 
-template <int TT>
-__device__ __forceinline__ bool is_masked(const Unit& u, uint32_t at) {
-  return u.bad_pages || at + TT > min(u.least, u.t1);
-}
+// Tokens from t0 on that are all there and seen by all rows: tiles among them need no mask.
+__device__ __forceinline__ uint32_t plain_end(const Unit& u) { return u.bad_pages ? u.t0 : max(u.t0, min(u.least, u.t1)); }
 
-// One step of four waves side by side: the tile at `at` lies in (k, v), the next one goes to (k2, v2).
-template <int DT, int DP>
-__device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, uint32_t at, uint32_t& page, const u32x4 (&query)[DP / 16], State<DP>& x,
-                                             const u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
+// One step of four waves side by side: the tile at `at` lies in (k, v), the next one goes to (k2, v2).  PLAIN: all rows see all of
+// the tile, and all of the next one is there; WHOLE: rows are DP elements long, too.
+template <int DT, int DP, bool PLAIN, bool WHOLE>
+__device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
+                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t& page, const u32x4 (&query)[DP / 16],
+                                             State<DP>& x, const u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
                                              u32x4 KVC_LDS* __restrict__ k2, u32x4 KVC_LDS* __restrict__ v2) {
   using S = Shape<DP, 4>;
   constexpr int NS = S::TT / 32;
-  const Sources<DP, 4> from = sources_of<DP, 4>(p, u, at + S::TT, page);
-  load_tile<DP, 4>(u.keys, from, k2);
-  load_tile<DP, 4>(u.values, from, v2);
+  wait_loads<0>();
+  from_here(page);
+  const Sources<DP, 4> from = sources_of<DP, 4, PLAIN>(p, u, at + S::TT, page);
+  __syncthreads();  // all of the tile is there, and the other one has been read
+  load_tile<DP, 4, WHOLE>(keys, from, k2);
+  load_tile<DP, 4, WHOLE>(values, from, v2);
   page = page_of_lane<S::TT>(p, u, at + 2 * S::TT);
   f32x16 s[NS];
   u32x4 w[NS][2];
   products<DT, DP, NS>(k, query, s);
-  if (is_masked<S::TT>(u, at)) {
-    mask<NS>(p, u, at, s);
-    weights<DT, DP, NS>(p, x, s, w);
-    add_seen_values<DT, DP, NS>(u, at, x, v, w);
-  } else {
-    weights<DT, DP, NS>(p, x, s, w);
-    add_values<DT, DP, NS>(x, v, w);
-  }
+  if constexpr (!PLAIN) mask<NS>(p, u, at, s);
+  weights<DT, DP, NS>(p, x, s, w);
+  if constexpr (PLAIN) add_values<DT, DP, NS>(x, v, w);
+  else add_seen_values<DT, DP, NS>(u, at, x, v, w);
 }
 
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
 // follow them as soon as each has been read.
-template <int DT, int DP>
-__device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u, uint32_t at, uint32_t next, uint32_t& page, const u32x4 (&query)[DP / 16],
-                                            State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
+template <int DT, int DP, bool PLAIN, bool WHOLE>
+__device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
+                                            const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
+                                            const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
   using S = Shape<DP, 1>;
   constexpr int N = S::LOADS;
   f32x16 s[1];
   u32x4 w[1][2];
-  wait_loads(N);  // K is there, V may be on its way
+  wait_loads<N>();  // K and the page are there, V may be on its way
+  from_here(page);
+  const Sources<DP, 1> from = sources_of<DP, 1, PLAIN>(p, u, at + next, page);
   products<DT, DP, 1>(k, query, s);
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at + next, page);
-  load_tile<DP, 1>(u.keys, from, k);
+  wait_reads();
+  load_tile<DP, 1, WHOLE>(keys, from, k);
   page = page_of_lane<S::TT>(p, u, at + 2 * next);
-  const bool masked = is_masked<S::TT>(u, at);
-  if (masked) mask<1>(p, u, at, s);
+  if constexpr (!PLAIN) mask<1>(p, u, at, s);
   weights<DT, DP, 1>(p, x, s, w);
-  wait_loads(N + 1);  // V is there; the next K and its successor's page follow
-  if (masked) add_seen_values<DT, DP, 1>(u, at, x, v, w);
-  else add_values<DT, DP, 1>(x, v, w);
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  load_tile<DP, 1>(u.values, from, v);
+  wait_loads<N + 1>();  // V is there; the next K and its successor's page follow
+  if constexpr (PLAIN) add_values<DT, DP, 1>(x, v, w);
+  else add_seen_values<DT, DP, 1>(u, at, x, v, w);
+  wait_reads();
+  load_tile<DP, 1, WHOLE>(values, from, v);
 }
 
 // One workgroup's unit: rows x head x piece of the tokens.
 template <int DT, int DP, int R>
-__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, u32x4 KVC_LDS* lds, Tops& tops) {
+__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, const Lds& lds, Tops& tops) {
   using S = Shape<DP, R>;
   constexpr int TT = S::TT, KK = DP / 16, DD = DP / 32;
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u, half = lane >> 5;
@@ -464,9 +485,10 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   }
   least = wave_uniform(least);
   if constexpr (R > 1) {
-    if (lane == 0) tops.most[wave] = most;
+    if (lane == 0) tops.most[wave] = most, tops.least[wave] = least;
     __syncthreads();
     most = max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3]));
+    least = wave_uniform(min(min(tops.least[0], tops.least[1]), min(tops.least[2], tops.least[3])));
   }
   most = wave_uniform(most);
 
@@ -493,7 +515,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   u.t1 = t1;
   u.limit = limit;
   u.least = least;
-  u.keys = (const uint8_t*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
+  u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
   u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
 
   // A page outside the pool is an error of the caller's that costs time only where it happens.
@@ -523,53 +545,59 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   for (int d = 0; d < DD; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) x.sum[d][i] = 0.0f;
+  const uint32_t plain = plain_end(u);
   if constexpr (R == 1) {
     constexpr uint32_t NEXT = 4 * TT;
-    u32x4 KVC_LDS* const k = lds + wave_uniform(wave) * (2 * S::TILE);
-    u32x4 KVC_LDS* const v = k + S::TILE;
-    uint32_t at = t0 + wave_uniform(wave) * TT;
+    const uint32_t self = wave_uniform(wave);
+    u32x4 KVC_LDS* const k = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
+    u32x4 KVC_LDS* const v = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
+    uint32_t at = t0 + self * TT;
     if (at < t1) {
       uint32_t page = page_of_lane<TT>(p, u, at);
-      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at, page);
-      load_tile<DP, 1>(u.keys, from, k);
+      const Sources<DP, 1> from = sources_of<DP, 1, false>(p, u, at, page);
+      load_tile<DP, 1, false>(u.keys, from, k);
       page = page_of_lane<TT>(p, u, at + NEXT);
-      load_tile<DP, 1>(u.values, from, v);
-      for (; at < t1; at += NEXT) step_of_one<DT, DP>(p, u, at, NEXT, page, query, x, k, v);
-      wait_loads(0);  // (of tiles that are not there: zeros, but they may not land on the sums)
+      load_tile<DP, 1, false>(u.values, from, v);
+      for (; at + NEXT + TT <= plain; at += NEXT) step_of_one<DT, DP, true, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
+      for (; at < t1; at += NEXT) step_of_one<DT, DP, false, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
+      wait_loads<0>();  // (of tiles that are not there: zeros, but they may not land on the sums)
     }
   } else {
-    u32x4 KVC_LDS *const k0 = lds, *const v0 = lds + S::TILE, *const k1 = lds + 2 * S::TILE, *const v1 = lds + 3 * S::TILE;
+    u32x4 KVC_LDS *k0 = lds.a, *v0 = lds.b, *k1 = lds.c, *v1 = lds.d;
     if (t0 < t1) {
       uint32_t page = page_of_lane<TT>(p, u, t0);
-      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, page);
-      load_tile<DP, 4>(u.keys, from, k0);
-      load_tile<DP, 4>(u.values, from, v0);
+      const Sources<DP, 4> from = sources_of<DP, 4, false>(p, u, t0, page);
+      load_tile<DP, 4, false>(u.keys, from, k0);
+      load_tile<DP, 4, false>(u.values, from, v0);
       page = page_of_lane<TT>(p, u, t0 + TT);
-      for (uint32_t at = t0; at < t1;) {
-        wait_loads(0);
-        __syncthreads();
-        step_of_four<DT, DP>(p, u, at, page, query, x, k0, v0, k1, v1);
-        if ((at += TT) >= t1) break;
-        wait_loads(0);
-        __syncthreads();
-        step_of_four<DT, DP>(p, u, at, page, query, x, k1, v1, k0, v0);
-        at += TT;
+      uint32_t at = t0;
+      if (p.D == DP)
+        for (; at + 3 * TT <= plain; at += 2 * TT) {
+          step_of_four<DT, DP, true, true>(p, u, u.keys, u.values, at, page, query, x, lds.a, lds.b, lds.c, lds.d);
+          step_of_four<DT, DP, true, true>(p, u, u.keys, u.values, at + TT, page, query, x, lds.c, lds.d, lds.a, lds.b);
+        }
+      for (; at < t1; at += TT) {
+        step_of_four<DT, DP, false, false>(p, u, u.keys, u.values, at, page, query, x, k0, v0, k1, v1);
+        u32x4 KVC_LDS* const k2 = k0;
+        u32x4 KVC_LDS* const v2 = v0;
+        k0 = k1, v0 = v1;
+        k1 = k2, v1 = v2;
       }
-      wait_loads(0);
+      wait_loads<0>();
     }
   }
   float m = x.m, l = x.l;
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   __syncthreads();
   l = half_sum(l);
-  float KVC_LDS* const sums = (float KVC_LDS*)lds;
+  f32x4 KVC_LDS* const mine = (f32x4 KVC_LDS*)lds.of(wave_uniform(wave));
   constexpr uint32_t QD = DP / 4;  // vectors of four sums of a row
 #pragma unroll
   for (int d = 0; d < DD; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t at = d * 8 + i * 2 + half;
-      *(f32x4 KVC_LDS*)(sums + ((wave * 32 + col) * QD + (at ^ (col & 15u))) * 4) = f32x4{x.sum[d][i * 4], x.sum[d][i * 4 + 1], x.sum[d][i * 4 + 2], x.sum[d][i * 4 + 3]};
+      mine[col * QD + (at ^ (col & 15u))] = f32x4{x.sum[d][i * 4], x.sum[d][i * 4 + 1], x.sum[d][i * 4 + 2], x.sum[d][i * 4 + 3]};
     }
   if (half == 0) {
     tops.m[wave][col] = m != kNone ? m * p.scale_log2 : l == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
@@ -596,13 +624,13 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       for (int k = 0; k < 4; ++k) {
         const float y = weight(tops.m[k][r], top);
         total += y * tops.l[k][r];
-        const f32x4 v = *(const f32x4 KVC_LDS*)(sums + ((k * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+        const f32x4 v = ((const f32x4 KVC_LDS*)lds.of(k))[r * QD + (at ^ (r & 15u))];
         if (tops.m[k][r] != kNone) o += y * v;
       }
     } else {
       top = tops.m[wave][r];
       total = tops.l[wave][r];
-      o = *(const f32x4 KVC_LDS*)(sums + ((wave * 32 + r) * QD + (at ^ (r & 15u))) * 4);
+      o = mine[r * QD + (at ^ (r & 15u))];
     }
     const uint64_t slot = ((uint64_t)piece * p.batch.n_new + row_token) * heads + head * p.G + gg;
     if (p.pieces > 1) {
@@ -621,15 +649,17 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
 
 template <int DT, int DP>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
-  __shared__ u32x4 store[lds_vectors<DP>()];
+  __shared__ u32x4 a[quarter<DP>()], b[quarter<DP>()], c[quarter<DP>()], d[quarter<DP>()];
   __shared__ Tops tops;
-  u32x4 KVC_LDS* const lds = (u32x4 KVC_LDS*)store;
-  // Workgroups go to the XCDs round-robin; units that follow one another (blocks of rows of the same tokens) share one.
-  const uint32_t per = gridDim.x / 8, unit = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
-  const bool shared = unit < p.part[0].units;
-  if (!shared && unit - p.part[0].units >= p.part[1].units) return;
+  const Lds lds = {(u32x4 KVC_LDS*)a, (u32x4 KVC_LDS*)b, (u32x4 KVC_LDS*)c, (u32x4 KVC_LDS*)d};
+  // Workgroups go to the XCDs round-robin.  Each XCD has an eighth of a part's units, which follow one another (blocks of rows of the
+  // same tokens, then pieces of the same head); the prefix's units, which may be long, are begun first.
+  const uint32_t front = (p.part[0].units + 7) / 8 * 8;
+  const bool shared = blockIdx.x < front;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  const uint32_t u = shared ? unit : unit - p.part[0].units;
+  const uint32_t at = shared ? blockIdx.x : blockIdx.x - front, per = (part.units + 7) / 8;
+  const uint32_t u = (at & 7u) * per + (at >> 3);
+  if (u >= part.units) return;
   if (part.waves == 1) attend_unit<DT, DP, 1>(p, part, shared, u, lds, tops);
   else attend_unit<DT, DP, 4>(p, part, shared, u, lds, tops);
 }
@@ -670,8 +700,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
 
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
-  const uint32_t units = p.part[0].units + p.part[1].units;
-  if (units) hipLaunchKernelGGL((attend_kernel<DT, DP>), dim3((units + 7) / 8 * 8), dim3(256), 0, stream, p);
+  const uint32_t groups = (p.part[0].units + 7) / 8 * 8 + (p.part[1].units + 7) / 8 * 8;
+  if (groups) hipLaunchKernelGGL((attend_kernel<DT, DP>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   if (p.pieces != 1) {  // (no piece at all: every row is empty)
     const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = 256 / (DP / 4);
