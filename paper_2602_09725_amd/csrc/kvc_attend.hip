@@ -219,14 +219,13 @@ struct Sources {
   bool real[Shape<DP, R>::LOADS];  // the token is there, and the vector within its row
 };
 
-// PLAIN: all tokens of the tile are there.
-template <int DP, int R, bool PLAIN>
+template <int DP, int R>
 __device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, const Unit& u, uint32_t at, uint32_t page) {
   using S = Shape<DP, R>;
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
   uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-  if (!PLAIN && (page >= p.pool.num_blocks || pos >= u.t1)) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  if (page >= p.pool.num_blocks || pos >= u.t1) slot = ~0u;  // (no slot is: there are fewer than 2^32)
   uint32_t from[S::LOADS];
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) from[i] = (uint32_t)__shfl((int)slot, (int)(first + i * S::STEP));
@@ -235,21 +234,21 @@ __device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, cons
   for (int i = 0; i < S::LOADS; ++i) {
     const uint32_t chunk = place<S::CH>(first + i * S::STEP, self % S::CH);
     s.at[i] = (uint64_t)from[i] * p.pool.token_bytes + chunk * 16;
-    s.real[i] = (PLAIN || from[i] != ~0u) && chunk * 8 < p.D;
+    s.real[i] = from[i] != ~0u && chunk * 8 < p.D;
   }
   return s;
 }
 
 // Loads a tile's K or V from memory straight into LDS: a wave's 64 vectors of one instruction lie side by side there.  The address
 // of the zeros is told as one from the base, too: the compiler knows then that loads do not touch the tile that is being read.
-template <int DP, int R, bool WHOLE>
+template <int DP, int R>
 __device__ __forceinline__ void load_tile(const uint8_t KVC_GLOBAL* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
   using S = Shape<DP, R>;
   const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
   const uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
-    const uint64_t from = WHOLE || s.real[i] ? s.at[i] : zeros;
+    const uint64_t from = s.real[i] ? s.at[i] : zeros;
     __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)(base + from), (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
   }
 }
@@ -383,12 +382,16 @@ __device__ __forceinline__ void add_seen_values(const Unit& u, uint32_t at, Stat
   }
 }
 
+// Whether a tile at position `at` has a token that is there and not seen by all rows.
+template <int TT>
+__device__ __forceinline__ bool hides_tokens(const Unit& u, uint32_t at) { return u.bad_pages || u.least < min(at + TT, u.t1); }
+
 // Tokens from t0 on that are all there and seen by all rows: tiles among them need no mask.
 __device__ __forceinline__ uint32_t plain_end(const Unit& u) { return u.bad_pages ? u.t0 : max(u.t0, min(u.least, u.t1)); }
 
 // One step of four waves side by side: the tile at `at` lies in (k, v), the next one goes to (k2, v2).  PLAIN: all rows see all of
-// the tile, and all of the next one is there; WHOLE: rows are DP elements long, too.
-template <int DT, int DP, bool PLAIN, bool WHOLE>
+// the tile.
+template <int DT, int DP, bool PLAIN>
 __device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                              const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t& page, const u32x4 (&query)[DP / 16],
                                              State<DP>& x, const u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
@@ -397,23 +400,28 @@ __device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& 
   constexpr int NS = S::TT / 32;
   wait_loads<0>();
   from_here(page);
-  const Sources<DP, 4> from = sources_of<DP, 4, PLAIN>(p, u, at + S::TT, page);
+  const Sources<DP, 4> from = sources_of<DP, 4>(p, u, at + S::TT, page);
   __syncthreads();  // all of the tile is there, and the other one has been read
-  load_tile<DP, 4, WHOLE>(keys, from, k2);
-  load_tile<DP, 4, WHOLE>(values, from, v2);
+  load_tile<DP, 4>(keys, from, k2);
+  load_tile<DP, 4>(values, from, v2);
   page = page_of_lane<S::TT>(p, u, at + 2 * S::TT);
   f32x16 s[NS];
   u32x4 w[NS][2];
   products<DT, DP, NS>(k, query, s);
   if constexpr (!PLAIN) mask<NS>(p, u, at, s);
   weights<DT, DP, NS>(p, x, s, w);
-  if constexpr (PLAIN) add_values<DT, DP, NS>(x, v, w);
-  else add_seen_values<DT, DP, NS>(u, at, x, v, w);
+  if constexpr (!PLAIN) {
+    if (hides_tokens<S::TT>(u, at)) {
+      add_seen_values<DT, DP, NS>(u, at, x, v, w);
+      return;
+    }
+  }
+  add_values<DT, DP, NS>(x, v, w);
 }
 
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
 // follow them as soon as each has been read.
-template <int DT, int DP, bool PLAIN, bool WHOLE>
+template <int DT, int DP, bool PLAIN>
 __device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
                                             const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
@@ -423,18 +431,18 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u
   u32x4 w[1][2];
   wait_loads<N>();  // K and the page are there, V may be on its way
   from_here(page);
-  const Sources<DP, 1> from = sources_of<DP, 1, PLAIN>(p, u, at + next, page);
+  const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at + next, page);
   products<DT, DP, 1>(k, query, s);
   wait_reads();
-  load_tile<DP, 1, WHOLE>(keys, from, k);
+  load_tile<DP, 1>(keys, from, k);
   page = page_of_lane<S::TT>(p, u, at + 2 * next);
   if constexpr (!PLAIN) mask<1>(p, u, at, s);
   weights<DT, DP, 1>(p, x, s, w);
   wait_loads<N + 1>();  // V is there; the next K and its successor's page follow
-  if constexpr (PLAIN) add_values<DT, DP, 1>(x, v, w);
-  else add_seen_values<DT, DP, 1>(u, at, x, v, w);
+  if (!PLAIN && hides_tokens<S::TT>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
+  else add_values<DT, DP, 1>(x, v, w);
   wait_reads();
-  load_tile<DP, 1, WHOLE>(values, from, v);
+  load_tile<DP, 1>(values, from, v);
 }
 
 // One workgroup's unit: rows x head x piece of the tokens.
@@ -554,30 +562,29 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     uint32_t at = t0 + self * TT;
     if (at < t1) {
       uint32_t page = page_of_lane<TT>(p, u, at);
-      const Sources<DP, 1> from = sources_of<DP, 1, false>(p, u, at, page);
-      load_tile<DP, 1, false>(u.keys, from, k);
+      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at, page);
+      load_tile<DP, 1>(u.keys, from, k);
       page = page_of_lane<TT>(p, u, at + NEXT);
-      load_tile<DP, 1, false>(u.values, from, v);
-      for (; at + NEXT + TT <= plain; at += NEXT) step_of_one<DT, DP, true, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
-      for (; at < t1; at += NEXT) step_of_one<DT, DP, false, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
+      load_tile<DP, 1>(u.values, from, v);
+      for (; at + TT <= plain; at += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
+      for (; at < t1; at += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
       wait_loads<0>();  // (of tiles that are not there: zeros, but they may not land on the sums)
     }
   } else {
     u32x4 KVC_LDS *k0 = lds.a, *v0 = lds.b, *k1 = lds.c, *v1 = lds.d;
     if (t0 < t1) {
       uint32_t page = page_of_lane<TT>(p, u, t0);
-      const Sources<DP, 4> from = sources_of<DP, 4, false>(p, u, t0, page);
-      load_tile<DP, 4, false>(u.keys, from, k0);
-      load_tile<DP, 4, false>(u.values, from, v0);
+      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, page);
+      load_tile<DP, 4>(u.keys, from, k0);
+      load_tile<DP, 4>(u.values, from, v0);
       page = page_of_lane<TT>(p, u, t0 + TT);
       uint32_t at = t0;
-      if (p.D == DP)
-        for (; at + 3 * TT <= plain; at += 2 * TT) {
-          step_of_four<DT, DP, true, true>(p, u, u.keys, u.values, at, page, query, x, lds.a, lds.b, lds.c, lds.d);
-          step_of_four<DT, DP, true, true>(p, u, u.keys, u.values, at + TT, page, query, x, lds.c, lds.d, lds.a, lds.b);
-        }
+      for (; at + 2 * TT <= plain; at += 2 * TT) {
+        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at, page, query, x, lds.a, lds.b, lds.c, lds.d);
+        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at + TT, page, query, x, lds.c, lds.d, lds.a, lds.b);
+      }
       for (; at < t1; at += TT) {
-        step_of_four<DT, DP, false, false>(p, u, u.keys, u.values, at, page, query, x, k0, v0, k1, v1);
+        step_of_four<DT, DP, false>(p, u, u.keys, u.values, at, page, query, x, k0, v0, k1, v1);
         u32x4 KVC_LDS* const k2 = k0;
         u32x4 KVC_LDS* const v2 = v0;
         k0 = k1, v0 = v1;
@@ -664,36 +671,84 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendPar
   else attend_unit<DT, DP, 4>(p, part, shared, u, lds, tops);
 }
 
-// Joins a row's pieces.  A row's QD lanes take four elements each; a workgroup takes 256 / QD rows.
-template <int DT, int DP>
+// Joins the pieces of rows: a workgroup takes LINES rows (a token and a head), and 256 / LINES threads a row.  First the weights of all of
+// its pieces are computed from their maxima, then the sums are added with many loads under way.
+template <int DT, int DP, int LINES>
 __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
-  constexpr uint32_t QD = DP / 4;
-  const uint32_t heads = p.H * p.G, at = threadIdx.x % QD;
-  const uint64_t line = (uint64_t)blockIdx.x * (256 / QD) + threadIdx.x / QD;  // token and head
-  const uint64_t lines = (uint64_t)p.batch.n_new * heads;
-  if (line >= lines) return;
-  const uint32_t token = (uint32_t)(line / heads), head = (uint32_t)(line - (uint64_t)token * heads);
+  fetch_params<AttendParams>();
+  extern __shared__ float weight_of[];  // [LINES][pieces]
+  __shared__ f32x4 part[256];
+  __shared__ float tops[8];
+  constexpr uint32_t QD = DP / 4, EACH = 256 / LINES, SIDE = EACH / QD;  // lanes and groups of lanes of a row
+  const uint32_t self = threadIdx.x % EACH, mine = threadIdx.x / EACH;
+  const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, line = (uint64_t)blockIdx.x * LINES + mine;
+  const bool there = line < lines;
+  uint32_t token, head;
+  fd_divmod(p.dheads, there ? (uint32_t)line : 0u, token, head);
   const Request q = request_at(p, request_of(p.batch, token));
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
-  const uint32_t a = p.part[0].splits ? (prefix + p.part[0].tokens - 1) / p.part[0].tokens : 0;
-  const uint32_t n = p.part[1].splits && limit > p.prefix && token - q.first < p.batch.most_new ? (limit - p.prefix + p.part[1].tokens - 1) / p.part[1].tokens : 0;
+  uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;
+  uint32_t n = p.part[1].splits && limit > p.prefix && token - q.first < p.batch.most_new ? fd_div(p.part[1].dtokens, limit - p.prefix + p.part[1].tokens - 1) : 0;
+  if (!there) a = n = 0;
+  n += a;
+  auto slot = [&](uint32_t i) { return (uint64_t)(i < a ? i : p.part[0].splits + i - a) * lines + line; };
+  // maxima, weights and the sum of weights: a row's threads share its pieces
+  float* const w = weight_of + mine * p.pieces;
   float top = kNone, total = 0.0f;
-  f32x4 o = {0, 0, 0, 0};
-  for (uint32_t i = 0; i < a + n; ++i) {
-    const uint64_t slot = (uint64_t)(i < a ? i : p.part[0].splits + i - a) * lines + line;
-    const f32x2 t = *(const KVC_GLOBAL f32x2*)(p.tops + slot * 2);
-    const f32x4 v = at * 4 < p.D ? *(const KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) : f32x4{0, 0, 0, 0};
-    if (t.x == kNone) continue;
-    const float now = fmaxf(top, t.x), x = weight(top, now), y = weight(t.x, now);
-    total = total * x + t.y * y;
-    o = o * x + v * y;
+  for (uint32_t i = self; i < n; i += EACH) {
+    const f32x2 t = *(const KVC_GLOBAL f32x2*)(p.tops + slot(i) * 2);
+    w[i] = t.x;
+    const float now = fmaxf(top, t.x), keep = weight(top, now);
+    total = total * keep + (t.x == kNone ? 0.0f : t.y * weight(t.x, now));
     top = now;
   }
-  const float x = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+  for (uint32_t d = 1; d < (EACH < 64 ? EACH : 64); d *= 2) {
+    const float m = __shfl_xor(top, d), l = __shfl_xor(total, d), now = fmaxf(top, m);
+    total = (top == kNone ? 0.0f : total * weight(top, now)) + (m == kNone ? 0.0f : l * weight(m, now));
+    top = now;
+  }
+  if constexpr (EACH > 64) {
+    if ((threadIdx.x & 63u) == 0) tops[threadIdx.x / 64] = top, tops[4 + threadIdx.x / 64] = total;
+    __syncthreads();
+    constexpr uint32_t WAVES = EACH / 64;
+    float m[WAVES], l[WAVES];
+#pragma unroll
+    for (uint32_t k = 0; k < WAVES; ++k) m[k] = tops[mine * WAVES + k], l[k] = tops[4 + mine * WAVES + k];
+    top = kNone;
+    total = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < WAVES; ++k) top = fmaxf(top, m[k]);
+#pragma unroll
+    for (uint32_t k = 0; k < WAVES; ++k) total += m[k] == kNone ? 0.0f : l[k] * weight(m[k], top);
+  }
+  for (uint32_t i = self; i < n; i += EACH) w[i] = weight(w[i], top);
+  __syncthreads();
+  // sums: group g of a row takes pieces g, g + SIDE, ..
+  const uint32_t at = self % QD, group = self / QD;
+  f32x4 o = {0, 0, 0, 0};
   if (at * 4 < p.D) {
-    const u32x2 w = {narrow_pair<DT>(o.x * x, o.y * x), narrow_pair<DT>(o.z * x, o.w * x)};
-    *(KVC_GLOBAL u32x2*)(p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4) = w;
+#pragma unroll 4
+    for (uint32_t i = group; i < n; i += SIDE) {
+      const float x = w[i];
+      const f32x4 v = *(const KVC_GLOBAL f32x4*)(p.sums + slot(i) * p.D + at * 4);
+      if (x != 0.0f) o += v * x;  // (a piece that saw nothing has a maximum of its own, -inf, and sums that mean nothing)
+    }
+  }
+  if constexpr (SIDE > 1) {
+    part[threadIdx.x] = o;
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+      for (uint32_t k = 1; k < SIDE; ++k) o += part[threadIdx.x + k * QD];
+    }
+  }
+  if (!there || group != 0) return;
+  const float y = total == 0.0f ? 0.0f : 1.0f / total;
+  if (at * 4 < p.D) {
+    const u32x2 r = {narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
+    *(KVC_GLOBAL u32x2*)(p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4) = r;
   }
   if (at == 0 && p.lse) p.lse[line] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
@@ -704,8 +759,12 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   if (groups) hipLaunchKernelGGL((attend_kernel<DT, DP>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   if (p.pieces != 1) {  // (no piece at all: every row is empty)
-    const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = 256 / (DP / 4);
-    hipLaunchKernelGGL((join_kernel<DT, DP>), dim3((uint32_t)((lines + each - 1) / each)), dim3(256), 0, stream, p);
+    // Few rows of many pieces take a workgroup each, many rows share one.
+    const uint32_t lines = p.batch.n_new * p.H * p.G;
+    if (lines <= 2048)
+      hipLaunchKernelGGL((join_kernel<DT, DP, 1>), dim3(lines), dim3(256), p.pieces * 4, stream, p);
+    else
+      hipLaunchKernelGGL((join_kernel<DT, DP, 4>), dim3((lines + 3) / 4), dim3(256), p.pieces * 16, stream, p);
   }
   return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_RUNTIME;
 }
@@ -714,6 +773,7 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 
 kvc_status plan_attend(AttendParams& p) {
   p.pieces = 0;
+  p.dheads = make_fastdiv(p.H * p.G);
   p.slack = 8.0f / p.scale_log2 < 1e30f ? 8.0f / p.scale_log2 : 1e30f;
   for (int i = 0; i < 2; ++i) {
     AttendPart& a = p.part[i];
@@ -740,6 +800,7 @@ kvc_status plan_attend(AttendParams& p) {
     a.drows = make_fastdiv(a.row_blocks);
     a.dsplits = make_fastdiv(a.splits);
     a.drequests = make_fastdiv(p.batch.n_requests);
+    a.dtokens = make_fastdiv(a.tokens);
     p.pieces += a.splits;
   }
   if ((uint64_t)p.part[0].units + p.part[1].units > 0x7ffffff0u) return KVC_ERR_UNSUPPORTED;

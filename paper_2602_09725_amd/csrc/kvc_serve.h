@@ -68,7 +68,7 @@ struct AttendPart {
   uint32_t splits;      // pieces of the tokens, 0: the part is empty
   uint32_t tokens;      // of a piece
   uint32_t units;       // workgroups
-  FastDiv drows, dsplits, drequests;
+  FastDiv drows, dsplits, drequests, dtokens;
 };
 
 struct AttendParams {
@@ -80,7 +80,7 @@ struct AttendParams {
   int64_t q_token, q_head, o_token, o_head;
   uint32_t layer, H, G, D, dtype;
   uint32_t prefix, prefix_row, most_tokens;
-  FastDiv dG;
+  FastDiv dG, dheads;   // dheads: query heads
   AttendPart part[2];   // prefix, own
   float scale, scale_log2;
   float slack;          // products that exceed the running maximum by no more than this leave it as it is
