@@ -389,25 +389,45 @@ __device__ __forceinline__ bool hides_tokens(const Unit& u, uint32_t at) { retur
 // Tokens from t0 on that are all there and seen by all rows: tiles among them need no mask.
 __device__ __forceinline__ uint32_t plain_end(const Unit& u) { return u.bad_pages ? u.t0 : max(u.t0, min(u.least, u.t1)); }
 
-// One step of four waves side by side: the tile at `at` lies in (k, v), the next one goes to (k2, v2).  PLAIN: all rows see all of
-// the tile.
+// All waves of a workgroup have come here, and their reads of LDS have come back; loads stay under way.
+__device__ __forceinline__ void meet() {
+  wait_reads();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// What four waves side by side have under way beside the tile that they compute: of the next tile K and, from its sources, V; the
+// pages of the two tiles after that.
+template <int DP>
+struct Ahead {
+  Sources<DP, 4> next;
+  uint32_t page, later;
+};
+
+// One step of four waves side by side, the tile at `at`: K in k, V in v, which are there or on their way.  K is read first, and
+// its place is taken by the K of the tile after the next while the weights are computed; V's place (v2 has been read by now) likewise
+// at the step's begin.  So every load has a step and a half, and about three half tiles are under way (one load a step ahead: 64
+// rows over 32K tokens 75 us instead of MEASURE).  PLAIN: all rows see all of the tile.
 template <int DT, int DP, bool PLAIN>
 __device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
-                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t& page, const u32x4 (&query)[DP / 16],
-                                             State<DP>& x, const u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
-                                             u32x4 KVC_LDS* __restrict__ k2, u32x4 KVC_LDS* __restrict__ v2) {
+                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, Ahead<DP>& ahead, const u32x4 (&query)[DP / 16],
+                                             State<DP>& x, u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
+                                             u32x4 KVC_LDS* __restrict__ v2) {
   using S = Shape<DP, 4>;
-  constexpr int NS = S::TT / 32;
-  wait_loads<0>();
-  from_here(page);
-  const Sources<DP, 4> from = sources_of<DP, 4>(p, u, at + S::TT, page);
-  __syncthreads();  // all of the tile is there, and the other one has been read
-  load_tile<DP, 4>(keys, from, k2);
-  load_tile<DP, 4>(values, from, v2);
-  page = page_of_lane<S::TT>(p, u, at + 2 * S::TT);
+  constexpr int NS = S::TT / 32, N = S::LOADS;
+  wait_loads<2 * N>();  // K; under way: V, the next K, perhaps a page
+  meet();
+  load_tile<DP, 4>(values, ahead.next, v2);
   f32x16 s[NS];
   u32x4 w[NS][2];
   products<DT, DP, NS>(k, query, s);
+  wait_loads<2 * N>();  // V; under way: the next K and V, perhaps a page
+  meet();
+  from_here(ahead.page);
+  ahead.next = sources_of<DP, 4>(p, u, at + 2 * S::TT, ahead.page);
+  ahead.page = ahead.later;
+  ahead.later = page_of_lane<S::TT>(p, u, at + 4 * S::TT);
+  load_tile<DP, 4>(keys, ahead.next, k);
   if constexpr (!PLAIN) mask<NS>(p, u, at, s);
   weights<DT, DP, NS>(p, x, s, w);
   if constexpr (!PLAIN) {
@@ -435,7 +455,8 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u
   products<DT, DP, 1>(k, query, s);
   wait_reads();
   load_tile<DP, 1>(keys, from, k);
-  page = page_of_lane<S::TT>(p, u, at + 2 * next);
+  asm volatile("" ::: "memory");
+  page = page_of_lane<S::TT>(p, u, at + 2 * next);  // (between this line and the wait below: it is one of the loads counted there)
   if constexpr (!PLAIN) mask<1>(p, u, at, s);
   weights<DT, DP, 1>(p, x, s, w);
   wait_loads<N + 1>();  // V is there; the next K and its successor's page follow
@@ -564,7 +585,9 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       uint32_t page = page_of_lane<TT>(p, u, at);
       const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at, page);
       load_tile<DP, 1>(u.keys, from, k);
+      asm volatile("" ::: "memory");
       page = page_of_lane<TT>(p, u, at + NEXT);
+      asm volatile("" ::: "memory");
       load_tile<DP, 1>(u.values, from, v);
       for (; at + TT <= plain; at += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
       for (; at < t1; at += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
@@ -573,18 +596,22 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   } else {
     u32x4 KVC_LDS *k0 = lds.a, *v0 = lds.b, *k1 = lds.c, *v1 = lds.d;
     if (t0 < t1) {
-      uint32_t page = page_of_lane<TT>(p, u, t0);
-      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, page);
+      Ahead<DP> ahead;
+      const uint32_t here = page_of_lane<TT>(p, u, t0), next = page_of_lane<TT>(p, u, t0 + TT);
+      ahead.page = page_of_lane<TT>(p, u, t0 + 2 * TT);
+      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, here);
+      ahead.next = sources_of<DP, 4>(p, u, t0 + TT, next);
       load_tile<DP, 4>(u.keys, from, k0);
       load_tile<DP, 4>(u.values, from, v0);
-      page = page_of_lane<TT>(p, u, t0 + TT);
+      ahead.later = page_of_lane<TT>(p, u, t0 + 3 * TT);
+      load_tile<DP, 4>(u.keys, ahead.next, k1);
       uint32_t at = t0;
       for (; at + 2 * TT <= plain; at += 2 * TT) {
-        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at, page, query, x, lds.a, lds.b, lds.c, lds.d);
-        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at + TT, page, query, x, lds.c, lds.d, lds.a, lds.b);
+        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at, ahead, query, x, lds.a, lds.b, lds.d);
+        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at + TT, ahead, query, x, lds.c, lds.d, lds.b);
       }
       for (; at < t1; at += TT) {
-        step_of_four<DT, DP, false>(p, u, u.keys, u.values, at, page, query, x, k0, v0, k1, v1);
+        step_of_four<DT, DP, false>(p, u, u.keys, u.values, at, ahead, query, x, k0, v0, v1);
         u32x4 KVC_LDS* const k2 = k0;
         u32x4 KVC_LDS* const v2 = v0;
         k0 = k1, v0 = v1;
