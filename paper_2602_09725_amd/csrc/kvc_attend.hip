@@ -62,11 +62,13 @@ struct Request {
   uint32_t faults;
 };
 
+// All of a request; what is out of range is told and made harmless.
 __device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r) {
   Request q;
   q.faults = 0;
   q.first = r;
   q.n = 1;
+  q.row = p.batch.rows ? (uint32_t)p.batch.rows[r] : r;
   if (p.batch.starts) {
     const uint32_t a = (uint32_t)p.batch.starts[r], b = (uint32_t)p.batch.starts[r + 1];
     q.first = a < p.batch.n_new ? a : p.batch.n_new;
@@ -74,14 +76,11 @@ __device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r)
     q.n = end > q.first ? end - q.first : 0;
     if (a > b || b > p.batch.n_new || q.n > p.batch.most_new) q.faults |= KVC_FAULT_LIST;
   }
-  q.row = p.batch.rows ? (uint32_t)p.batch.rows[r] : r;
-  q.len = 0;
-  if (q.row < p.pool.n_rows) q.len = (uint32_t)p.pool.lens[q.row];
-  else q.faults |= KVC_FAULT_LIST, q.row = 0;
-  if (q.len > p.most_tokens) {
-    q.faults |= KVC_FAULT_LIST;
-    if (q.len > 0x7fffffffu) q.len = 0;
-  }
+  const bool known = q.row < p.pool.n_rows;
+  q.row = known ? q.row : 0;
+  q.len = (uint32_t)p.pool.lens[q.row];
+  if (!known || q.len > p.most_tokens) q.faults |= KVC_FAULT_LIST;
+  if (!known || q.len > 0x7fffffffu) q.len = 0;
   return q;
 }
 
@@ -174,8 +173,9 @@ struct Tops {
 struct Unit {
   const uint8_t KVC_GLOBAL *keys, *values;  // of the head: slot 0
   const int32_t* table;
-  uint32_t t0, t1, limit, least;  // tokens of the unit; those below `limit` are seen by the lane's row, below `least` by all of them
-  bool bad_pages;
+  uint32_t t0, t1, bound;  // tokens of the unit that are there; none that the host knows of lies at or beyond `bound`
+  uint32_t limit, least;   // those below `limit` are seen by the lane's row, below `least` by all of them
+  bool bad_pages;          // a page outside the pool has been met: an error of the caller's, and only then looked for token by token
 };
 
 // Running state of a lane's row: a number near the largest product so far, sum of this half's weights, sums of values.
@@ -202,11 +202,12 @@ __device__ __forceinline__ void wait_reads() {
   asm volatile("" ::: "memory");
 }
 
-// Page of token lane % TT of the tile at position `at`, if it is there.  (Always one load: waits count it.)
+// Page of token lane % TT of the tile at position `at`, if it is there.  (Always one load: waits count it.  It lies within the table,
+// and need not wait for the row's length.)
 template <int TT>
 __device__ __forceinline__ uint32_t page_of_lane(const AttendParams& p, const Unit& u, uint32_t at) {
   const uint32_t pos = at + (threadIdx.x & (uint32_t)(TT - 1));
-  return (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))];
+  return (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.bound - 1))];
 }
 
 // What has been loaded is not looked at before this point, so that no wait is put in front of it.
@@ -220,12 +221,14 @@ struct Sources {
 };
 
 template <int DP, int R>
-__device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, const Unit& u, uint32_t at, uint32_t page) {
+__device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, Unit& u, uint32_t at, uint32_t page) {
   using S = Shape<DP, R>;
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
   uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-  if (page >= p.pool.num_blocks || pos >= u.t1) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  const bool bad = page >= p.pool.num_blocks;
+  if (bad || pos >= u.t1) slot = ~0u;  // (no slot is: there are fewer than 2^32)
+  u.bad_pages |= __any(bad && pos < u.t1);
   uint32_t from[S::LOADS];
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) from[i] = (uint32_t)__shfl((int)slot, (int)(first + i * S::STEP));
@@ -387,7 +390,7 @@ template <int TT>
 __device__ __forceinline__ bool hides_tokens(const Unit& u, uint32_t at) { return u.bad_pages || u.least < min(at + TT, u.t1); }
 
 // Tokens from t0 on that are all there and seen by all rows: tiles among them need no mask.
-__device__ __forceinline__ uint32_t plain_end(const Unit& u) { return u.bad_pages ? u.t0 : max(u.t0, min(u.least, u.t1)); }
+__device__ __forceinline__ uint32_t plain_end(const Unit& u) { return max(u.t0, min(u.least, u.t1)); }
 
 // All waves of a workgroup have come here, and their reads of LDS have come back; loads stay under way.
 __device__ __forceinline__ void meet() {
@@ -409,7 +412,7 @@ struct Ahead {
 // at the step's begin.  So every load has a step and a half, and about three half tiles are under way (one load a step ahead: 64
 // rows over 32K tokens 75 us instead of MEASURE).  PLAIN: all rows see all of the tile.
 template <int DT, int DP, bool PLAIN>
-__device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
+__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                              const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, Ahead<DP>& ahead, const u32x4 (&query)[DP / 16],
                                              State<DP>& x, u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
                                              u32x4 KVC_LDS* __restrict__ v2) {
@@ -442,7 +445,7 @@ __device__ __forceinline__ void step_of_four(const AttendParams& p, const Unit& 
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
 // follow them as soon as each has been read.
 template <int DT, int DP, bool PLAIN>
-__device__ __forceinline__ void step_of_one(const AttendParams& p, const Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
+__device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
                                             const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
   using S = Shape<DP, 1>;
@@ -480,92 +483,91 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   if (!shared) fd_divmod(part.drequests, rest, head, request);
   const uint32_t heads = p.H * p.G;
 
-  // The lane's row: its token, query head, and how far it sees.
-  const uint32_t base_row = (block * R + (R == 1 ? 0 : wave)) * 32;
-  Request q{};
-  if (!shared) {
-    q = request_at(p, request);
-    if (threadIdx.x == 0) fault(p, q.faults);
-  }
-  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
-  uint32_t token, g, limit = 0;
-  bool there;
-  {
-    uint32_t t;
-    fd_divmod(p.dG, base_row + col, t, g);
-    there = t < new_tokens;
-    token = there ? t : 0;
-    if (shared) {
-      if (there) {
-        q = request_at(p, request_of(p.batch, token));
-        if (split == 0 && head == 0 && half == 0) fault(p, q.faults);
-        limit = limit_of(p, q, token);
-      }
-    } else if (there) {
-      token += q.first;
-      limit = limit_of(p, q, token);
-    }
-  }
-  uint32_t most = limit, least = there ? limit : ~0u;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    least = min(least, (uint32_t)__shfl_xor((int)least, d));
-  }
-  least = wave_uniform(least);
-  if constexpr (R > 1) {
-    if (lane == 0) tops.most[wave] = most, tops.least[wave] = least;
-    __syncthreads();
-    most = max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3]));
-    least = wave_uniform(min(min(tops.least[0], tops.least[1]), min(tops.least[2], tops.least[3])));
-  }
-  most = wave_uniform(most);
-
-  // The unit's tokens.
-  uint32_t t0, t1, row;
-  if (shared) {
-    t0 = split * part.tokens;
-    t1 = prefix_there(p);
-    if (t1 < p.prefix && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
-    row = p.prefix_row;
-  } else {
-    t0 = p.prefix + split * part.tokens;
-    t1 = p.most_tokens;
-    row = wave_uniform(q.row);
-  }
-  t1 = min(min(t1, t0 + part.tokens), most);
-  if (t0 >= t1) {
-    if (p.pieces > 1) return;
-    t1 = t0;
-  }
+  // What can be asked for at once is: lists, pages, queries; then lengths; then the first tiles, and only then is worked out who sees
+  // what.  (One after the other these made half of a short call's time.)
   Unit u;
-  u.table = p.pool.tables + (uint64_t)row * p.pool.table_len;
-  u.t0 = t0;
-  u.t1 = t1;
-  u.limit = limit;
-  u.least = least;
-  u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
-  u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
+  Request q{};
+  if (!shared) q = request_at(p, request);
+  u.bound = shared ? p.prefix : p.most_tokens;
+  u.t0 = (shared ? 0 : p.prefix) + split * part.tokens;
+  u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
+  constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a wave to its next
+  const uint32_t start = u.t0 + (R == 1 ? wave_uniform(wave) * TT : 0);
+  uint32_t page[4];
+#pragma unroll
+  for (int i = 0; i < (R == 1 ? 2 : 4); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
 
-  // A page outside the pool is an error of the caller's that costs time only where it happens.
-  bool bad_pages = false;
-  if (t0 < t1) {
-    const uint32_t last = fd_div(p.pool.dbs, t1 - 1);
-    for (uint32_t b = fd_div(p.pool.dbs, t0) + threadIdx.x; b <= last; b += 256) bad_pages |= (uint32_t)u.table[b] >= p.pool.num_blocks;
-  }
-  u.bad_pages = __syncthreads_or(bad_pages);
-  if (u.bad_pages && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
-
-  // The rows' queries: column `col`, elements 16 k + 8 half ...
+  // The lane's row: its token and query head; its queries: column `col`, elements 16 k + 8 half ...
+  const uint32_t base_row = (block * R + (R == 1 ? 0 : wave)) * 32;
+  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
+  uint32_t token, g;
+  fd_divmod(p.dG, base_row + col, token, g);
+  const bool there = token < new_tokens;
+  token = (there ? token : 0) + (shared ? 0 : min(q.first, p.batch.n_new - 1));
   u32x4 query[KK];
   {
     const uint16_t* from = p.q + (int64_t)token * p.q_token + (int64_t)(head * p.G + g) * p.q_head;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
       const uint32_t at = k * 16 + half * 8;
-      query[k] = there && at < p.D ? *(const KVC_GLOBAL u32x4*)(from + at) : u32x4{0, 0, 0, 0};
+      query[k] = *(const KVC_GLOBAL u32x4*)(from + (at < p.D ? at : 0));
+      if (!there || at >= p.D) query[k] = u32x4{0, 0, 0, 0};
     }
   }
+  u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
+  u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
+  if (shared) q = request_at(p, request_of(p.batch, token));
+  u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
+  if (shared ? u.t1 < p.prefix && threadIdx.x == 0 : false) fault(p, KVC_FAULT_LIST);
+  u.t1 = min(u.t1, u.t0 + part.tokens);
+  u.bad_pages = false;
+  u.limit = u.least = 0;
+
+  // The first tiles.
+  const bool any = u.t0 < u.t1, has_tile = start < u.t1;
+  u32x4 KVC_LDS *k0, *v0, *k1 = nullptr, *v1 = nullptr;
+  Ahead<DP> ahead;
+  if constexpr (R == 1) {
+    const uint32_t self = wave_uniform(wave);
+    k0 = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
+    v0 = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
+    if (has_tile) {
+      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, start, page[0]);
+      load_tile<DP, 1>(u.keys, from, k0);
+      load_tile<DP, 1>(u.values, from, v0);
+      wait_loads<2 * S::LOADS>();  // (what has been asked for before)
+    }
+  } else {
+    k0 = lds.a, v0 = lds.b, k1 = lds.c, v1 = lds.d;
+    if (any) {
+      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, start, page[0]);
+      ahead.next = sources_of<DP, 4>(p, u, start + TT, page[1]);
+      ahead.page = page[2];
+      ahead.later = page[3];
+      load_tile<DP, 4>(u.keys, from, k0);
+      load_tile<DP, 4>(u.values, from, v0);
+      load_tile<DP, 4>(u.keys, ahead.next, k1);
+      wait_loads<3 * S::LOADS>();
+    }
+  }
+
+  // How far the rows see.
+  if (shared ? there && split == 0 && head == 0 && half == 0 : threadIdx.x == 0) fault(p, q.faults);
+  u.limit = there ? limit_of(p, q, token) : 0;
+  uint32_t most = u.limit, least = there ? u.limit : ~0u;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    least = min(least, (uint32_t)__shfl_xor((int)least, d));
+  }
+  if constexpr (R > 1) {
+    if (lane == 0) tops.most[wave] = most, tops.least[wave] = least;
+    meet();
+    most = max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3]));
+    least = min(min(tops.least[0], tops.least[1]), min(tops.least[2], tops.least[3]));
+  }
+  u.least = wave_uniform(least);
+  const uint32_t end = min(u.t1, wave_uniform(most)), plain = min(plain_end(u), end);
 
   State<DP> x;
   x.m = kNone;
@@ -574,52 +576,26 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   for (int d = 0; d < DD; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) x.sum[d][i] = 0.0f;
-  const uint32_t plain = plain_end(u);
+  uint32_t pos = start;
   if constexpr (R == 1) {
-    constexpr uint32_t NEXT = 4 * TT;
-    const uint32_t self = wave_uniform(wave);
-    u32x4 KVC_LDS* const k = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
-    u32x4 KVC_LDS* const v = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
-    uint32_t at = t0 + self * TT;
-    if (at < t1) {
-      uint32_t page = page_of_lane<TT>(p, u, at);
-      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at, page);
-      load_tile<DP, 1>(u.keys, from, k);
-      asm volatile("" ::: "memory");
-      page = page_of_lane<TT>(p, u, at + NEXT);
-      asm volatile("" ::: "memory");
-      load_tile<DP, 1>(u.values, from, v);
-      for (; at + TT <= plain; at += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
-      for (; at < t1; at += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, at, NEXT, page, query, x, k, v);
-      wait_loads<0>();  // (of tiles that are not there: zeros, but they may not land on the sums)
-    }
+    for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
+    for (; pos < end; pos += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
   } else {
-    u32x4 KVC_LDS *k0 = lds.a, *v0 = lds.b, *k1 = lds.c, *v1 = lds.d;
-    if (t0 < t1) {
-      Ahead<DP> ahead;
-      const uint32_t here = page_of_lane<TT>(p, u, t0), next = page_of_lane<TT>(p, u, t0 + TT);
-      ahead.page = page_of_lane<TT>(p, u, t0 + 2 * TT);
-      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, t0, here);
-      ahead.next = sources_of<DP, 4>(p, u, t0 + TT, next);
-      load_tile<DP, 4>(u.keys, from, k0);
-      load_tile<DP, 4>(u.values, from, v0);
-      ahead.later = page_of_lane<TT>(p, u, t0 + 3 * TT);
-      load_tile<DP, 4>(u.keys, ahead.next, k1);
-      uint32_t at = t0;
-      for (; at + 2 * TT <= plain; at += 2 * TT) {
-        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at, ahead, query, x, lds.a, lds.b, lds.d);
-        step_of_four<DT, DP, true>(p, u, u.keys, u.values, at + TT, ahead, query, x, lds.c, lds.d, lds.b);
-      }
-      for (; at < t1; at += TT) {
-        step_of_four<DT, DP, false>(p, u, u.keys, u.values, at, ahead, query, x, k0, v0, v1);
-        u32x4 KVC_LDS* const k2 = k0;
-        u32x4 KVC_LDS* const v2 = v0;
-        k0 = k1, v0 = v1;
-        k1 = k2, v1 = v2;
-      }
-      wait_loads<0>();
+    for (; pos + 2 * TT <= plain && !u.bad_pages; pos += 2 * TT) {
+      step_of_four<DT, DP, true>(p, u, u.keys, u.values, pos, ahead, query, x, lds.a, lds.b, lds.d);
+      step_of_four<DT, DP, true>(p, u, u.keys, u.values, pos + TT, ahead, query, x, lds.c, lds.d, lds.b);
+    }
+    for (; pos < end; pos += TT) {
+      step_of_four<DT, DP, false>(p, u, u.keys, u.values, pos, ahead, query, x, k0, v0, v1);
+      u32x4 KVC_LDS* const k2 = k0;
+      u32x4 KVC_LDS* const v2 = v0;
+      k0 = k1, v0 = v1;
+      k1 = k2, v1 = v2;
     }
   }
+  wait_loads<0>();  // (of tiles that nobody reads: they may not land on the sums, nor after the workgroup's end)
+  if (u.bad_pages && lane == 0) fault(p, KVC_FAULT_PAGE);
+  if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
   float m = x.m, l = x.l;
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   __syncthreads();
@@ -813,8 +789,11 @@ kvc_status plan_attend(AttendParams& p) {
     a.drows = a.dsplits = a.drequests = make_fastdiv(1);
     if (tokens == 0) continue;
     if (whole >> 31) return KVC_ERR_UNSUPPORTED;
-    uint64_t splits = 512 / whole;
-    if (splits < 1) splits = 1;
+    // One workgroup a CU where a piece is short (of 32K tokens and 32 rows 32 or 64 pieces of 8 heads 51 or 59 us), two of them where it
+    // is long (64 rows, twice the rows of queries a workgroup has: of 32K tokens 16 or 32 pieces 76 or 74 us, of 64K 130 or 118); where more than
+    // two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms instead of 1.75).
+    uint64_t splits = whole <= 512 && tokens * whole >= 1024 * 512 ? 512 / whole : whole <= 256 ? 256 / whole : 1;
+    if (whole > 512 && tokens >= 4096 && 20 * ((whole + 511) / 512) * 512 > 23 * whole) splits = 2;
     uint64_t each = (tokens + splits - 1) / splits;
     const uint64_t least = 128;
     each = (each + least - 1) / least * least;
