@@ -218,6 +218,7 @@ template <int DP, int R>
 struct Sources {
   uint64_t at[Shape<DP, R>::LOADS];
   bool real[Shape<DP, R>::LOADS];  // the token is there, and the vector within its row
+  bool all;                        // all of the wave's are
 };
 
 template <int DP, int R>
@@ -226,18 +227,19 @@ __device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, Unit
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
   uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-  const bool bad = page >= p.pool.num_blocks;
-  if (bad || pos >= u.t1) slot = ~0u;  // (no slot is: there are fewer than 2^32)
-  u.bad_pages |= __any(bad && pos < u.t1);
+  const bool bad = page >= p.pool.num_blocks, gone = pos >= u.t1;
+  slot = (int)bad | (int)gone ? ~0u : slot;  // (no slot is: there are fewer than 2^32)
+  u.bad_pages |= __any((int)bad & (int)!gone);
   uint32_t from[S::LOADS];
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) from[i] = (uint32_t)__shfl((int)slot, (int)(first + i * S::STEP));
   Sources<DP, R> s;
+  s.all = !__any(slot == ~0u) && p.D == DP;
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
     const uint32_t chunk = place<S::CH>(first + i * S::STEP, self % S::CH);
     s.at[i] = (uint64_t)from[i] * p.pool.token_bytes + chunk * 16;
-    s.real[i] = from[i] != ~0u && chunk * 8 < p.D;
+    s.real[i] = (int)(from[i] != ~0u) & (int)(chunk * 8 < p.D);
   }
   return s;
 }
@@ -249,11 +251,16 @@ __device__ __forceinline__ void load_tile(const uint8_t KVC_GLOBAL* base, const 
   using S = Shape<DP, R>;
   const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
   const uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
+  uint64_t from[S::LOADS];
 #pragma unroll
-  for (int i = 0; i < S::LOADS; ++i) {
-    const uint64_t from = s.real[i] ? s.at[i] : zeros;
-    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)(base + from), (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
+  for (int i = 0; i < S::LOADS; ++i) from[i] = s.at[i];
+  if (!s.all) {
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) from[i] = s.real[i] ? s.at[i] : zeros;
   }
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i)
+    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)(base + from[i]), (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
 }
 
 // V^T of dims 32 d .., tokens 16 k .. in the lane's order.
@@ -273,20 +280,26 @@ __device__ __forceinline__ u32x4 values_at(const u32x4 KVC_LDS* v, int k, int d)
   return a;
 }
 
-// S^T of a tile.
+// S^T of a tile.  K's vectors are read 32 tokens ahead of the products that take them: left to itself the compiler reads each one just
+// before its product and waits for it.
 template <int DT, int DP, int NS>
 __device__ __forceinline__ void products(const u32x4 KVC_LDS* k, const u32x4 (&query)[DP / 16], f32x16 (&s)[NS]) {
-  constexpr int CH = DP / 8;
+  constexpr int CH = DP / 8, KK = DP / 16;
   const uint32_t lane = threadIdx.x & 63u, col = lane & 31u, half = lane >> 5;
+  u32x4 f[2][KK];
+#pragma unroll
+  for (int e = 0; e < KK; ++e) f[0][e] = k[col * CH + place<CH>(col, e * 2 + half)];
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (n + 1 < NS) {
+      const uint32_t t = (n + 1) * 32 + col;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < DP / 16; ++e) {
-      const uint32_t t = n * 32 + col;
-      s[n] = mfma<DT>(k[t * CH + place<CH>(t, e * 2 + half)], query[e], s[n]);
+      for (int e = 0; e < KK; ++e) f[(n + 1) & 1][e] = k[t * CH + place<CH>(t, e * 2 + half)];
     }
+    s[n] = mfma<DT>(f[n & 1][0], query[0], f32x16{});
+#pragma unroll
+    for (int e = 1; e < KK; ++e) s[n] = mfma<DT>(f[n & 1][e], query[e], s[n]);
   }
 }
 
