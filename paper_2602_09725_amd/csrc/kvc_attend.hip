@@ -141,7 +141,7 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
 template <int DP, int R>
 struct Shape {
   static constexpr int CH = DP / 8;                          // vectors of a token's row
-  static constexpr int TT = R == 1 || DP > 128 ? 32 : 64;    // tokens of a tile
+  static constexpr int TT = R == 1 ? 32 : 64;                // tokens of a tile
   static constexpr int GROUPS = 4 / R;                       // waves along the tokens, each with tiles of its own
   static constexpr int BUFFERS = R == 1 ? 1 : 2;
   static constexpr int LOADS = TT * CH / (R * 64);           // vectors of K (and of V) that a thread loads
@@ -250,7 +250,8 @@ template <int DP, int R>
 __device__ __forceinline__ void load_tile(const uint8_t KVC_GLOBAL* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
   using S = Shape<DP, R>;
   const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
-  const uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
+  uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
+  asm("" : "+s"(zeros));  // (or it sees through this)
   uint64_t from[S::LOADS];
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) from[i] = s.at[i];
@@ -318,16 +319,11 @@ __device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint3
     }
 }
 
-// Weights of a tile, rounded to the type, from its products; the state is moved to them.
-template <int DT, int DP, int NS>
-__device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, const f32x16 (&s)[NS], u32x4 (&w)[NS][2]) {
-  float top = kNone;
-#pragma unroll
-  for (int n = 0; n < NS; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+// Moves the state's base if a product exceeds it by too much; top: the largest of the lane's.  (The number subtracted need not be the
+// maximum: as long as no weight exceeds 2^8, sums and types hold them as well.)
+template <int DP>
+__device__ __forceinline__ void move_base(const AttendParams& p, State<DP>& x, float top) {
   top = half_max(top);
-  // The number subtracted need not be the maximum: as long as no weight exceeds 2^8, sums and types hold them as well.
   if (__any(top > x.m + p.slack)) {
     const float now = fmaxf(x.m, top), keep = weight(x.m * p.scale_log2, now * p.scale_log2);
     x.m = now;
@@ -337,6 +333,17 @@ __device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, con
 #pragma unroll
       for (int i = 0; i < 16; ++i) x.sum[d][i] *= keep;
   }
+}
+
+// Weights of a tile, rounded to the type, from its products; the state is moved to them.
+template <int DT, int DP, int NS>
+__device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, const f32x16 (&s)[NS], u32x4 (&w)[NS][2]) {
+  float top = kNone;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+  move_base<DP>(p, x, top);
   const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
 #pragma unroll
   for (int n = 0; n < NS; ++n)
@@ -412,47 +419,107 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
-// What four waves side by side have under way beside the tile that they compute: of the next tile K and, from its sources, V; the
-// pages of the two tiles after that.
+// The e-th vector of 32 tokens of K, the one that a lane has in the product.
 template <int DP>
-struct Ahead {
-  Sources<DP, 4> next;
-  uint32_t page, later;
-};
+__device__ __forceinline__ u32x4 key_at(const u32x4 KVC_LDS* k, int e) {
+  const uint32_t lane = threadIdx.x & 63u, col = lane & 31u, half = lane >> 5;
+  return k[col * (DP / 8) + place<DP / 8>(col, (uint32_t)e * 2 + half)];
+}
 
-// One step of four waves side by side, the tile at `at`: K in k, V in v, which are there or on their way.  K is read first, and
-// its place is taken by the K of the tile after the next while the weights are computed; V's place (v2 has been read by now) likewise
-// at the step's begin.  So every load has a step and a half, and about three half tiles are under way (one load a step ahead: 64
-// rows over 32K tokens 75 us instead of MEASURE).  PLAIN: all rows see all of the tile.
-template <int DT, int DP, bool PLAIN>
-__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
-                                             const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, Ahead<DP>& ahead, const u32x4 (&query)[DP / 16],
-                                             State<DP>& x, u32x4 KVC_LDS* __restrict__ k, const u32x4 KVC_LDS* __restrict__ v,
-                                             u32x4 KVC_LDS* __restrict__ v2) {
-  using S = Shape<DP, 4>;
-  constexpr int NS = S::TT / 32, N = S::LOADS;
-  wait_loads<2 * N>();  // K; under way: V, the next K, perhaps a page
-  meet();
-  load_tile<DP, 4>(values, ahead.next, v2);
-  f32x16 s[NS];
-  u32x4 w[NS][2];
-  products<DT, DP, NS>(k, query, s);
-  wait_loads<2 * N>();  // V; under way: the next K and V, perhaps a page
-  meet();
-  from_here(ahead.page);
-  ahead.next = sources_of<DP, 4>(p, u, at + 2 * S::TT, ahead.page);
-  ahead.page = ahead.later;
-  ahead.later = page_of_lane<S::TT>(p, u, at + 4 * S::TT);
-  load_tile<DP, 4>(keys, ahead.next, k);
-  if constexpr (!PLAIN) mask<NS>(p, u, at, s);
-  weights<DT, DP, NS>(p, x, s, w);
-  if constexpr (!PLAIN) {
-    if (hides_tokens<S::TT>(u, at)) {
-      add_seen_values<DT, DP, NS>(u, at, x, v, w);
-      return;
+// 32 tokens that all rows see all of: their products are in s, V in v; s gets the products of the 32 at k.  `first` holds K's first two
+// vectors, and gets those of the 32 tokens after these, at k2.  more: what is at k will be taken.  The matrix unit and the other
+// ones work side by side if they are given their instructions in turn: beside each product stands some of the weights' arithmetic, and
+// reads of LDS are two vectors ahead.  The order is the source's (left to itself the compiler makes blocks of either).
+template <int DT, int DP>
+__device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x, const u32x4 (&query)[DP / 16], f32x16& s, u32x4 (&first)[2],
+                                            const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2, bool more) {
+  constexpr int KK = DP / 16, DD = DP / 32, STEPS = 2 * DD;
+  f32x16 next;
+  u32x4 w[2], f[3] = {first[0], first[1], first[1]};
+  const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
+#pragma unroll
+  for (int e = 0; e < KK; ++e) {
+    f[(e + 2) % 3] = e + 2 < KK ? key_at<DP>(k, e + 2) : values_at<DP / 8>(v, (e + 2 - KK) / DD, (e + 2 - KK) % DD);
+    next = mfma<DT>(f[e % 3], query[e], e ? next : f32x16{});
+#pragma unroll
+    for (int i = e * 16 / KK; i < (e + 1) * 16 / KK; i += 2) {  // (16 / KK of them: one pair, two or a half)
+      if (i % 2) continue;
+      const float a = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -shift));
+      const float b = __builtin_amdgcn_exp2f(fmaf(s[i + 1], p.scale_log2, -shift));
+      x.l += a + b;
+      w[i / 8][(i % 8) / 2] = narrow_pair<DT>(a, b);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  add_values<DT, DP, NS>(x, v, w);
+  float top = kNone;
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const u32x4 ahead = j + 2 < STEPS ? values_at<DP / 8>(v, (j + 2) / DD, (j + 2) % DD) : key_at<DP>(k2, j + 2 - STEPS);
+    f[(KK + j + 2) % 3] = ahead;
+    if (j + 2 >= STEPS) first[j + 2 - STEPS] = ahead;
+    x.sum[j % DD] = mfma<DT>(f[(KK + j) % 3], w[j / DD], x.sum[j % DD]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i * STEPS / 16 == j) top = fmaxf(top, next[i]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  s = next;
+  if (more) move_base<DP>(p, x, top);
+}
+
+// The first half of a step of four waves side by side: V of the tile at hand is there for all of them, and the next one's is loaded
+// to the place of the one before.
+template <int DP>
+__device__ __forceinline__ void begin_values(const Unit& u, const Sources<DP, 4>& next, u32x4 KVC_LDS* v2) {
+  wait_loads<Shape<DP, 4>::LOADS>();  // under way: the next K
+  meet();
+  load_tile<DP, 4>(u.values, next, v2);
+}
+
+// The second half: the next tile's K is there, and the one after it is loaded to the place of this one's, which has been read.  Its page
+// was asked for two steps ago; two pages are under way, of the tiles with even and with odd numbers.
+template <int DP>
+__device__ __forceinline__ void begin_keys(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, u32x4 KVC_LDS* k) {
+  using S = Shape<DP, 4>;
+  wait_loads<S::LOADS>();  // under way: the next V
+  meet();
+  from_here(page);
+  next = sources_of<DP, 4>(p, u, at + 2 * S::TT, page);
+  page = page_of_lane<S::TT>(p, u, at + 4 * S::TT);
+  load_tile<DP, 4>(u.keys, next, k);
+}
+
+// The tile at `at`, which all rows see all of: K in k, V in v; the next one in k2, to v2.  s holds the products of its first half.
+template <int DT, int DP>
+__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, const u32x4 (&query)[DP / 16],
+                                             State<DP>& x, f32x16& s, u32x4 (&first)[2], u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2,
+                                             u32x4 KVC_LDS* v2, bool more) {
+  constexpr int HALF = 32 * (DP / 8);
+  begin_values<DP>(u, next, v2);
+  take_tokens<DT, DP>(p, x, query, s, first, k + HALF, v, k2, true);
+  begin_keys<DP>(p, u, at, next, page, k);
+  take_tokens<DT, DP>(p, x, query, s, first, k2, v + HALF, k2 + HALF, more);
+}
+
+// A tile that needs a mask, or comes after one.
+template <int DT, int DP>
+__device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page,
+                                                    const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, u32x4 KVC_LDS* v2) {
+  constexpr int HALF = 32 * (DP / 8);
+  begin_values<DP>(u, next, v2);
+  wait_loads<Shape<DP, 4>::LOADS>();
+  f32x16 s[2];
+  products<DT, DP, 2>(k, query, s);
+  begin_keys<DP>(p, u, at, next, page, k);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    f32x16 one[1] = {s[n]};
+    u32x4 w[1][2];
+    mask<1>(p, u, at + n * 32, one);
+    weights<DT, DP, 1>(p, x, one, w);
+    if (hides_tokens<32>(u, at + n * 32)) add_seen_values<DT, DP, 1>(u, at + n * 32, x, v + n * HALF, w);
+    else add_values<DT, DP, 1>(x, v + n * HALF, w);
+  }
 }
 
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
@@ -482,6 +549,100 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   load_tile<DP, 1>(values, from, v);
 }
 
+// Which part of the work a unit is.
+struct Place {
+  uint32_t block, split, head, request;
+};
+
+__device__ __forceinline__ Place place_of_unit(const AttendParams& p, const AttendPart& part, bool shared, uint32_t unit) {
+  Place w;
+  uint32_t rest;
+  fd_divmod(part.drows, unit, rest, w.block);
+  fd_divmod(part.dsplits, rest, rest, w.split);
+  w.head = rest;
+  w.request = 0;
+  if (!shared) fd_divmod(part.drequests, rest, w.head, w.request);
+  return w;
+}
+
+// The query of a row, element 16 k + 8 half of it in the k-th vector; 0 where there is none.  Returns whether there is a row, and its token.
+template <int DP>
+__device__ __forceinline__ bool load_query(const AttendParams& p, const Request& q, bool shared, uint32_t new_tokens, uint32_t row, uint32_t head,
+                                           uint32_t& token, u32x4 (&query)[DP / 16]) {
+  const uint32_t half = (threadIdx.x >> 5) & 1u;
+  uint32_t t, g;
+  fd_divmod(p.dG, row, t, g);
+  const bool there = t < new_tokens;
+  token = (there ? t : 0) + (shared ? 0 : min(q.first, p.batch.n_new - 1));
+  const uint16_t* from = p.q + (int64_t)token * p.q_token + (int64_t)(head * p.G + g) * p.q_head;
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) {
+    const uint32_t at = k * 16 + half * 8;
+    query[k] = *(const KVC_GLOBAL u32x4*)(from + (at < p.D ? at : 0));
+    if (!there || at >= p.D) query[k] = u32x4{0, 0, 0, 0};
+  }
+  return there;
+}
+
+// From the lanes' rows to all rows of a workgroup of four waves side by side: the most and the least that one sees.
+__device__ __forceinline__ void lanes_see(uint32_t& most, uint32_t& least) {
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    least = min(least, (uint32_t)__shfl_xor((int)least, d));
+  }
+}
+__device__ __forceinline__ void rows_see(Tops& tops, uint32_t& most, uint32_t& least) {
+  const uint32_t wave = threadIdx.x >> 6;
+  lanes_see(most, least);
+  if ((threadIdx.x & 63u) == 0) tops.most[wave] = most, tops.least[wave] = least;
+  meet();
+  most = wave_uniform(max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3])));
+  least = wave_uniform(min(min(tops.least[0], tops.least[1]), min(tops.least[2], tops.least[3])));
+}
+
+// A wave's 32 rows of sums into LDS, in vectors of four, and their bases and sums of weights.
+template <int DP>
+__device__ __forceinline__ void put_sums(const AttendParams& p, const State<DP>& x, f32x4 KVC_LDS* sums, float* m, float* l) {
+  constexpr uint32_t QD = DP / 4;
+  const uint32_t lane = threadIdx.x & 63u, col = lane & 31u, half = lane >> 5;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t at = d * 8 + i * 2 + half;
+      sums[col * QD + (at ^ (col & 15u))] = f32x4{x.sum[d][i * 4], x.sum[d][i * 4 + 1], x.sum[d][i * 4 + 2], x.sum[d][i * 4 + 3]};
+    }
+  const float total = half_sum(x.l);
+  if (half == 0) {
+    m[col] = x.m != kNone ? x.m * p.scale_log2 : total == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
+    l[col] = total;
+  }
+}
+
+// Four sums of a row, the at-th vector of them: to the pieces, or divided to the result.
+template <int DT>
+__device__ __forceinline__ void write_row(const AttendParams& p, bool shared, const Place& w, const Request& q, uint32_t new_tokens, uint32_t row, uint32_t at,
+                                          f32x4 o, float top, float total) {
+  uint32_t t, g;
+  fd_divmod(p.dG, row, t, g);
+  if (t >= new_tokens) return;
+  const uint32_t token = shared ? t : q.first + t, head = w.head * p.G + g;
+  const uint32_t piece = shared ? w.split : p.part[0].splits + w.split;
+  const uint64_t slot = ((uint64_t)piece * p.batch.n_new + token) * (p.H * p.G) + head;
+  if (p.pieces > 1) {
+    if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
+    if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
+    return;
+  }
+  const float y = total == 0.0f ? 0.0f : 1.0f / total;
+  if (at * 4 < p.D) {
+    const u32x2 r = {narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
+    *(KVC_GLOBAL u32x2*)(p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4) = r;
+  }
+  if (at == 0 && p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
 // One workgroup's unit: rows x head x piece of the tokens.
 template <int DT, int DP, int R>
 __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, const Lds& lds, Tops& tops) {
@@ -489,20 +650,15 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   constexpr int TT = S::TT, KK = DP / 16, DD = DP / 32;
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u, half = lane >> 5;
 
-  uint32_t rest, block, split, head, request = 0;
-  fd_divmod(part.drows, unit, rest, block);
-  fd_divmod(part.dsplits, rest, rest, split);
-  head = rest;
-  if (!shared) fd_divmod(part.drequests, rest, head, request);
-  const uint32_t heads = p.H * p.G;
+  const Place at_work = place_of_unit(p, part, shared, unit);
 
   // What can be asked for at once is: lists, pages, queries; then lengths; then the first tiles, and only then is worked out who sees
   // what.  (One after the other these made half of a short call's time.)
   Unit u;
   Request q{};
-  if (!shared) q = request_at(p, request);
+  if (!shared) q = request_at(p, at_work.request);
   u.bound = shared ? p.prefix : p.most_tokens;
-  u.t0 = (shared ? 0 : p.prefix) + split * part.tokens;
+  u.t0 = (shared ? 0 : p.prefix) + at_work.split * part.tokens;
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
   constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a wave to its next
   const uint32_t start = u.t0 + (R == 1 ? wave_uniform(wave) * TT : 0);
@@ -510,24 +666,12 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
 #pragma unroll
   for (int i = 0; i < (R == 1 ? 2 : 4); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
 
-  // The lane's row: its token and query head; its queries: column `col`, elements 16 k + 8 half ...
-  const uint32_t base_row = (block * R + (R == 1 ? 0 : wave)) * 32;
+  const uint32_t base_row = (at_work.block * R + (R == 1 ? 0 : wave)) * 32;
   const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
-  uint32_t token, g;
-  fd_divmod(p.dG, base_row + col, token, g);
-  const bool there = token < new_tokens;
-  token = (there ? token : 0) + (shared ? 0 : min(q.first, p.batch.n_new - 1));
+  uint32_t token;
   u32x4 query[KK];
-  {
-    const uint16_t* from = p.q + (int64_t)token * p.q_token + (int64_t)(head * p.G + g) * p.q_head;
-#pragma unroll
-    for (int k = 0; k < KK; ++k) {
-      const uint32_t at = k * 16 + half * 8;
-      query[k] = *(const KVC_GLOBAL u32x4*)(from + (at < p.D ? at : 0));
-      if (!there || at >= p.D) query[k] = u32x4{0, 0, 0, 0};
-    }
-  }
-  u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)head * p.D * 2;
+  const bool there = load_query<DP>(p, q, shared, new_tokens, base_row + col, at_work.head, token, query);
+  u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)at_work.head * p.D * 2;
   u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
   if (shared) q = request_at(p, request_of(p.batch, token));
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
@@ -539,7 +683,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   // The first tiles.
   const bool any = u.t0 < u.t1, has_tile = start < u.t1;
   u32x4 KVC_LDS *k0, *v0, *k1 = nullptr, *v1 = nullptr;
-  Ahead<DP> ahead;
+  Sources<DP, 4> next;
   if constexpr (R == 1) {
     const uint32_t self = wave_uniform(wave);
     k0 = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
@@ -554,31 +698,20 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     k0 = lds.a, v0 = lds.b, k1 = lds.c, v1 = lds.d;
     if (any) {
       const Sources<DP, 4> from = sources_of<DP, 4>(p, u, start, page[0]);
-      ahead.next = sources_of<DP, 4>(p, u, start + TT, page[1]);
-      ahead.page = page[2];
-      ahead.later = page[3];
+      next = sources_of<DP, 4>(p, u, start + TT, page[1]);
       load_tile<DP, 4>(u.keys, from, k0);
       load_tile<DP, 4>(u.values, from, v0);
-      load_tile<DP, 4>(u.keys, ahead.next, k1);
+      load_tile<DP, 4>(u.keys, next, k1);
       wait_loads<3 * S::LOADS>();
     }
   }
 
   // How far the rows see.
-  if (shared ? there && split == 0 && head == 0 && half == 0 : threadIdx.x == 0) fault(p, q.faults);
+  if (shared ? there && at_work.split == 0 && at_work.head == 0 && half == 0 : threadIdx.x == 0) fault(p, q.faults);
   u.limit = there ? limit_of(p, q, token) : 0;
   uint32_t most = u.limit, least = there ? u.limit : ~0u;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    least = min(least, (uint32_t)__shfl_xor((int)least, d));
-  }
-  if constexpr (R > 1) {
-    if (lane == 0) tops.most[wave] = most, tops.least[wave] = least;
-    meet();
-    most = max(max(tops.most[0], tops.most[1]), max(tops.most[2], tops.most[3]));
-    least = min(min(tops.least[0], tops.least[1]), min(tops.least[2], tops.least[3]));
-  }
+  if constexpr (R == 1) lanes_see(most, least);
+  else rows_see(tops, most, least);
   u.least = wave_uniform(least);
   const uint32_t end = min(u.t1, wave_uniform(most)), plain = min(plain_end(u), end);
 
@@ -594,12 +727,37 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
     for (; pos < end; pos += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
   } else {
-    for (; pos + 2 * TT <= plain && !u.bad_pages; pos += 2 * TT) {
-      step_of_four<DT, DP, true>(p, u, u.keys, u.values, pos, ahead, query, x, lds.a, lds.b, lds.d);
-      step_of_four<DT, DP, true>(p, u, u.keys, u.values, pos + TT, ahead, query, x, lds.c, lds.d, lds.b);
+    if (pos + TT <= plain && !u.bad_pages) {
+      f32x16 s;
+      u32x4 first[2];
+      wait_loads<2 * S::LOADS>();  // the first K
+      meet();
+      s = mfma<DT>(key_at<DP>(k0, 0), query[0], f32x16{});
+#pragma unroll
+      for (int e = 1; e < KK; ++e) s = mfma<DT>(key_at<DP>(k0, e), query[e], s);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) first[e] = key_at<DP>(k0 + 32 * S::CH, e);
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      move_base<DP>(p, x, top);
+      // (whether a page is bad is known two tiles ahead)
+      for (; pos + 2 * TT <= plain && !u.bad_pages; pos += 2 * TT) {
+        step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, s, first, lds.a, lds.b, lds.c, lds.d, true);
+        step_of_four<DT, DP>(p, u, pos + TT, next, page[3], query, x, s, first, lds.c, lds.d, lds.a, lds.b, pos + 3 * TT <= plain);
+      }
+      if (pos + TT <= plain && !u.bad_pages) {
+        step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, s, first, lds.a, lds.b, lds.c, lds.d, false);
+        pos += TT;
+        k0 = lds.c, v0 = lds.d, k1 = lds.a, v1 = lds.b;
+        const uint32_t other = page[3];
+        page[3] = page[2], page[2] = other;
+      }
     }
     for (; pos < end; pos += TT) {
-      step_of_four<DT, DP, false>(p, u, u.keys, u.values, pos, ahead, query, x, k0, v0, v1);
+      masked_step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, k0, v0, v1);
+      const uint32_t other = page[3];
+      page[3] = page[2], page[2] = other;
       u32x4 KVC_LDS* const k2 = k0;
       u32x4 KVC_LDS* const v2 = v0;
       k0 = k1, v0 = v1;
@@ -609,35 +767,18 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   wait_loads<0>();  // (of tiles that nobody reads: they may not land on the sums, nor after the workgroup's end)
   if (u.bad_pages && lane == 0) fault(p, KVC_FAULT_PAGE);
   if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
-  float m = x.m, l = x.l;
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   __syncthreads();
-  l = half_sum(l);
   f32x4 KVC_LDS* const mine = (f32x4 KVC_LDS*)lds.of(wave_uniform(wave));
-  constexpr uint32_t QD = DP / 4;  // vectors of four sums of a row
-#pragma unroll
-  for (int d = 0; d < DD; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t at = d * 8 + i * 2 + half;
-      mine[col * QD + (at ^ (col & 15u))] = f32x4{x.sum[d][i * 4], x.sum[d][i * 4 + 1], x.sum[d][i * 4 + 2], x.sum[d][i * 4 + 3]};
-    }
-  if (half == 0) {
-    tops.m[wave][col] = m != kNone ? m * p.scale_log2 : l == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
-    tops.l[wave][col] = l;
-  }
+  put_sums<DP>(p, x, mine, tops.m[wave], tops.l[wave]);
   __syncthreads();
+  constexpr uint32_t QD = DP / 4;                         // vectors of four sums of a row
   constexpr uint32_t SIDE = 64 / QD == 0 ? 1 : 64 / QD;  // rows that a wave writes at a time
   constexpr uint32_t MINE = R == 1 ? 8 : 32;             // rows that it writes in all
   const uint32_t begin = R == 1 ? wave * 8 : 0, at = lane % QD;
-  const uint32_t piece = shared ? split : p.part[0].splits + split;
 #pragma unroll 2
   for (uint32_t i = 0; i < MINE; i += SIDE) {
     const uint32_t r = begin + i + lane / QD;
-    uint32_t t, gg;
-    fd_divmod(p.dG, base_row + r, t, gg);
-    if (t >= new_tokens) continue;
-    const uint32_t row_token = shared ? t : q.first + t;
     f32x4 o = {0, 0, 0, 0};
     float top = kNone, total = 0.0f;
     if constexpr (R == 1) {
@@ -655,19 +796,18 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       total = tops.l[wave][r];
       o = mine[r * QD + (at ^ (r & 15u))];
     }
-    const uint64_t slot = ((uint64_t)piece * p.batch.n_new + row_token) * heads + head * p.G + gg;
-    if (p.pieces > 1) {
-      if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
-      if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
-    } else {
-      const float y = total == 0.0f ? 0.0f : 1.0f / total;
-      if (at * 4 < p.D) {
-        const u32x2 w = {narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
-        *(KVC_GLOBAL u32x2*)(p.out + (int64_t)row_token * p.o_token + (int64_t)(head * p.G + gg) * p.o_head + at * 4) = w;
-      }
-      if (at == 0 && p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
-    }
+    write_row<DT>(p, shared, at_work, q, new_tokens, base_row + r, at, o, top, total);
   }
+}
+
+// Workgroups go to the XCDs round-robin.  Each XCD has an eighth of a part's units, which follow one another (blocks of rows of the
+// same tokens, then pieces of the same head); the prefix's units, which may be long, are begun first.
+__device__ __forceinline__ bool unit_of(const AttendParams& p, bool& shared, uint32_t& unit) {
+  const uint32_t front = (p.part[0].units + 7) / 8 * 8;
+  shared = blockIdx.x < front;
+  const uint32_t units = p.part[shared ? 0 : 1].units, at = shared ? blockIdx.x : blockIdx.x - front;
+  unit = (at & 7u) * ((units + 7) / 8) + (at >> 3);
+  return unit < units;
 }
 
 template <int DT, int DP>
@@ -675,16 +815,12 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendPar
   __shared__ u32x4 a[quarter<DP>()], b[quarter<DP>()], c[quarter<DP>()], d[quarter<DP>()];
   __shared__ Tops tops;
   const Lds lds = {(u32x4 KVC_LDS*)a, (u32x4 KVC_LDS*)b, (u32x4 KVC_LDS*)c, (u32x4 KVC_LDS*)d};
-  // Workgroups go to the XCDs round-robin.  Each XCD has an eighth of a part's units, which follow one another (blocks of rows of the
-  // same tokens, then pieces of the same head); the prefix's units, which may be long, are begun first.
-  const uint32_t front = (p.part[0].units + 7) / 8 * 8;
-  const bool shared = blockIdx.x < front;
+  bool shared;
+  uint32_t unit;
+  if (!unit_of(p, shared, unit)) return;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  const uint32_t at = shared ? blockIdx.x : blockIdx.x - front, per = (part.units + 7) / 8;
-  const uint32_t u = (at & 7u) * per + (at >> 3);
-  if (u >= part.units) return;
-  if (part.waves == 1) attend_unit<DT, DP, 1>(p, part, shared, u, lds, tops);
-  else attend_unit<DT, DP, 4>(p, part, shared, u, lds, tops);
+  if (part.waves == 1) attend_unit<DT, DP, 1>(p, part, shared, unit, lds, tops);
+  else attend_unit<DT, DP, 4>(p, part, shared, unit, lds, tops);
 }
 
 // Joins the pieces of rows: a workgroup takes LINES rows (a token and a head), and 256 / LINES threads a row.  First the weights of all of
@@ -791,13 +927,14 @@ kvc_status plan_attend(AttendParams& p) {
   p.pieces = 0;
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = 8.0f / p.scale_log2 < 1e30f ? 8.0f / p.scale_log2 : 1e30f;
+  const uint64_t chip = p.D <= 128 ? 512 : 256;  // workgroups that run at a time
   for (int i = 0; i < 2; ++i) {
     AttendPart& a = p.part[i];
     a = AttendPart{};
     const uint64_t tokens = i == 0 ? p.prefix : p.most_tokens - p.prefix;
     const uint64_t rows = (uint64_t)(i == 0 ? p.batch.n_new : p.batch.most_new) * p.G;
     a.waves = rows <= 32 ? 1 : 4;
-    const uint64_t blocks = (rows + 32 * a.waves - 1) / (32 * a.waves);
+    const uint64_t each_block = a.waves == 1 ? 32 : 128, blocks = (rows + each_block - 1) / each_block;
     const uint64_t whole = blocks * p.H * (i == 0 ? 1 : p.batch.n_requests);
     a.drows = a.dsplits = a.drequests = make_fastdiv(1);
     if (tokens == 0) continue;
@@ -805,8 +942,8 @@ kvc_status plan_attend(AttendParams& p) {
     // One workgroup a CU where a piece is short (of 32K tokens and 32 rows 32 or 64 pieces of 8 heads 51 or 59 us), two of them where it
     // is long (64 rows, twice the rows of queries a workgroup has: of 32K tokens 16 or 32 pieces 76 or 74 us, of 64K 130 or 118); where more than
     // two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms instead of 1.75).
-    uint64_t splits = whole <= 512 && tokens * whole >= 1024 * 512 ? 512 / whole : whole <= 256 ? 256 / whole : 1;
-    if (whole > 512 && tokens >= 4096 && 20 * ((whole + 511) / 512) * 512 > 23 * whole) splits = 2;
+    uint64_t splits = whole <= chip && tokens * whole >= 1024 * chip ? chip / whole : whole <= 256 ? 256 / whole : 1;
+    if (whole > chip && tokens >= 4096 && 20 * ((whole + chip - 1) / chip) * chip > 23 * whole) splits = 2;
     uint64_t each = (tokens + splits - 1) / splits;
     const uint64_t least = 128;
     each = (each + least - 1) / least * least;
