@@ -426,21 +426,25 @@ __device__ __forceinline__ u32x4 key_at(const u32x4 KVC_LDS* k, int e) {
   return k[col * (DP / 8) + place<DP / 8>(col, (uint32_t)e * 2 + half)];
 }
 
-// 32 tokens that all rows see all of: their products are in s, V in v; s gets the products of the 32 at k.  `first` holds K's first two
+constexpr int kReads = 4;  // reads of LDS that are under way
+
+// 32 tokens that all rows see all of: their products are in s, V in v; s gets the products of the 32 at k.  `first` holds K's first
 // vectors, and gets those of the 32 tokens after these, at k2.  more: what is at k will be taken.  The matrix unit and the other
 // ones work side by side if they are given their instructions in turn: beside each product stands some of the weights' arithmetic, and
-// reads of LDS are two vectors ahead.  The order is the source's (left to itself the compiler makes blocks of either).
+// reads of LDS are kReads vectors ahead.  The order is the source's (left to itself the compiler makes blocks of either).
 template <int DT, int DP>
-__device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x, const u32x4 (&query)[DP / 16], f32x16& s, u32x4 (&first)[2],
+__device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x, const u32x4 (&query)[DP / 16], f32x16& s, u32x4 (&first)[kReads],
                                             const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2, bool more) {
-  constexpr int KK = DP / 16, DD = DP / 32, STEPS = 2 * DD;
+  constexpr int KK = DP / 16, DD = DP / 32, STEPS = 2 * DD, A = kReads;
   f32x16 next;
-  u32x4 w[2], f[3] = {first[0], first[1], first[1]};
+  u32x4 w[2], f[A + 1];
+#pragma unroll
+  for (int e = 0; e < A; ++e) f[e] = first[e];
   const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
 #pragma unroll
   for (int e = 0; e < KK; ++e) {
-    f[(e + 2) % 3] = e + 2 < KK ? key_at<DP>(k, e + 2) : values_at<DP / 8>(v, (e + 2 - KK) / DD, (e + 2 - KK) % DD);
-    next = mfma<DT>(f[e % 3], query[e], e ? next : f32x16{});
+    f[(e + A) % (A + 1)] = e + A < KK ? key_at<DP>(k, e + A) : values_at<DP / 8>(v, (e + A - KK) / DD, (e + A - KK) % DD);
+    next = mfma<DT>(f[e % (A + 1)], query[e], e ? next : f32x16{});
 #pragma unroll
     for (int i = e * 16 / KK; i < (e + 1) * 16 / KK; i += 2) {  // (16 / KK of them: one pair, two or a half)
       if (i % 2) continue;
@@ -454,10 +458,10 @@ __device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x,
   float top = kNone;
 #pragma unroll
   for (int j = 0; j < STEPS; ++j) {
-    const u32x4 ahead = j + 2 < STEPS ? values_at<DP / 8>(v, (j + 2) / DD, (j + 2) % DD) : key_at<DP>(k2, j + 2 - STEPS);
-    f[(KK + j + 2) % 3] = ahead;
-    if (j + 2 >= STEPS) first[j + 2 - STEPS] = ahead;
-    x.sum[j % DD] = mfma<DT>(f[(KK + j) % 3], w[j / DD], x.sum[j % DD]);
+    const u32x4 ahead = j + A < STEPS ? values_at<DP / 8>(v, (j + A) / DD, (j + A) % DD) : key_at<DP>(k2, j + A - STEPS);
+    f[(KK + j + A) % (A + 1)] = ahead;
+    if (j + A >= STEPS) first[j + A - STEPS] = ahead;
+    x.sum[j % DD] = mfma<DT>(f[(KK + j) % (A + 1)], w[j / DD], x.sum[j % DD]);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i * STEPS / 16 == j) top = fmaxf(top, next[i]);
@@ -492,7 +496,7 @@ __device__ __forceinline__ void begin_keys(const AttendParams& p, Unit& u, uint3
 // The tile at `at`, which all rows see all of: K in k, V in v; the next one in k2, to v2.  s holds the products of its first half.
 template <int DT, int DP>
 __device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, const u32x4 (&query)[DP / 16],
-                                             State<DP>& x, f32x16& s, u32x4 (&first)[2], u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2,
+                                             State<DP>& x, f32x16& s, u32x4 (&first)[kReads], u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2,
                                              u32x4 KVC_LDS* v2, bool more) {
   constexpr int HALF = 32 * (DP / 8);
   begin_values<DP>(u, next, v2);
@@ -729,14 +733,14 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   } else {
     if (pos + TT <= plain && !u.bad_pages) {
       f32x16 s;
-      u32x4 first[2];
+      u32x4 first[kReads];
       wait_loads<2 * S::LOADS>();  // the first K
       meet();
       s = mfma<DT>(key_at<DP>(k0, 0), query[0], f32x16{});
 #pragma unroll
       for (int e = 1; e < KK; ++e) s = mfma<DT>(key_at<DP>(k0, e), query[e], s);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) first[e] = key_at<DP>(k0 + 32 * S::CH, e);
+      for (int e = 0; e < kReads; ++e) first[e] = key_at<DP>(k0 + 32 * S::CH, e);
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
