@@ -429,10 +429,10 @@ __device__ __forceinline__ u32x4 key_at(const u32x4 KVC_LDS* k, int e) {
 constexpr int kReads = 4;  // reads of LDS that are under way
 
 // 32 tokens that all rows see all of: their products are in s, V in v; s gets the products of the 32 at k.  `first` holds K's first
-// vectors, and gets those of the 32 tokens after these, at k2.  more: what is at k will be taken.  The matrix unit and the other
+// vectors, and gets those of the 32 tokens after these, at k2, if they are there by now (NEXT).  more: what is at k will be taken.  The matrix unit and the other
 // ones work side by side if they are given their instructions in turn: beside each product stands some of the weights' arithmetic, and
 // reads of LDS are kReads vectors ahead.  The order is the source's (left to itself the compiler makes blocks of either).
-template <int DT, int DP>
+template <int DT, int DP, bool NEXT>
 __device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x, const u32x4 (&query)[DP / 16], f32x16& s, u32x4 (&first)[kReads],
                                             const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2, bool more) {
   constexpr int KK = DP / 16, DD = DP / 32, STEPS = 2 * DD, A = kReads;
@@ -458,9 +458,8 @@ __device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x,
   float top = kNone;
 #pragma unroll
   for (int j = 0; j < STEPS; ++j) {
-    const u32x4 ahead = j + A < STEPS ? values_at<DP / 8>(v, (j + A) / DD, (j + A) % DD) : key_at<DP>(k2, j + A - STEPS);
-    f[(KK + j + A) % (A + 1)] = ahead;
-    if (j + A >= STEPS) first[j + A - STEPS] = ahead;
+    if (j + A < STEPS) f[(KK + j + A) % (A + 1)] = values_at<DP / 8>(v, (j + A) / DD, (j + A) % DD);
+    else if (NEXT) first[j + A - STEPS] = key_at<DP>(k2, j + A - STEPS);
     x.sum[j % DD] = mfma<DT>(f[(KK + j) % (A + 1)], w[j / DD], x.sum[j % DD]);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -483,10 +482,13 @@ __device__ __forceinline__ void begin_values(const Unit& u, const Sources<DP, 4>
 // The second half: the next tile's K is there, and the one after it is loaded to the place of this one's, which has been read.  Its page
 // was asked for two steps ago; two pages are under way, of the tiles with even and with odd numbers.
 template <int DP>
-__device__ __forceinline__ void begin_keys(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, u32x4 KVC_LDS* k) {
+__device__ __forceinline__ void begin_keys(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, u32x4 KVC_LDS* k,
+                                           u32x4 (&first)[kReads], const u32x4 KVC_LDS* k2) {
   using S = Shape<DP, 4>;
   wait_loads<S::LOADS>();  // under way: the next V
   meet();
+#pragma unroll
+  for (int e = 0; e < kReads; ++e) first[e] = key_at<DP>(k2, e);
   from_here(page);
   next = sources_of<DP, 4>(p, u, at + 2 * S::TT, page);
   page = page_of_lane<S::TT>(p, u, at + 4 * S::TT);
@@ -500,9 +502,9 @@ __device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uin
                                              u32x4 KVC_LDS* v2, bool more) {
   constexpr int HALF = 32 * (DP / 8);
   begin_values<DP>(u, next, v2);
-  take_tokens<DT, DP>(p, x, query, s, first, k + HALF, v, k2, true);
-  begin_keys<DP>(p, u, at, next, page, k);
-  take_tokens<DT, DP>(p, x, query, s, first, k2, v + HALF, k2 + HALF, more);
+  take_tokens<DT, DP, false>(p, x, query, s, first, k + HALF, v, nullptr, true);
+  begin_keys<DP>(p, u, at, next, page, k, first, k2);
+  take_tokens<DT, DP, true>(p, x, query, s, first, k2, v + HALF, k2 + HALF, more);
 }
 
 // A tile that needs a mask, or comes after one.
@@ -511,10 +513,10 @@ __device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit&
                                                     const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, u32x4 KVC_LDS* v2) {
   constexpr int HALF = 32 * (DP / 8);
   begin_values<DP>(u, next, v2);
-  wait_loads<Shape<DP, 4>::LOADS>();
   f32x16 s[2];
   products<DT, DP, 2>(k, query, s);
-  begin_keys<DP>(p, u, at, next, page, k);
+  u32x4 unused[kReads];
+  begin_keys<DP>(p, u, at, next, page, k, unused, k);
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     f32x16 one[1] = {s[n]};
@@ -529,9 +531,8 @@ __device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit&
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
 // follow them as soon as each has been read.
 template <int DT, int DP, bool PLAIN>
-__device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
-                                            const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
-                                            const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
+__device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* keys, const uint8_t KVC_GLOBAL* values, uint32_t at,
+                                            uint32_t next, uint32_t& page, const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, u32x4 KVC_LDS* v) {
   using S = Shape<DP, 1>;
   constexpr int N = S::LOADS;
   f32x16 s[1];
@@ -551,6 +552,15 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   else add_values<DT, DP, 1>(x, v, w);
   wait_reads();
   load_tile<DP, 1>(values, from, v);
+}
+
+// The step for tiles that need no mask.  Loads of K do not touch V: told so the compiler does not have reads of one wait for the other.
+// (It keeps such notes for few loads of a kernel only; the steps with a mask go without.)
+template <int DT, int DP>
+__device__ __forceinline__ void plain_step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
+                                                  const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
+                                                  const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
+  step_of_one<DT, DP, true>(p, u, keys, values, at, next, page, query, x, k, v);
 }
 
 // Which part of the work a unit is.
@@ -728,7 +738,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     for (int i = 0; i < 16; ++i) x.sum[d][i] = 0.0f;
   uint32_t pos = start;
   if constexpr (R == 1) {
-    for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) step_of_one<DT, DP, true>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
+    for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) plain_step_of_one<DT, DP>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
     for (; pos < end; pos += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
   } else {
     if (pos + TT <= plain && !u.bad_pages) {
