@@ -111,9 +111,6 @@ __device__ __forceinline__ uint32_t prefix_there(const AttendParams& p) {
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------------
 
-// What a load of a token that is not there reads.
-__device__ const u32x4 kZeros = {0, 0, 0, 0};
-
 // Where the 16-byte vector `chunk` of a token's row lies in the row in LDS.  Reads of K take one chunk of 32 tokens that follow one
 // another, transposing reads of V two of four: both find them in different banks.
 template <int CH>
@@ -173,6 +170,7 @@ struct Tops {
 struct Unit {
   const uint8_t KVC_GLOBAL *keys, *values;  // of the head: slot 0
   const int32_t* table;
+  uint32_t span;           // bytes from there to the end of the layer's keys (and values), if they fit
   uint32_t t0, t1, bound;  // tokens of the unit that are there; none that the host knows of lies at or beyond `bound`
   uint32_t limit, least;   // those below `limit` are seen by the lane's row, below `least` by all of them
   bool bad_pages;          // a page outside the pool has been met: an error of the caller's, and only then looked for token by token
@@ -213,55 +211,62 @@ __device__ __forceinline__ uint32_t page_of_lane(const AttendParams& p, const Un
 // What has been loaded is not looked at before this point, so that no wait is put in front of it.
 __device__ __forceinline__ void from_here(uint32_t& v) { asm volatile("" : "+v"(v)); }
 
-// Where a thread's vectors of a tile come from: offsets from the first slot's key or value.
-template <int DP, int R>
+// Where a thread's vectors of a tile come from.  They are loaded through a descriptor of the memory, so that a vector that is not there
+// reads as 0 if its offset lies beyond the end.  Offsets have 32 bits: where a layer's K is larger than that (BIG), bits 31 and up
+// go into the descriptor's base, which differs from lane to lane then, and the compiler makes a loop over the bases that occur.
+// (Loads by address instead, which need no such loop, have the compiler wait for all of a wave's reads of LDS where it would
+// wait for the oldest.)
+template <int DP, int R, bool BIG>
 struct Sources {
-  uint64_t at[Shape<DP, R>::LOADS];
-  bool real[Shape<DP, R>::LOADS];  // the token is there, and the vector within its row
-  bool all;                        // all of the wave's are
+  uint32_t at[Shape<DP, R>::LOADS];
+  uint32_t base[BIG ? Shape<DP, R>::LOADS : 1];
 };
 
-template <int DP, int R>
-__device__ __forceinline__ Sources<DP, R> sources_of(const AttendParams& p, Unit& u, uint32_t at, uint32_t page) {
+template <int DP, int R, bool BIG>
+__device__ __forceinline__ Sources<DP, R, BIG> sources_of(const AttendParams& p, Unit& u, uint32_t at, uint32_t page) {
   using S = Shape<DP, R>;
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
-  uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
+  const uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
   const bool bad = page >= p.pool.num_blocks, gone = pos >= u.t1;
-  slot = (int)bad | (int)gone ? ~0u : slot;  // (no slot is: there are fewer than 2^32)
   u.bad_pages |= __any((int)bad & (int)!gone);
-  uint32_t from[S::LOADS];
-#pragma unroll
-  for (int i = 0; i < S::LOADS; ++i) from[i] = (uint32_t)__shfl((int)slot, (int)(first + i * S::STEP));
-  Sources<DP, R> s;
-  s.all = !__any(slot == ~0u) && p.D == DP;
+  uint32_t offset, base = 0;
+  if constexpr (BIG) {
+    const uint64_t all = (uint64_t)slot * p.pool.token_bytes;
+    offset = (uint32_t)all & 0x7fffffffu;
+    base = (int)bad | (int)gone ? 0 : (uint32_t)(all >> 31);
+  } else {
+    offset = slot * p.pool.token_bytes;
+  }
+  if ((int)bad | (int)gone) offset = ~0u;
+  Sources<DP, R, BIG> s;
+  s.base[0] = 0;
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
+    const int from = (int)(first * 4 + i * S::STEP * 4);
     const uint32_t chunk = place<S::CH>(first + i * S::STEP, self % S::CH);
-    s.at[i] = (uint64_t)from[i] * p.pool.token_bytes + chunk * 16;
-    s.real[i] = (int)(from[i] != ~0u) & (int)(chunk * 8 < p.D);
+    s.at[i] = __builtin_elementwise_add_sat((uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)offset), chunk * 8 < p.D ? chunk * 16 : ~0u);
+    if constexpr (BIG) s.base[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)base);
   }
   return s;
 }
 
-// Loads a tile's K or V from memory straight into LDS: a wave's 64 vectors of one instruction lie side by side there.  The address
-// of the zeros is told as one from the base, too: the compiler knows then that loads do not touch the tile that is being read.
-template <int DP, int R>
-__device__ __forceinline__ void load_tile(const uint8_t KVC_GLOBAL* base, const Sources<DP, R>& s, u32x4 KVC_LDS* to) {
-  using S = Shape<DP, R>;
+// Loads a tile's K or V, or COUNT of a thread's vectors of it from FIRST on, from memory straight into LDS: a wave's 64 vectors of one
+// instruction lie side by side there.
+template <int FIRST, int COUNT, int DP, int R, bool BIG>
+__device__ __forceinline__ void load_part(const Unit& u, const uint8_t KVC_GLOBAL* from, const Sources<DP, R, BIG>& s, u32x4 KVC_LDS* to) {
   const uint32_t wave = R == 1 ? 0 : wave_uniform(threadIdx.x >> 6);
-  uint64_t zeros = (uint64_t)&kZeros - (uint64_t)base;
-  asm("" : "+s"(zeros));  // (or it sees through this)
-  uint64_t from[S::LOADS];
 #pragma unroll
-  for (int i = 0; i < S::LOADS; ++i) from[i] = s.at[i];
-  if (!s.all) {
-#pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) from[i] = s.real[i] ? s.at[i] : zeros;
+  for (int i = 0; i < COUNT; ++i) {
+    // (a row begins below bit 31, but may end above it)
+    const auto memory = __builtin_amdgcn_make_buffer_rsrc((void*)(from + (BIG ? (uint64_t)s.base[BIG ? FIRST + i : 0] << 31 : 0)), 0,
+                                                          BIG ? 0x80000000u + DP * 2 : u.span, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(memory, (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, (int)s.at[FIRST + i], 0, 0, 0);
   }
-#pragma unroll
-  for (int i = 0; i < S::LOADS; ++i)
-    __builtin_amdgcn_global_load_lds((const KVC_GLOBAL void*)(base + from[i]), (void KVC_LDS*)(to + i * (R * 64) + wave * 64), 16, 0, 0);
+}
+template <int DP, int R, bool BIG>
+__device__ __forceinline__ void load_tile(const Unit& u, const uint8_t KVC_GLOBAL* from, const Sources<DP, R, BIG>& s, u32x4 KVC_LDS* to) {
+  load_part<0, Shape<DP, R>::LOADS>(u, from, s, to);
 }
 
 // V^T of dims 32 d .., tokens 16 k .. in the lane's order.
@@ -470,67 +475,70 @@ __device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x,
   if (more) move_base<DP>(p, x, top);
 }
 
-// The first half of a step of four waves side by side: V of the tile at hand is there for all of them, and the next one's is loaded
-// to the place of the one before.
-template <int DP>
-__device__ __forceinline__ void begin_values(const Unit& u, const Sources<DP, 4>& next, u32x4 KVC_LDS* v2) {
-  wait_loads<Shape<DP, 4>::LOADS>();  // under way: the next K
-  meet();
-  load_tile<DP, 4>(u.values, next, v2);
-}
+// Four waves side by side take a tile's 64 tokens in a step.  The products run 32 tokens ahead of the values, so a step needs the K
+// of its tile's second half and of the next tile's first: these two lie together in LDS, and there is one barrier a
+// step, behind which stands all that it reads, and before which all has been read that its loads replace.  Each load has a whole step's time.
 
-// The second half: the next tile's K is there, and the one after it is loaded to the place of this one's, which has been read.  Its page
-// was asked for two steps ago; two pages are under way, of the tiles with even and with odd numbers.
-template <int DP>
-__device__ __forceinline__ void begin_keys(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, u32x4 KVC_LDS* k,
-                                           u32x4 (&first)[kReads], const u32x4 KVC_LDS* k2) {
+// The begin of the step of the tile at `at`: V of the next tile goes to v2, K of its second half and of the first half after it to k2.
+// `next` holds the next tile's sources, `page` the page after it.
+template <int DP, bool BIG>
+__device__ __forceinline__ void begin_step(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4, BIG>& next, uint32_t& page, u32x4 (&first)[kReads],
+                                           const u32x4 KVC_LDS* k, u32x4 KVC_LDS* k2, u32x4 KVC_LDS* v2) {
   using S = Shape<DP, 4>;
-  wait_loads<S::LOADS>();  // under way: the next V
+  wait_loads<0>();
   meet();
 #pragma unroll
-  for (int e = 0; e < kReads; ++e) first[e] = key_at<DP>(k2, e);
+  for (int e = 0; e < kReads; ++e) first[e] = key_at<DP>(k, e);
+  load_tile(u, u.values, next, v2);
+  load_part<S::LOADS / 2, S::LOADS / 2>(u, u.keys, next, k2);
   from_here(page);
-  next = sources_of<DP, 4>(p, u, at + 2 * S::TT, page);
-  page = page_of_lane<S::TT>(p, u, at + 4 * S::TT);
-  load_tile<DP, 4>(u.keys, next, k);
+  next = sources_of<DP, 4, BIG>(p, u, at + 2 * S::TT, page);
+  load_part<0, S::LOADS / 2>(u, u.keys, next, k2 + S::TILE / 2);
+  page = page_of_lane<S::TT>(p, u, at + 3 * S::TT);
 }
 
-// The tile at `at`, which all rows see all of: K in k, V in v; the next one in k2, to v2.  s holds the products of its first half.
-template <int DT, int DP>
-__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page, const u32x4 (&query)[DP / 16],
-                                             State<DP>& x, f32x16& s, u32x4 (&first)[kReads], u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, const u32x4 KVC_LDS* k2,
-                                             u32x4 KVC_LDS* v2, bool more) {
-  constexpr int HALF = 32 * (DP / 8);
-  begin_values<DP>(u, next, v2);
-  take_tokens<DT, DP, false>(p, x, query, s, first, k + HALF, v, nullptr, true);
-  begin_keys<DP>(p, u, at, next, page, k, first, k2);
-  take_tokens<DT, DP, true>(p, x, query, s, first, k2, v + HALF, k2 + HALF, more);
+// A tile that all rows see all of.  s holds the products of its first half, and gets those of the next tile's.  more: these are seen by
+// all rows as well.
+template <int DT, int DP, bool BIG>
+__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4, BIG>& next, uint32_t& page, const u32x4 (&query)[DP / 16],
+                                             State<DP>& x, f32x16& s, const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, u32x4 KVC_LDS* k2, u32x4 KVC_LDS* v2,
+                                             bool more) {
+  constexpr int HALF = Shape<DP, 4>::TILE / 2;
+  u32x4 first[kReads];
+  begin_step<DP, BIG>(p, u, at, next, page, first, k, k2, v2);
+  take_tokens<DT, DP, true>(p, x, query, s, first, k, v, k + HALF, true);
+  take_tokens<DT, DP, false>(p, x, query, s, first, k + HALF, v + HALF, nullptr, more);
 }
 
-// A tile that needs a mask, or comes after one.
+// 32 tokens at `at` that need a mask, or come after some that do.
 template <int DT, int DP>
-__device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4>& next, uint32_t& page,
-                                                    const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, u32x4 KVC_LDS* v2) {
-  constexpr int HALF = 32 * (DP / 8);
-  begin_values<DP>(u, next, v2);
-  f32x16 s[2];
-  products<DT, DP, 2>(k, query, s);
+__device__ __forceinline__ void take_masked(const AttendParams& p, const Unit& u, uint32_t at, State<DP>& x, const f32x16& products, const u32x4 KVC_LDS* v) {
+  f32x16 s[1] = {products};
+  u32x4 w[1][2];
+  mask<1>(p, u, at, s);
+  weights<DT, DP, 1>(p, x, s, w);
+  if (hides_tokens<32>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
+  else add_values<DT, DP, 1>(x, v, w);
+}
+
+template <int DT, int DP, bool BIG>
+__device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4, BIG>& next, uint32_t& page,
+                                                    const u32x4 (&query)[DP / 16], State<DP>& x, f32x16& s, const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v,
+                                                    u32x4 KVC_LDS* k2, u32x4 KVC_LDS* v2) {
+  constexpr int HALF = Shape<DP, 4>::TILE / 2;
   u32x4 unused[kReads];
-  begin_keys<DP>(p, u, at, next, page, k, unused, k);
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    f32x16 one[1] = {s[n]};
-    u32x4 w[1][2];
-    mask<1>(p, u, at + n * 32, one);
-    weights<DT, DP, 1>(p, x, one, w);
-    if (hides_tokens<32>(u, at + n * 32)) add_seen_values<DT, DP, 1>(u, at + n * 32, x, v + n * HALF, w);
-    else add_values<DT, DP, 1>(x, v + n * HALF, w);
-  }
+  begin_step<DP, BIG>(p, u, at, next, page, unused, k, k2, v2);
+  f32x16 second[1], after[1];
+  products<DT, DP, 1>(k, query, second);
+  take_masked<DT, DP>(p, u, at, x, s, v);
+  products<DT, DP, 1>(k + HALF, query, after);
+  take_masked<DT, DP>(p, u, at + 32, x, second[0], v + HALF);
+  s = after[0];
 }
 
 // One step of a wave that has its tokens to itself: the tile's K and V are in (k, v) or on their way there, the next tile's
 // follow them as soon as each has been read.
-template <int DT, int DP, bool PLAIN>
+template <int DT, int DP, bool BIG, bool PLAIN>
 __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* keys, const uint8_t KVC_GLOBAL* values, uint32_t at,
                                             uint32_t next, uint32_t& page, const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, u32x4 KVC_LDS* v) {
   using S = Shape<DP, 1>;
@@ -539,10 +547,10 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   u32x4 w[1][2];
   wait_loads<N>();  // K and the page are there, V may be on its way
   from_here(page);
-  const Sources<DP, 1> from = sources_of<DP, 1>(p, u, at + next, page);
+  const Sources<DP, 1, BIG> from = sources_of<DP, 1, BIG>(p, u, at + next, page);
   products<DT, DP, 1>(k, query, s);
   wait_reads();
-  load_tile<DP, 1>(keys, from, k);
+  load_tile(u, keys, from, k);
   asm volatile("" ::: "memory");
   page = page_of_lane<S::TT>(p, u, at + 2 * next);  // (between this line and the wait below: it is one of the loads counted there)
   if constexpr (!PLAIN) mask<1>(p, u, at, s);
@@ -551,16 +559,16 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   if (!PLAIN && hides_tokens<S::TT>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
   else add_values<DT, DP, 1>(x, v, w);
   wait_reads();
-  load_tile<DP, 1>(values, from, v);
+  load_tile(u, values, from, v);
 }
 
 // The step for tiles that need no mask.  Loads of K do not touch V: told so the compiler does not have reads of one wait for the other.
 // (It keeps such notes for few loads of a kernel only; the steps with a mask go without.)
-template <int DT, int DP>
+template <int DT, int DP, bool BIG>
 __device__ __forceinline__ void plain_step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                                   const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
                                                   const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
-  step_of_one<DT, DP, true>(p, u, keys, values, at, next, page, query, x, k, v);
+  step_of_one<DT, DP, BIG, true>(p, u, keys, values, at, next, page, query, x, k, v);
 }
 
 // Which part of the work a unit is.
@@ -658,7 +666,7 @@ __device__ __forceinline__ void write_row(const AttendParams& p, bool shared, co
 }
 
 // One workgroup's unit: rows x head x piece of the tokens.
-template <int DT, int DP, int R>
+template <int DT, int DP, int R, bool BIG>
 __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, const Lds& lds, Tops& tops) {
   using S = Shape<DP, R>;
   constexpr int TT = S::TT, KK = DP / 16, DD = DP / 32;
@@ -676,9 +684,9 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
   constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a wave to its next
   const uint32_t start = u.t0 + (R == 1 ? wave_uniform(wave) * TT : 0);
-  uint32_t page[4];
+  uint32_t page[3];
 #pragma unroll
-  for (int i = 0; i < (R == 1 ? 2 : 4); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
+  for (int i = 0; i < (R == 1 ? 2 : 3); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
 
   const uint32_t base_row = (at_work.block * R + (R == 1 ? 0 : wave)) * 32;
   const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
@@ -687,6 +695,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   const bool there = load_query<DP>(p, q, shared, new_tokens, base_row + col, at_work.head, token, query);
   u.keys = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer] + (uint64_t)at_work.head * p.D * 2;
   u.values = u.keys + (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
+  u.span = (uint32_t)((uint64_t)p.pool.num_blocks * p.pool.page_bytes - (uint64_t)at_work.head * p.D * 2);
   if (shared) q = request_at(p, request_of(p.batch, token));
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
   if (shared ? u.t1 < p.prefix && threadIdx.x == 0 : false) fault(p, KVC_FAULT_LIST);
@@ -697,26 +706,27 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   // The first tiles.
   const bool any = u.t0 < u.t1, has_tile = start < u.t1;
   u32x4 KVC_LDS *k0, *v0, *k1 = nullptr, *v1 = nullptr;
-  Sources<DP, 4> next;
+  Sources<DP, 4, BIG> next;
   if constexpr (R == 1) {
     const uint32_t self = wave_uniform(wave);
     k0 = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
     v0 = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
     if (has_tile) {
-      const Sources<DP, 1> from = sources_of<DP, 1>(p, u, start, page[0]);
-      load_tile<DP, 1>(u.keys, from, k0);
-      load_tile<DP, 1>(u.values, from, v0);
+      const Sources<DP, 1, BIG> from = sources_of<DP, 1, BIG>(p, u, start, page[0]);
+      load_tile(u, u.keys, from, k0);
+      load_tile(u, u.values, from, v0);
       wait_loads<2 * S::LOADS>();  // (what has been asked for before)
     }
   } else {
     k0 = lds.a, v0 = lds.b, k1 = lds.c, v1 = lds.d;
     if (any) {
-      const Sources<DP, 4> from = sources_of<DP, 4>(p, u, start, page[0]);
-      next = sources_of<DP, 4>(p, u, start + TT, page[1]);
-      load_tile<DP, 4>(u.keys, from, k0);
-      load_tile<DP, 4>(u.values, from, v0);
-      load_tile<DP, 4>(u.keys, next, k1);
-      wait_loads<3 * S::LOADS>();
+      const Sources<DP, 4, BIG> from = sources_of<DP, 4, BIG>(p, u, start, page[0]);
+      next = sources_of<DP, 4, BIG>(p, u, start + TT, page[1]);
+      load_part<0, S::LOADS / 2>(u, u.keys, from, k1 + S::TILE / 2);
+      load_part<S::LOADS / 2, S::LOADS / 2>(u, u.keys, from, k0);
+      load_tile(u, u.values, from, v0);
+      load_part<0, S::LOADS / 2>(u, u.keys, next, k0 + S::TILE / 2);
+      wait_loads<5 * S::LOADS / 2>();
     }
   }
 
@@ -738,40 +748,31 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     for (int i = 0; i < 16; ++i) x.sum[d][i] = 0.0f;
   uint32_t pos = start;
   if constexpr (R == 1) {
-    for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) plain_step_of_one<DT, DP>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
-    for (; pos < end; pos += NEXT) step_of_one<DT, DP, false>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
+    for (; pos + TT <= plain && !u.bad_pages; pos += NEXT) plain_step_of_one<DT, DP, BIG>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
+    for (; pos < end; pos += NEXT) step_of_one<DT, DP, BIG, false>(p, u, u.keys, u.values, pos, NEXT, page[1], query, x, k0, v0);
   } else {
+    f32x16 s[1];
+    wait_loads<2 * S::LOADS>();  // K of the first 32 tokens
+    meet();
+    products<DT, DP, 1>(k1 + S::TILE / 2, query, s);
     if (pos + TT <= plain && !u.bad_pages) {
-      f32x16 s;
-      u32x4 first[kReads];
-      wait_loads<2 * S::LOADS>();  // the first K
-      meet();
-      s = mfma<DT>(key_at<DP>(k0, 0), query[0], f32x16{});
+      float top = s[0][0];
 #pragma unroll
-      for (int e = 1; e < KK; ++e) s = mfma<DT>(key_at<DP>(k0, e), query[e], s);
-#pragma unroll
-      for (int e = 0; e < kReads; ++e) first[e] = key_at<DP>(k0 + 32 * S::CH, e);
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
       move_base<DP>(p, x, top);
       // (whether a page is bad is known two tiles ahead)
       for (; pos + 2 * TT <= plain && !u.bad_pages; pos += 2 * TT) {
-        step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, s, first, lds.a, lds.b, lds.c, lds.d, true);
-        step_of_four<DT, DP>(p, u, pos + TT, next, page[3], query, x, s, first, lds.c, lds.d, lds.a, lds.b, pos + 3 * TT <= plain);
+        step_of_four<DT, DP, BIG>(p, u, pos, next, page[2], query, x, s[0], lds.a, lds.b, lds.c, lds.d, true);
+        step_of_four<DT, DP, BIG>(p, u, pos + TT, next, page[2], query, x, s[0], lds.c, lds.d, lds.a, lds.b, pos + 3 * TT <= plain);
       }
       if (pos + TT <= plain && !u.bad_pages) {
-        step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, s, first, lds.a, lds.b, lds.c, lds.d, false);
+        step_of_four<DT, DP, BIG>(p, u, pos, next, page[2], query, x, s[0], lds.a, lds.b, lds.c, lds.d, false);
         pos += TT;
         k0 = lds.c, v0 = lds.d, k1 = lds.a, v1 = lds.b;
-        const uint32_t other = page[3];
-        page[3] = page[2], page[2] = other;
       }
     }
     for (; pos < end; pos += TT) {
-      masked_step_of_four<DT, DP>(p, u, pos, next, page[2], query, x, k0, v0, v1);
-      const uint32_t other = page[3];
-      page[3] = page[2], page[2] = other;
+      masked_step_of_four<DT, DP, BIG>(p, u, pos, next, page[2], query, x, s[0], k0, v0, k1, v1);
       u32x4 KVC_LDS* const k2 = k0;
       u32x4 KVC_LDS* const v2 = v0;
       k0 = k1, v0 = v1;
@@ -824,7 +825,7 @@ __device__ __forceinline__ bool unit_of(const AttendParams& p, bool& shared, uin
   return unit < units;
 }
 
-template <int DT, int DP>
+template <int DT, int DP, bool BIG>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
   __shared__ u32x4 a[quarter<DP>()], b[quarter<DP>()], c[quarter<DP>()], d[quarter<DP>()];
   __shared__ Tops tops;
@@ -833,8 +834,8 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendPar
   uint32_t unit;
   if (!unit_of(p, shared, unit)) return;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  if (part.waves == 1) attend_unit<DT, DP, 1>(p, part, shared, unit, lds, tops);
-  else attend_unit<DT, DP, 4>(p, part, shared, unit, lds, tops);
+  if (part.waves == 1) attend_unit<DT, DP, 1, BIG>(p, part, shared, unit, lds, tops);
+  else attend_unit<DT, DP, 4, BIG>(p, part, shared, unit, lds, tops);
 }
 
 // Joins the pieces of rows: a workgroup takes LINES rows (a token and a head), and 256 / LINES threads a row.  First the weights of all of
@@ -922,7 +923,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   const uint32_t groups = (p.part[0].units + 7) / 8 * 8 + (p.part[1].units + 7) / 8 * 8;
-  if (groups) hipLaunchKernelGGL((attend_kernel<DT, DP>), dim3(groups), dim3(256), 0, stream, p);
+  const bool big = (uint64_t)p.pool.num_blocks * p.pool.page_bytes > 0xffff0000u;  // (offsets of what is not there lie above)
+  if (groups && big) hipLaunchKernelGGL((attend_kernel<DT, DP, true>), dim3(groups), dim3(256), 0, stream, p);
+  if (groups && !big) hipLaunchKernelGGL((attend_kernel<DT, DP, false>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   if (p.pieces != 1) {  // (no piece at all: every row is empty)
     // Few rows of many pieces take a workgroup each, many rows share one.
