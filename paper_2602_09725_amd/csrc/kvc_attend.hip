@@ -580,6 +580,7 @@ __device__ __forceinline__ Place place_of_unit(const AttendParams& p, const Atte
   Place w;
   uint32_t rest;
   fd_divmod(part.drows, unit, rest, w.block);
+  if (!shared) w.block = part.row_blocks - 1 - w.block;  // (of a prompt the last rows see the most, and are begun first)
   fd_divmod(part.dsplits, rest, rest, w.split);
   w.head = rest;
   w.request = 0;
