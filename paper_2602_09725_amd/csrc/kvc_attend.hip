@@ -111,12 +111,12 @@ __device__ __forceinline__ uint32_t prefix_there(const AttendParams& p) {
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------------
 
-// Where the 16-byte vector `chunk` of a token's row lies in the row in LDS.  Reads of K take one chunk of 32 tokens that follow one
-// another, transposing reads of V two of four: both find them in different banks.
+// Where the 16-byte vector `chunk` of a token's row lies in the row in LDS, whose 64 banks hold 16 such vectors.  Reads of K take one chunk of 16
+// tokens that follow one another at a time, transposing reads of V four chunks of four tokens: both find them in different banks.
 template <int CH>
 __device__ __forceinline__ uint32_t place(uint32_t token, uint32_t chunk) {
-  constexpr uint32_t B = CH >= 16 ? 16 : CH, LOG = B == 16 ? 4 : 3;
-  return chunk ^ (((token << 1) & (B - 1)) | ((token >> (LOG - 1)) & 1u));
+  if constexpr (CH >= 16) return chunk ^ ((token & 3u) << 2 | ((token >> 2) & 3u));
+  else return chunk ^ (((token >> 1) & 1u) << 2 | ((token >> 2) & 3u));  // (two rows lie side by side)
 }
 
 template <int DT>
@@ -431,7 +431,7 @@ __device__ __forceinline__ u32x4 key_at(const u32x4 KVC_LDS* k, int e) {
   return k[col * (DP / 8) + place<DP / 8>(col, (uint32_t)e * 2 + half)];
 }
 
-constexpr int kReads = 4;  // reads of LDS that are under way
+constexpr int kReads = 3;  // reads of LDS that are under way
 
 // 32 tokens that all rows see all of: their products are in s, V in v; s gets the products of the 32 at k.  `first` holds K's first
 // vectors, and gets those of the 32 tokens after these, at k2, if they are there by now (NEXT).  more: what is at k will be taken.  The matrix unit and the other
