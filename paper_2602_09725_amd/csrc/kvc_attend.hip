@@ -497,14 +497,27 @@ __device__ __forceinline__ void begin_step(const AttendParams& p, Unit& u, uint3
   page = page_of_lane<S::TT>(p, u, at + 3 * S::TT);
 }
 
+// Rows of more than 128 elements take a wave's whole registers, half of which only matrix instructions use at once: what they use goes there.
+// (Left to itself the compiler keeps the queries in memory, and reading them waits for the loads of the next tile as well.)
+template <int DP>
+__device__ __forceinline__ void hold(u32x4 (&query)[DP / 16], State<DP>& x) {
+  if constexpr (DP > 128) {
+#pragma unroll
+    for (int e = 0; e < DP / 16; ++e) asm volatile("" : "+a"(query[e]));
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) asm volatile("" : "+a"(x.sum[d]));
+  }
+}
+
 // A tile that all rows see all of.  s holds the products of its first half, and gets those of the next tile's.  more: these are seen by
 // all rows as well.
 template <int DT, int DP, bool BIG>
-__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4, BIG>& next, uint32_t& page, const u32x4 (&query)[DP / 16],
+__device__ __forceinline__ void step_of_four(const AttendParams& p, Unit& u, uint32_t at, Sources<DP, 4, BIG>& next, uint32_t& page, u32x4 (&query)[DP / 16],
                                              State<DP>& x, f32x16& s, const u32x4 KVC_LDS* k, const u32x4 KVC_LDS* v, u32x4 KVC_LDS* k2, u32x4 KVC_LDS* v2,
                                              bool more) {
   constexpr int HALF = Shape<DP, 4>::TILE / 2;
   u32x4 first[kReads];
+  hold<DP>(query, x);
   begin_step<DP, BIG>(p, u, at, next, page, first, k, k2, v2);
   take_tokens<DT, DP, true>(p, x, query, s, first, k, v, k + HALF, true);
   take_tokens<DT, DP, false>(p, x, query, s, first, k + HALF, v + HALF, nullptr, more);
@@ -540,11 +553,12 @@ __device__ __forceinline__ void masked_step_of_four(const AttendParams& p, Unit&
 // follow them as soon as each has been read.
 template <int DT, int DP, bool BIG, bool PLAIN>
 __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* keys, const uint8_t KVC_GLOBAL* values, uint32_t at,
-                                            uint32_t next, uint32_t& page, const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, u32x4 KVC_LDS* v) {
+                                            uint32_t next, uint32_t& page, u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* k, u32x4 KVC_LDS* v) {
   using S = Shape<DP, 1>;
   constexpr int N = S::LOADS;
   f32x16 s[1];
   u32x4 w[1][2];
+  hold<DP>(query, x);
   wait_loads<N>();  // K and the page are there, V may be on its way
   from_here(page);
   const Sources<DP, 1, BIG> from = sources_of<DP, 1, BIG>(p, u, at + next, page);
@@ -567,7 +581,7 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
 template <int DT, int DP, bool BIG>
 __device__ __forceinline__ void plain_step_of_one(const AttendParams& p, Unit& u, const uint8_t KVC_GLOBAL* __restrict__ keys,
                                                   const uint8_t KVC_GLOBAL* __restrict__ values, uint32_t at, uint32_t next, uint32_t& page,
-                                                  const u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
+                                                  u32x4 (&query)[DP / 16], State<DP>& x, u32x4 KVC_LDS* __restrict__ k, u32x4 KVC_LDS* __restrict__ v) {
   step_of_one<DT, DP, BIG, true>(p, u, keys, values, at, next, page, query, x, k, v);
 }
 
