@@ -1,9 +1,10 @@
 // Pages of a pool: copied, forked, taken, freed, compacted; and the tokens of a step written to their slots.
 //
-// The books are small (four bytes a page) and the pages large, so every call that takes pages has two launches: a survey
-// that leaves a bit for each free page, the number of free ones of each segment of 4096 pages and, from the list, how
-// many pages the entries before each entry take; then one in which every workgroup finds the pages of its own entry in the
-// bits by their rank.  Nothing depends on the order in which workgroups run: the k-th page taken is the k-th free one,
+// The books are small (four bytes a page) and the pages large.  The books of a pool of up to kOnePages pages are one workgroup's
+// work, which has a bit for each free page in LDS: growing rows is one launch, and forking and compacting are this one and a second one that moves
+// the data.  In larger pools a survey by many workgroups leaves a bit for each free page, the number of free ones of each segment of
+// 4096 pages and, from the list, how many pages the entries before each entry take; then every workgroup finds the pages of its
+// own entry in the bits by their rank.  Nothing depends on the order in which workgroups run: the k-th page taken is the k-th free one,
 // counts change by atomic additions of whole numbers, and what one workgroup reads of the books no other one of the launch writes.
 #include <hip/hip_runtime.h>
 
@@ -53,21 +54,71 @@ __device__ uint64_t group_scan(uint32_t v, uint64_t* sums, uint64_t* total) {
   return before + inclusive - v;
 }
 
-// Checks a fork's or a grow's list and counts the pages its entries take.  `seen` has a bit for each row.
+// Notes a row that an entry of a list changes in `seen`, a bit for each row; len: its length.
+template <PageList LIST>
+__device__ __forceinline__ uint32_t note_row(const PoolView& p, uint32_t row, int32_t len, uint32_t* seen) {
+  if (row >= p.n_rows) return KVC_FAULT_LIST;
+  const bool twice = atomicOr(&seen[row / 32], 1u << (row % 32)) >> (row % 32) & 1u;
+  return twice || (LIST == PageList::kFork && len != 0) ? KVC_FAULT_LIST : 0u;
+}
+
+// A fork's parent may not be a row that the call changes.
+__device__ __forceinline__ uint32_t parent_noted(const PoolView& p, uint32_t row, const uint32_t* seen) {
+  return row < p.n_rows && (seen[row / 32] >> (row % 32) & 1u) ? KVC_FAULT_LIST : 0u;
+}
+
+// What an entry of a list takes: its row (a fork's parent), the row's length and pages, and how many pages it needs for `more` tokens.
+struct Entry {
+  uint32_t row, len, held, need, more;
+  uint32_t last;  // page that is filled in part, if there is one
+};
+
+template <PageList LIST>
+__device__ __forceinline__ Entry entry_of(const PoolView& p, uint32_t row, int32_t more, uint32_t& bad) {
+  Entry e{};
+  const uint32_t len = row < p.n_rows ? (uint32_t)p.lens[row] : ~0u;
+  if (row >= p.n_rows || len > p.capacity) {
+    bad |= KVC_FAULT_LIST;
+    return e;
+  }
+  e.row = row;
+  e.len = len;
+  const uint32_t whole = fd_div(p.dbs, len);
+  e.held = pages_of(p, len);
+  const bool part = e.held != whole;
+  if (part) e.last = (uint32_t)p.tables[(uint64_t)row * p.table_len + whole];
+  if (LIST == PageList::kFork) {
+    e.need = part;
+  } else if (more < 0) {
+    bad |= KVC_FAULT_LIST;
+  } else if ((uint32_t)more > p.capacity - len) {
+    bad |= KVC_FAULT_NO_ROOM;
+  } else {
+    e.more = (uint32_t)more;
+    e.need = pages_of(p, len + e.more) - e.held;
+    if (part && more > 0) {  // its last page will be written to
+      if (e.last >= p.num_blocks) fault(p, KVC_FAULT_PAGE);
+      else if (p.refs[e.last] > 1) bad |= KVC_FAULT_LIST;
+    }
+  }
+  return e;
+}
+
+// The faults that any thread of a workgroup has met; all of them call it.
+__device__ __forceinline__ uint32_t all_faults(uint32_t bad) {
+  return (__syncthreads_or(bad & KVC_FAULT_LIST) ? KVC_FAULT_LIST : 0u) | (__syncthreads_or(bad & KVC_FAULT_NO_ROOM) ? KVC_FAULT_NO_ROOM : 0u);
+}
+
+// Checks a fork's or a grow's list and counts the pages its entries take.
 template <PageList LIST>
 __device__ void plan_list(const PoolView& p, const PageSpace& w, const int32_t* a, const int32_t* b, uint32_t n, uint32_t* seen, uint64_t* sums) {
   for (uint32_t i = threadIdx.x; i < (p.n_rows + 31) / 32; i += blockDim.x) seen[i] = 0;
   __syncthreads();
   uint32_t bad = 0;
-  const int32_t* written = LIST == PageList::kFork ? b : a;  // rows that the call changes
+  const int32_t* written = LIST == PageList::kFork ? b : a;
   for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
     const uint32_t row = (uint32_t)written[i];
-    if (row >= p.n_rows) {
-      bad |= KVC_FAULT_LIST;
-      continue;
-    }
-    if (atomicOr(&seen[row / 32], 1u << (row % 32)) >> (row % 32) & 1u) bad |= KVC_FAULT_LIST;
-    if (LIST == PageList::kFork && p.lens[row] != 0) bad |= KVC_FAULT_LIST;
+    bad |= note_row<LIST>(p, row, row < p.n_rows ? p.lens[row] : 0, seen);
   }
   __syncthreads();
   uint64_t all = 0;
@@ -76,28 +127,8 @@ __device__ void plan_list(const PoolView& p, const PageSpace& w, const int32_t* 
     uint32_t need = 0;
     if (i < n) {
       const uint32_t row = (uint32_t)a[i];
-      const uint32_t len = row < p.n_rows ? (uint32_t)p.lens[row] : ~0u;
-      if (row >= p.n_rows || len > p.capacity) {
-        bad |= KVC_FAULT_LIST;
-      } else if (LIST == PageList::kFork) {
-        if (seen[row / 32] >> (row % 32) & 1u) bad |= KVC_FAULT_LIST;
-        need = len - fd_div(p.dbs, len) * p.block_size != 0;
-      } else {
-        const int32_t more = b ? b[i] : 1;
-        const uint32_t held = pages_of(p, len), whole = fd_div(p.dbs, len);
-        if (more < 0) {
-          bad |= KVC_FAULT_LIST;
-        } else if ((uint32_t)more > p.capacity - len) {
-          bad |= KVC_FAULT_NO_ROOM;
-        } else {
-          need = pages_of(p, len + (uint32_t)more) - held;
-          if (held != whole && more > 0) {  // its last page will be written to
-            const uint32_t page = (uint32_t)p.tables[(uint64_t)row * p.table_len + whole];
-            if (page >= p.num_blocks) fault(p, KVC_FAULT_PAGE);
-            else if (p.refs[page] > 1) bad |= KVC_FAULT_LIST;
-          }
-        }
-      }
+      if (LIST == PageList::kFork) bad |= parent_noted(p, row, seen);
+      need = entry_of<LIST>(p, row, LIST == PageList::kGrow && b ? b[i] : 1, bad).need;
     }
     uint64_t total;
     const uint64_t before = group_scan(need, sums, &total);
@@ -105,7 +136,7 @@ __device__ void plan_list(const PoolView& p, const PageSpace& w, const int32_t* 
     all += total;
   }
   if (all > p.num_blocks) bad |= KVC_FAULT_NO_ROOM;
-  const uint32_t faults = (__syncthreads_or(bad & KVC_FAULT_LIST) ? KVC_FAULT_LIST : 0u) | (__syncthreads_or(bad & KVC_FAULT_NO_ROOM) ? KVC_FAULT_NO_ROOM : 0u);
+  const uint32_t faults = all_faults(bad);
   if (threadIdx.x == 0) {
     w.head[kPlanFaults] = faults;
     w.head[kPlanNeed] = (uint32_t)all;
@@ -197,6 +228,186 @@ __device__ void take_pages(const PageSpace& w, uint32_t first, uint32_t m, Emit 
   }
 }
 
+// Compact's lists, at one page: of a page in use at a place below the number of pages in use `moved` gets the place, of a free one -1, of one
+// that moves -2 - its rank among these.  word: the bits of its 32 pages; before: free pages before these; low: free places below `used`.
+__device__ __forceinline__ void list_page(const PoolView& p, const PageSpace& w, uint32_t page, uint32_t word, uint32_t before, uint32_t used,
+                                          uint32_t low) {
+  const uint32_t bit = page % 32, free_rank = before + (uint32_t)__popc(word & ((1u << bit) - 1u));
+  int32_t to = -1;
+  if (word >> bit & 1u) {
+    if (page < used) w.places[free_rank] = (int32_t)page;
+  } else if (page < used) {
+    to = (int32_t)page;
+  } else {
+    const uint32_t rank = page - free_rank - (used - low);  // pages in use before it, but for those below `used`
+    w.sources[rank] = (int32_t)page;
+    to = -2 - (int32_t)rank;
+  }
+  w.moved[page] = to;
+  w.refs[page] = p.refs[page] < 0 ? 0 : p.refs[page];
+}
+
+// ---- small pools ----------------------------------------------------------------------------------------------------------
+
+// The books of a small pool in one workgroup: a bit for each free page, and the free ones before each word of them.
+constexpr uint32_t kOneThreads = 1024, kOneWords = kOnePages / 32;
+struct OneBooks {
+  uint64_t sums[kOneThreads / 64];
+  uint32_t words[kOneWords], before[kOneWords];
+  uint32_t faults;
+};
+
+// What a thread's entry of a list takes, how many pages the entries before it take, and what is true of all.
+struct OnePlan {
+  Entry e;
+  uint32_t first, free_pages, total, faults;
+};
+
+// Fills the books and checks a fork's or a grow's list, an entry a thread.  The call's time is that of memory's answers one after the other, so what can be
+// asked for at once is, and free pages and needs are added up together (2^14 free ones at most, the needs below them).
+template <PageList LIST>
+__device__ __forceinline__ OnePlan plan_one(const PoolView& p, OneBooks& s, const int32_t* a, const int32_t* b, uint32_t n, uint32_t* seen) {
+  constexpr uint32_t kWaves = kOneThreads / 64;
+  const uint32_t self = threadIdx.x, wave = self / 64;
+  const bool mine = LIST != PageList::kNone && self < n;
+  OnePlan plan{};
+  uint32_t row = ~0u, bad = 0;
+  int32_t other = 1, other_len = 0;
+  if (mine) {
+    row = (uint32_t)a[self];
+    if (LIST == PageList::kFork || b) other = b[self];
+  }
+  int32_t refs[kOnePages / kOneThreads];
+#pragma unroll
+  for (uint32_t i = 0; i < kOnePages / kOneThreads; ++i) {
+    const uint32_t page = i * kOneThreads + self;
+    refs[i] = page < p.num_blocks ? p.refs[page] : 1;
+  }
+  if (LIST != PageList::kNone)
+    for (uint32_t i = self; i < (p.n_rows + 31) / 32; i += kOneThreads) seen[i] = 0;
+  if (self == 0) s.faults = 0;
+  if (mine) {
+    if (LIST == PageList::kFork && (uint32_t)other < p.n_rows) other_len = p.lens[other];
+    plan.e = entry_of<LIST>(p, row, other, bad);
+  }
+  bool below = false;
+#pragma unroll
+  for (uint32_t i = 0; i < kOnePages / kOneThreads; ++i) {
+    const uint64_t bits = __ballot(refs[i] <= 0);
+    below |= refs[i] < 0;
+    if (lane_id() == 0) {
+      uint32_t* to = s.words + (i * kOneThreads + self) / 32;
+      to[0] = (uint32_t)bits;
+      to[1] = (uint32_t)(bits >> 32);
+    }
+  }
+  if (__any(below) && lane_id() == 0) fault(p, KVC_FAULT_LIST);
+  __syncthreads();
+  if (mine) bad |= note_row<LIST>(p, LIST == PageList::kFork ? (uint32_t)other : row, other_len, seen);
+  const uint64_t v = (uint64_t)(self < kOneWords ? __popc(s.words[self]) : 0) << 44 | plan.e.need;
+  const uint64_t inclusive = wave_scan<unsigned long long>(v);
+  if (lane_id() == 63) s.sums[wave] = inclusive;
+  if (LIST == PageList::kFork) {
+    __syncthreads();
+    if (mine) bad |= parent_noted(p, row, seen);
+  }
+  if (bad) atomicOr(&s.faults, bad);
+  __syncthreads();
+  uint64_t before = inclusive - v, all = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kWaves; ++w) {
+    if (w < wave) before += s.sums[w];
+    all += s.sums[w];
+  }
+  if (self < kOneWords) s.before[self] = (uint32_t)(before >> 44);
+  const uint64_t needs = (1ull << 44) - 1;
+  plan.first = (uint32_t)(before & needs);  // (used only where all of them are fewer than the free pages)
+  plan.free_pages = (uint32_t)(all >> 44);
+  plan.total = (uint32_t)(all & needs);
+  plan.faults = s.faults & (KVC_FAULT_LIST | KVC_FAULT_NO_ROOM);
+  if (!plan.faults && (all & needs) > plan.free_pages) plan.faults = KVC_FAULT_NO_ROOM;
+  if (self == 0) fault(p, plan.faults);
+  return plan;  // (s.before is there for all threads after the next barrier)
+}
+
+// The free page of a rank that there is.
+__device__ uint32_t page_of_rank(const OneBooks& s, uint32_t rank) {
+  uint32_t k = 0;
+#pragma unroll
+  for (uint32_t step = kOneWords / 2; step; step /= 2)
+    if (s.before[k + step] <= rank) k += step;
+  uint32_t bits = s.words[k];
+  for (uint32_t skip = rank - s.before[k]; skip; --skip) bits &= bits - 1;
+  return k * 32 + (uint32_t)__ffs(bits) - 1;
+}
+
+// What a fork leaves for the launch that copies: where the tokens of the parent's last page come from and go to, and how many they are.
+__global__ void __launch_bounds__(kOneThreads) plan_fork_kernel(PoolView p, PageSpace w, const int32_t* parents, const int32_t* children, uint32_t n) {
+  extern __shared__ uint32_t seen[];
+  __shared__ OneBooks s;
+  const uint32_t i = threadIdx.x;
+  const uint32_t child = i < n ? (uint32_t)children[i] : 0u;
+  const OnePlan plan = plan_one<PageList::kFork>(p, s, parents, children, n, seen);
+  const Entry& e = plan.e;
+  if (i == 0) w.head[kPlanFaults] = plan.faults;
+  __syncthreads();
+  if (i >= n || plan.faults) return;
+  ForkJob job = {0, 0, 0, e.len};
+  if (e.need) {
+    const uint64_t whole = e.held - 1;
+    job.to = page_of_rank(s, plan.first);
+    job.from = e.last;
+    job.tokens = e.len - (uint32_t)whole * p.block_size;
+    p.tables[(uint64_t)child * p.table_len + whole] = (int32_t)job.to;
+    p.refs[job.to] = 1;
+    if (job.from >= p.num_blocks) {
+      fault(p, KVC_FAULT_PAGE);
+      job.tokens = 0;
+    }
+  }
+  p.lens[child] = (int32_t)e.len;
+  w.jobs[i] = job;
+}
+
+__global__ void __launch_bounds__(kOneThreads) grow_one_kernel(PoolView p, const int32_t* rows, const int32_t* counts, uint32_t n) {
+  extern __shared__ uint32_t seen[];
+  __shared__ OneBooks s;
+  __shared__ uint32_t first[kOneThreads];
+  __shared__ uint64_t to[kOneThreads];
+  const uint32_t i = threadIdx.x;
+  const OnePlan plan = plan_one<PageList::kGrow>(p, s, rows, counts, n, seen);
+  const Entry& e = plan.e;
+  first[i] = i < n ? plan.first : ~0u;
+  to[i] = (uint64_t)e.row * p.table_len + e.held;
+  __syncthreads();
+  if (plan.faults) return;
+  for (uint32_t rank = i; rank < plan.total; rank += kOneThreads) {
+    uint32_t k = 0;  // the last entry that begins at or before it: those after it that need none begin later
+#pragma unroll
+    for (uint32_t step = kOneThreads / 2; step; step /= 2)
+      if (first[k + step] <= rank) k += step;
+    const uint32_t page = page_of_rank(s, rank);
+    p.tables[to[k] + rank - first[k]] = (int32_t)page;
+    p.refs[page] = 1;
+  }
+  if (i < n) p.lens[e.row] = (int32_t)(e.len + e.more);
+}
+
+// The lists of compact, as compact_lists_kernel leaves them.
+__global__ void __launch_bounds__(kOneThreads) compact_one_kernel(PoolView p, PageSpace w) {
+  __shared__ OneBooks s;
+  const uint32_t used = p.num_blocks - plan_one<PageList::kNone>(p, s, nullptr, nullptr, 0, nullptr).free_pages;
+  __syncthreads();
+  const uint32_t word = used / 32;  // (none is free if all are in use)
+  const uint32_t low = used < p.num_blocks ? s.before[word] + (uint32_t)__popc(s.words[word] & ((1u << used % 32) - 1u)) : 0u;
+  for (uint32_t page = threadIdx.x; page < p.num_blocks; page += kOneThreads)
+    list_page(p, w, page, s.words[page / 32], s.before[page / 32], used, low);
+  if (threadIdx.x == 0) {
+    w.head[kPlanUsed] = used;
+    w.head[kPlanMoves] = low;
+  }
+}
+
 // ---- moving data ----------------------------------------------------------------------------------------------------------
 
 constexpr uint32_t kPiece = 32768;  // bytes that a workgroup of 256 threads moves in one go, eight loads a thread in flight
@@ -211,14 +422,21 @@ __device__ __forceinline__ void copy_piece(uint8_t* dst, const uint8_t* src, uin
     for (uint32_t u = 0; u < U; ++u) v[u] = stream_load<u32x4>(src + first + u * 4096);
 #pragma unroll
     for (uint32_t u = 0; u < U; ++u) stream_store<u32x4>(dst + first + u * 4096, v[u]);
-  } else {  // two at a time
-    for (uint32_t at = first; at < bytes; at += 8192) {
-      const bool two = at + 4096 < bytes;
-      const u32x4 a = stream_load<u32x4>(src + at), b = stream_load<u32x4>(src + (two ? at + 4096 : at));
-      stream_store<u32x4>(dst + at, a);
-      if (two) stream_store<u32x4>(dst + at + 4096, b);
-    }
+  } else {
+    u32x4 v[U];
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (first + u * 4096 < bytes) v[u] = stream_load<u32x4>(src + first + u * 4096);
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (first + u * 4096 < bytes) stream_store<u32x4>(dst + first + u * 4096, v[u]);
   }
+}
+
+// Bytes of the k-th piece of so many.  (In 32 bits: of a choice by a 64-bit comparison of uniform values the compiler has been seen to take
+// the wrong side, the comparison in one flag and the choice by another.)
+__device__ __forceinline__ uint32_t piece_bytes(uint64_t all, uint32_t k) {
+  return k < (uint32_t)(all / kPiece) ? kPiece : (uint32_t)all % kPiece;
 }
 
 __device__ __forceinline__ uint8_t* page_at(const PoolView& p, uint32_t layer, uint32_t kind, uint32_t page) {
@@ -237,51 +455,65 @@ __global__ void __launch_bounds__(256) copy_kernel(PoolView p, const int32_t* sr
     if (threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
     return;
   }
-  const uint64_t at = (uint64_t)piece * kPiece, left = p.page_bytes - at;
+  const uint64_t at = (uint64_t)piece * kPiece;
   copy_piece(page_at(p, layer_kind / 2, layer_kind % 2, to) + at, page_at(p, layer_kind / 2, layer_kind % 2, from) + at,
-             left < kPiece ? (uint32_t)left : kPiece);
+             piece_bytes(p.page_bytes, piece));
 }
 
-// Workgroup: one layer of one fork.
-__global__ void __launch_bounds__(256) fork_kernel(PoolView p, PageSpace w, const int32_t* parents, const int32_t* children, FastDiv dL) {
-  uint32_t i, layer;
-  fd_divmod(dL, blockIdx.x, i, layer);
-  if (!plan_stands(p, w)) return;
-  const uint32_t parent = (uint32_t)as_const(parents)[i], child = (uint32_t)as_const(children)[i];
-  const uint32_t len = (uint32_t)p.lens[parent], whole = fd_div(p.dbs, len), part = len - whole * p.block_size;
-  const int32_t* from = p.tables + (uint64_t)parent * p.table_len;
-  int32_t* to = p.tables + (uint64_t)child * p.table_len;
-  if (layer == 0) {
-    for (uint32_t j = threadIdx.x; j < whole; j += 256) {
-      const uint32_t page = (uint32_t)from[j];
-      to[j] = (int32_t)page;
-      if (page < p.num_blocks) atomicAdd(p.refs + page, 1);
-      else fault(p, KVC_FAULT_PAGE);
-    }
-    if (threadIdx.x == 0) p.lens[child] = (int32_t)len;
+// Workgroup: one kind of one layer of one fork.  KNOWN: plan_fork_kernel has written the books but for the pages that are shared.
+template <bool KNOWN>
+__global__ void __launch_bounds__(256) fork_kernel(PoolView p, PageSpace w, const int32_t* parents, const int32_t* children, FastDiv dkinds) {
+  uint32_t i, layer_kind;
+  fd_divmod(dkinds, blockIdx.x, i, layer_kind);
+  ForkJob job;
+  if constexpr (KNOWN) {
+    job = __builtin_bit_cast(ForkJob, as_const(reinterpret_cast<const u32x4*>(w.jobs))[i]);
+    if (as_const(w.head)[kPlanFaults]) return;
+  } else {
+    if (!plan_stands(p, w)) return;
+    job.len = (uint32_t)p.lens[as_const(parents)[i]];
   }
-  if (part == 0) return;
-  __shared__ uint32_t taken;
-  if (threadIdx.x < 64)
-    take_pages(w, w.first[i], 1, [&](uint32_t, uint32_t page) {
-      taken = page;
-      if (layer == 0) {
-        to[whole] = (int32_t)page;
-        p.refs[page] = 1;
+  const uint32_t whole = fd_div(p.dbs, job.len);
+  if (layer_kind == 0 || !KNOWN) {
+    const uint32_t parent = (uint32_t)as_const(parents)[i], child = (uint32_t)as_const(children)[i];
+    const int32_t* from = p.tables + (uint64_t)parent * p.table_len;
+    int32_t* to = p.tables + (uint64_t)child * p.table_len;
+    if (layer_kind == 0) {
+      for (uint32_t j = threadIdx.x; j < whole; j += 256) {
+        const uint32_t page = (uint32_t)from[j];
+        to[j] = (int32_t)page;
+        if (page < p.num_blocks) atomicAdd(p.refs + page, 1);
+        else fault(p, KVC_FAULT_PAGE);
       }
-    });
-  __syncthreads();
-  const uint32_t page = taken, source = (uint32_t)from[whole];
-  if (source >= p.num_blocks) {
-    if (threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
-    return;
+    }
+    if constexpr (!KNOWN) {
+      job.tokens = job.len - whole * p.block_size;
+      if (layer_kind == 0 && threadIdx.x == 0) p.lens[child] = (int32_t)job.len;
+      if (job.tokens == 0) return;
+      __shared__ uint32_t taken;
+      if (threadIdx.x < 64)
+        take_pages(w, w.first[i], 1, [&](uint32_t, uint32_t page) {
+          taken = page;
+          if (layer_kind == 0) {
+            to[whole] = (int32_t)page;
+            p.refs[page] = 1;
+          }
+        });
+      __syncthreads();
+      job.to = taken;
+      job.from = (uint32_t)from[whole];
+      if (job.from >= p.num_blocks) {
+        if (threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
+        return;
+      }
+    }
   }
-  const uint64_t bytes = (uint64_t)part * p.token_bytes;
-  for (uint32_t kind = 0; kind < 2; ++kind) {
-    uint8_t* d = page_at(p, layer, kind, page);
-    const uint8_t* s = page_at(p, layer, kind, source);
-    for (uint64_t at = 0; at < bytes; at += kPiece) copy_piece(d + at, s + at, bytes - at < kPiece ? (uint32_t)(bytes - at) : kPiece);
-  }
+  if (job.tokens == 0) return;
+  const uint64_t bytes = (uint64_t)job.tokens * p.token_bytes;
+  uint8_t* d = page_at(p, layer_kind / 2, layer_kind % 2, job.to);
+  const uint8_t* s = page_at(p, layer_kind / 2, layer_kind % 2, job.from);
+  const uint32_t pieces = (uint32_t)((bytes + kPiece - 1) / kPiece);
+  for (uint32_t k = 0; k < pieces; ++k) copy_piece(d + (uint64_t)k * kPiece, s + (uint64_t)k * kPiece, piece_bytes(bytes, k));
 }
 
 // Wave: one row of the list.
@@ -330,8 +562,7 @@ __global__ void __launch_bounds__(256) free_kernel(PoolView p, const int32_t* ro
 
 // ---- compact --------------------------------------------------------------------------------------------------------------
 
-// Workgroup: a segment.  Of a page in use at a place below the number of pages in use `moved` gets the place, of a free one -1, of one that
-// moves -2 - its rank among these.
+// Workgroup: a segment.
 __global__ void __launch_bounds__(256) compact_lists_kernel(PoolView p, PageSpace w) {
   __shared__ uint32_t words[kSegmentWords], before[kSegmentWords];
   const uint32_t seg = blockIdx.x;
@@ -360,20 +591,7 @@ __global__ void __launch_bounds__(256) compact_lists_kernel(PoolView p, PageSpac
   for (uint32_t i = 0; i < kSegment / 256; ++i) {
     const uint32_t at = i * 256 + threadIdx.x, page = seg * kSegment + at;
     if (page >= p.num_blocks) break;
-    const uint32_t word = words[at / 32], bit = at % 32;
-    const uint32_t free_rank = free_earlier + before[at / 32] + (uint32_t)__popc(word & ((1u << bit) - 1u));
-    int32_t to = -1;
-    if (word >> bit & 1u) {
-      if (page < used) w.places[free_rank] = (int32_t)page;
-    } else if (page < used) {
-      to = (int32_t)page;
-    } else {
-      const uint32_t rank = page - free_rank - (used - moves);  // pages in use before it, but for those below `used`
-      w.sources[rank] = (int32_t)page;
-      to = -2 - (int32_t)rank;
-    }
-    w.moved[page] = to;
-    w.refs[page] = p.refs[page] < 0 ? 0 : p.refs[page];
+    list_page(p, w, page, words[at / 32], free_earlier + before[at / 32], used, moves);
   }
   if (seg == 0 && threadIdx.x == 0) {
     w.head[kPlanUsed] = used;
@@ -395,9 +613,10 @@ __global__ void __launch_bounds__(256) compact_kernel(PoolView p, PageSpace w, i
     const uint64_t units = (uint64_t)moves * a_page;
     for (uint64_t unit = blockIdx.x; unit < units; unit += movers) {
       const uint32_t k = (uint32_t)(unit / a_page), rest = (uint32_t)(unit - (uint64_t)k * a_page), lk = rest / pieces;
-      const uint64_t at = (uint64_t)(rest - lk * pieces) * kPiece, left = p.page_bytes - at;
+      const uint32_t piece = rest - lk * pieces;
+      const uint64_t at = (uint64_t)piece * kPiece;
       copy_piece(page_at(p, lk / 2, lk % 2, (uint32_t)as_const(w.places)[k]) + at, page_at(p, lk / 2, lk % 2, (uint32_t)as_const(w.sources)[k]) + at,
-                 left < kPiece ? (uint32_t)left : kPiece);
+                 piece_bytes(p.page_bytes, piece));
     }
     return;
   }
@@ -513,6 +732,11 @@ kvc_status launched() { return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ER
 
 }  // namespace
 
+namespace {
+
+// Whether one workgroup looks after a call's books: of pools of kOnePages pages, and lists of an entry a thread.
+bool one_group(const PoolView& pool, uint32_t n) { return pool.num_blocks <= kOnePages && n <= kOneThreads; }
+
 kvc_status launch_survey(const PoolView& pool, const PageSpace& w, PageList list, const int32_t* a, const int32_t* b, uint32_t n,
                          hipStream_t stream) {
   const uint32_t seen = list == PageList::kNone ? 0 : (pool.n_rows + 31) / 32 * 4;
@@ -520,15 +744,32 @@ kvc_status launch_survey(const PoolView& pool, const PageSpace& w, PageList list
   return launched();
 }
 
+}  // namespace
+
 kvc_status launch_fork(const PoolView& pool, const PageSpace& w, const int32_t* parents, const int32_t* children, uint32_t n,
                        hipStream_t stream) {
-  if ((uint64_t)n * pool.L >> 31) return KVC_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(fork_kernel, dim3(n * pool.L), dim3(256), 0, stream, pool, w, parents, children, make_fastdiv(pool.L));
+  const uint32_t kinds = 2 * pool.L;
+  if ((uint64_t)n * kinds >> 31) return KVC_ERR_UNSUPPORTED;
+  if (one_group(pool, n)) {
+    hipLaunchKernelGGL(plan_fork_kernel, dim3(1), dim3(kOneThreads), (pool.n_rows + 31) / 32 * 4, stream, pool, w, parents, children, n);
+    if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
+    hipLaunchKernelGGL(fork_kernel<true>, dim3(n * kinds), dim3(256), 0, stream, pool, w, parents, children, make_fastdiv(kinds));
+    return launched();
+  }
+  const kvc_status st = launch_survey(pool, w, PageList::kFork, parents, children, n, stream);
+  if (st != KVC_OK) return st;
+  hipLaunchKernelGGL(fork_kernel<false>, dim3(n * kinds), dim3(256), 0, stream, pool, w, parents, children, make_fastdiv(kinds));
   return launched();
 }
 
 kvc_status launch_grow(const PoolView& pool, const PageSpace& w, const int32_t* rows, const int32_t* counts, uint32_t n,
                        hipStream_t stream) {
+  if (one_group(pool, n)) {
+    hipLaunchKernelGGL(grow_one_kernel, dim3(1), dim3(kOneThreads), (pool.n_rows + 31) / 32 * 4, stream, pool, rows, counts, n);
+    return launched();
+  }
+  const kvc_status st = launch_survey(pool, w, PageList::kGrow, rows, counts, n, stream);
+  if (st != KVC_OK) return st;
   hipLaunchKernelGGL(grow_kernel, dim3((n + 3) / 4), dim3(256), 0, stream, pool, w, rows, counts, n);
   return launched();
 }
@@ -541,7 +782,13 @@ kvc_status launch_free(const PoolView& pool, const int32_t* rows, uint32_t n, hi
 kvc_status launch_compact(const PoolView& pool, const PageSpace& w, int32_t* map, int32_t* tables, int32_t* refs, hipStream_t stream) {
   const uint64_t pieces = (pool.page_bytes + kPiece - 1) / kPiece;
   if (2 * pool.L * pieces >> 31) return KVC_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(compact_lists_kernel, dim3(w.segments), dim3(256), 0, stream, pool, w);
+  if (one_group(pool, 0)) {
+    hipLaunchKernelGGL(compact_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, pool, w);
+  } else {
+    const kvc_status st = launch_survey(pool, w, PageList::kNone, nullptr, nullptr, 0, stream);
+    if (st != KVC_OK) return st;
+    hipLaunchKernelGGL(compact_lists_kernel, dim3(w.segments), dim3(256), 0, stream, pool, w);
+  }
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   const uint32_t movers = 2048;
   const uint64_t books = ((uint64_t)pool.n_rows * pool.table_len + pool.num_blocks + 1023) / 1024;

@@ -21,6 +21,12 @@ struct PoolView {
 
 // Books are surveyed in segments of this many pages: for each of them the number of free ones, and a bit for each page.
 constexpr uint32_t kSegment = 4096, kSegmentWords = kSegment / 32;
+// Pools of up to this many pages are surveyed by one workgroup.
+constexpr uint32_t kOnePages = 16384;
+
+struct ForkJob {
+  uint32_t from, to, tokens, len;  // pages, tokens that are copied, tokens of the parent
+};
 
 // The workspace of fork, grow and compact.
 struct PageSpace {
@@ -28,6 +34,7 @@ struct PageSpace {
   uint32_t* counts;  // [segments] free pages
   uint32_t* bits;    // [segments][kSegmentWords] 1: free
   uint32_t* first;   // [n_rows + 1] pages that the entries of the list before this one take
+  ForkJob* jobs;     // [n_rows] fork of a small pool
   int32_t *places, *sources, *moved, *refs;  // compact, [num_blocks] each
   uint32_t segments;
 };
@@ -35,8 +42,6 @@ enum { kPlanFaults = 0, kPlanNeed = 1, kPlanUsed = 2, kPlanMoves = 3, kPlanWords
 
 enum class PageList { kNone, kFork, kGrow };
 
-kvc_status launch_survey(const PoolView& pool, const PageSpace& w, PageList list, const int32_t* a, const int32_t* b, uint32_t n,
-                         hipStream_t stream);
 kvc_status launch_fork(const PoolView& pool, const PageSpace& w, const int32_t* parents, const int32_t* children, uint32_t n,
                        hipStream_t stream);
 kvc_status launch_grow(const PoolView& pool, const PageSpace& w, const int32_t* rows, const int32_t* counts, uint32_t n,

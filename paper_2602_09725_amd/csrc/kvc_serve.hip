@@ -56,6 +56,7 @@ size_t lay_out(const PoolView& v, uint8_t* base, PageSpace* w) {
   w->counts = reinterpret_cast<uint32_t*>(take((size_t)w->segments * 4));
   w->bits = reinterpret_cast<uint32_t*>(take((size_t)w->segments * kSegmentWords * 4));
   w->first = reinterpret_cast<uint32_t*>(take(((size_t)v.n_rows + 1) * 4));
+  w->jobs = reinterpret_cast<ForkJob*>(take((size_t)v.n_rows * sizeof(ForkJob)));
   for (int32_t** list : {&w->places, &w->sources, &w->moved, &w->refs}) *list = reinterpret_cast<int32_t*>(take((size_t)v.num_blocks * 4));
   return at;
 }
@@ -159,8 +160,6 @@ kvc_status kvc_pages_fork(const kvc_pool* pool, const int32_t* d_parents, const 
   if (n == 0) return KVC_OK;
   if (!d_parents || !d_children || !aligned(d_parents, 4) || !aligned(d_children, 4)) return KVC_ERR_INVALID_ARG;
   if ((st = space_of(v, workspace, workspace_bytes, &w)) != KVC_OK) return st;
-  if ((uint64_t)n * v.L >> 31) return KVC_ERR_UNSUPPORTED;
-  if ((st = launch_survey(v, w, PageList::kFork, d_parents, d_children, (uint32_t)n, as_stream(stream))) != KVC_OK) return st;
   return launch_fork(v, w, d_parents, d_children, (uint32_t)n, as_stream(stream));
 }
 
@@ -174,7 +173,6 @@ kvc_status kvc_pages_grow(const kvc_pool* pool, const int32_t* d_rows, const int
   if (n == 0) return KVC_OK;
   if (!d_rows || !aligned(d_rows, 4) || !aligned(d_counts, 4)) return KVC_ERR_INVALID_ARG;
   if ((st = space_of(v, workspace, workspace_bytes, &w)) != KVC_OK) return st;
-  if ((st = launch_survey(v, w, PageList::kGrow, d_rows, d_counts, (uint32_t)n, as_stream(stream))) != KVC_OK) return st;
   return launch_grow(v, w, d_rows, d_counts, (uint32_t)n, as_stream(stream));
 }
 
@@ -197,7 +195,6 @@ kvc_status kvc_pages_compact(const kvc_pool* pool, int32_t* d_map, int32_t* d_ta
   if (!d_map || !d_tables_out || !d_refs_out) return KVC_ERR_INVALID_ARG;
   if (!aligned(d_map, 4) || !aligned(d_tables_out, 4) || !aligned(d_refs_out, 4)) return KVC_ERR_INVALID_ARG;
   if ((st = space_of(v, workspace, workspace_bytes, &w)) != KVC_OK) return st;
-  if ((st = launch_survey(v, w, PageList::kNone, nullptr, nullptr, 0, as_stream(stream))) != KVC_OK) return st;
   return launch_compact(v, w, d_map, d_tables_out, d_refs_out, as_stream(stream));
 }
 

@@ -280,6 +280,87 @@ def test_compact_goes_on_where_entries_are_wrong(kvc_lib):
     d.check_data(before)
 
 
+# ---- pools on both sides of what one workgroup looks after: 16384 pages, lists of 1024 entries
+
+
+def half_taken(books, seed):
+    rng = random.Random(seed)
+    for page in range(books.blocks):
+        if books.refs[page] == 0 and rng.random() < 0.6:
+            books.refs[page] = 1
+    return books
+
+
+@pytest.mark.parametrize("entries", [1, 1024, 1025])
+@pytest.mark.parametrize("blocks", [16383, 16384, 16385, 50000])
+def test_lists_and_pools_of_many_pages(kvc_lib, blocks, entries):
+    lens = [3 * (i % 5) + i % 3 for i in range(entries)]
+    books = half_taken(filled(2 * entries + 1, 24, 3, blocks, lens, seed=entries), blocks)
+    d = DevicePool(books, 1, 1, 8)
+    before = d.copy()
+    parents, children = list(range(entries)), list(range(2 * entries - 1, entries - 1, -1))
+    a, b = i32(parents), i32(children)
+    kvc.kvc_pages_fork(d.pool, a.data_ptr(), b.data_ptr(), entries, *d.room())
+    books.fork(parents, children)
+    d.check(before)
+    counts = [(5 * i + 1) % 12 for i in range(entries)]
+    c = i32(counts)
+    kvc.kvc_pages_grow(d.pool, b.data_ptr(), c.data_ptr(), entries, *d.room())
+    books.grow(children, counts)
+    d.check(before)
+    kvc.kvc_pages_free(d.pool, a.data_ptr(), entries, hz.stream_handle())
+    books.free(parents)
+    d.check(before)
+    assert books.err == 0
+
+
+@pytest.mark.parametrize("blocks", [40, 20000])
+@pytest.mark.parametrize("what", ["twice", "no room", "exactly enough", "bad page", "count below 0"])
+def test_faults_in_pools_of_any_size(kvc_lib, blocks, what):
+    """A list at fault changes nothing, in small pools as in large ones; the last free page can be taken."""
+    books = filled(8, 5, 4, blocks, [9, 6, 4, 0, 0, 0], seed=blocks)
+    free = [page for page in range(blocks) if books.refs[page] == 0]
+    if what in ("no room", "exactly enough"):  # two forks need a page each
+        for page in free[:-2] if what == "exactly enough" else free[:-1]:
+            books.refs[page] = 1
+    if what == "bad page":
+        books.tables[0][2] = blocks
+    if what == "count below 0":
+        books.refs[free[3]] = -1
+    children = [3, 3, 5] if what == "twice" else [3, 4, 5]
+    d = DevicePool(books, 2, 1, 16)
+    before = d.copy()
+    a, b = i32([0, 1, 2]), i32(children)
+    kvc.kvc_pages_fork(d.pool, a.data_ptr(), b.data_ptr(), 3, *d.room())
+    books.fork([0, 1, 2], children)
+    want = {"twice": model.FAULT_LIST, "no room": model.FAULT_NO_ROOM, "exactly enough": 0, "bad page": model.FAULT_PAGE,
+            "count below 0": model.FAULT_LIST}[what]
+    assert books.err == want
+    d.check(before)
+    if what == "exactly enough":  # and now there is none
+        c, counts = i32([2, 0]), i32([1, 1])
+        kvc.kvc_pages_grow(d.pool, c.data_ptr(), counts.data_ptr(), 2, *d.room())
+        books.grow([2, 0], [1, 1])
+        assert books.err == model.FAULT_NO_ROOM
+        d.check(before)
+
+
+@pytest.mark.parametrize("blocks,used", [(16384, 1), (16384, 16384), (16384, 5000), (16385, 8191), (16385, 16385), (40000, 0), (33000, 20000)])
+def test_compact_of_many_pages(kvc_lib, blocks, used):
+    lens = [2 * (used // 4)] * 4 + [2 * (used % 4)]
+    books = filled(6, max(1, used), 2, blocks, lens, seed=used)
+    d = DevicePool(books, 1, 1, 8)
+    before = d.copy()
+    where, tables, refs = torch.empty_like(d.refs), torch.empty_like(d.tables), torch.empty_like(d.refs)
+    kvc.kvc_pages_compact(d.pool, where.data_ptr(), tables.data_ptr(), refs.data_ptr(), *d.room())
+    want = books.compact()
+    torch.cuda.synchronize()
+    assert (where.tolist(), refs.tolist()) == (want[0], want[2])
+    assert torch.equal(tables, i32(want[1]))
+    assert int(d.err.item()) == books.err == 0
+    d.check_data(before)
+
+
 # ---- append
 
 BATCHES = [  # tokens of the rows after the call, new ones of each (None: one each)
