@@ -862,24 +862,37 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   __shared__ f32x4 part[256];
   __shared__ float tops[8];
   constexpr uint32_t QD = DP / 4, EACH = 256 / LINES, SIDE = EACH / QD;  // lanes and groups of lanes of a row
+  constexpr uint32_t AHEAD = 4;
   const uint32_t self = threadIdx.x % EACH, mine = threadIdx.x / EACH;
   const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, line = (uint64_t)blockIdx.x * LINES + mine;
   const bool there = line < lines;
   uint32_t token, head;
   fd_divmod(p.dheads, there ? (uint32_t)line : 0u, token, head);
+  const uint32_t at = self % QD, group = self / QD;
+  auto slot = [&](uint32_t i) { return (uint64_t)i * lines + (there ? line : 0); };
+  // What the row's pieces hold is asked for before it is known which of them hold something: all are memory of the call's.
+  f32x4 ahead[AHEAD];
+#pragma unroll
+  for (uint32_t k = 0; k < AHEAD; ++k) {
+    const uint32_t i = group + k * SIDE;
+    if (i < p.pieces && at * 4 < p.D) ahead[k] = *(const KVC_GLOBAL f32x4*)(p.sums + slot(i) * p.D + at * 4);
+  }
+  f32x2 first = {kNone, 0.0f};
+  if (self < p.pieces) first = *(const KVC_GLOBAL f32x2*)(p.tops + slot(self) * 2);
   const Request q = request_at(p, request_of(p.batch, token));
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
   uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;
   uint32_t n = p.part[1].splits && limit > p.prefix && token - q.first < p.batch.most_new ? fd_div(p.part[1].dtokens, limit - p.prefix + p.part[1].tokens - 1) : 0;
   if (!there) a = n = 0;
-  n += a;
-  auto slot = [&](uint32_t i) { return (uint64_t)(i < a ? i : p.part[0].splits + i - a) * lines + line; };
+  const uint32_t split = p.part[0].splits, end = split + n;
+  auto holds = [&](uint32_t i) { return i < a || (i >= split && i < end); };
   // maxima, weights and the sum of weights: a row's threads share its pieces
   float* const w = weight_of + mine * p.pieces;
   float top = kNone, total = 0.0f;
-  for (uint32_t i = self; i < n; i += EACH) {
-    const f32x2 t = *(const KVC_GLOBAL f32x2*)(p.tops + slot(i) * 2);
+  for (uint32_t i = self; i < p.pieces; i += EACH) {
+    f32x2 t = i == self ? first : *(const KVC_GLOBAL f32x2*)(p.tops + slot(i) * 2);
+    if (!holds(i)) t.x = kNone;
     w[i] = t.x;
     const float now = fmaxf(top, t.x), keep = weight(top, now);
     total = total * keep + (t.x == kNone ? 0.0f : t.y * weight(t.x, now));
@@ -905,17 +918,21 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
 #pragma unroll
     for (uint32_t k = 0; k < WAVES; ++k) total += m[k] == kNone ? 0.0f : l[k] * weight(m[k], top);
   }
-  for (uint32_t i = self; i < n; i += EACH) w[i] = weight(w[i], top);
+  for (uint32_t i = self; i < p.pieces; i += EACH) w[i] = weight(w[i], top);
   __syncthreads();
   // sums: group g of a row takes pieces g, g + SIDE, ..
-  const uint32_t at = self % QD, group = self / QD;
   f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t k = 0; k < AHEAD; ++k) {
+    const float x = group + k * SIDE < p.pieces ? w[group + k * SIDE] : 0.0f;
+    if (x != 0.0f) o += ahead[k] * x;  // (the sums of a piece that saw nothing mean nothing)
+  }
   if (at * 4 < p.D) {
 #pragma unroll 4
-    for (uint32_t i = group; i < n; i += SIDE) {
+    for (uint32_t i = group + AHEAD * SIDE; i < p.pieces; i += SIDE) {
       const float x = w[i];
       const f32x4 v = *(const KVC_GLOBAL f32x4*)(p.sums + slot(i) * p.D + at * 4);
-      if (x != 0.0f) o += v * x;  // (a piece that saw nothing has a maximum of its own, -inf, and sums that mean nothing)
+      if (x != 0.0f) o += v * x;
     }
   }
   if constexpr (SIDE > 1) {
@@ -972,9 +989,11 @@ kvc_status plan_attend(AttendParams& p) {
     if (tokens == 0) continue;
     if (whole >> 31) return KVC_ERR_UNSUPPORTED;
     // One workgroup a CU where a piece is short (of 32K tokens and 32 rows 32 or 64 pieces of 8 heads 51 or 59 us), two of them where it
-    // is long (64 rows, twice the rows of queries a workgroup has: of 32K tokens 16 or 32 pieces 76 or 74 us, of 64K 130 or 118); where more than
-    // two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms instead of 1.75).
-    uint64_t splits = whole <= chip && tokens * whole >= 1024 * chip ? chip / whole : whole <= 256 ? 256 / whole : 1;
+    // is long (64 rows of queries, 256 of a head: of 64K tokens 16 or 32 pieces 125 or 120 us; of 32K, where the rows' own 500 tokens each take the
+    // second workgroup's place, 66 or 76); where more than two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms
+    // instead of 1.75).
+    const uint64_t lengthy = i == 0 && p.most_tokens > p.prefix ? 2048 : 1024;
+    uint64_t splits = whole <= chip && tokens * whole >= lengthy * chip ? chip / whole : whole <= 256 ? 256 / whole : 1;
     if (whole > chip && tokens >= 4096 && 20 * ((whole + chip - 1) / chip) * chip > 23 * whole) splits = 2;
     uint64_t each = (tokens + splits - 1) / splits;
     const uint64_t least = 128;
