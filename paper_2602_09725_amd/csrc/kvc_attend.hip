@@ -840,7 +840,8 @@ __device__ __forceinline__ bool unit_of(const AttendParams& p, bool& shared, uin
   return unit < units;
 }
 
-template <int DT, int DP, bool BIG>
+// ONES: neither part has four waves side by side.
+template <int DT, int DP, bool BIG, bool ONES>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
   __shared__ u32x4 a[quarter<DP>()], b[quarter<DP>()], c[quarter<DP>()], d[quarter<DP>()];
   __shared__ Tops tops;
@@ -849,8 +850,8 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendPar
   uint32_t unit;
   if (!unit_of(p, shared, unit)) return;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  if (part.waves == 1) attend_unit<DT, DP, 1, BIG>(p, part, shared, unit, lds, tops);
-  else attend_unit<DT, DP, 4, BIG>(p, part, shared, unit, lds, tops);
+  if (ONES || part.waves == 1) attend_unit<DT, DP, 1, BIG>(p, part, shared, unit, lds, tops);
+  else if constexpr (!ONES) attend_unit<DT, DP, 4, BIG>(p, part, shared, unit, lds, tops);
 }
 
 // Joins the pieces of rows: a workgroup takes LINES rows (a token and a head), and 256 / LINES threads a row.  First the weights of all of
@@ -956,16 +957,22 @@ template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   const uint32_t groups = (p.part[0].units + 7) / 8 * 8 + (p.part[1].units + 7) / 8 * 8;
   const bool big = (uint64_t)p.pool.num_blocks * p.pool.page_bytes > 0xffff0000u;  // (offsets of what is not there lie above)
-  if (groups && big) hipLaunchKernelGGL((attend_kernel<DT, DP, true>), dim3(groups), dim3(256), 0, stream, p);
-  if (groups && !big) hipLaunchKernelGGL((attend_kernel<DT, DP, false>), dim3(groups), dim3(256), 0, stream, p);
+  // Few rows have a kernel of the one body alone, with fewer registers (4 rows over 1000 tokens 14.6 -> 13.9 us, 30 rows of 32 heads over 3000 tokens 40.8 ->
+  // 39.2); caches beyond 32 bits go without.
+  const bool ones = p.part[0].waves <= 1 && p.part[1].waves <= 1;
+  if (groups && big) hipLaunchKernelGGL((attend_kernel<DT, DP, true, false>), dim3(groups), dim3(256), 0, stream, p);
+  if (groups && !big && ones) hipLaunchKernelGGL((attend_kernel<DT, DP, false, true>), dim3(groups), dim3(256), 0, stream, p);
+  if (groups && !big && !ones) hipLaunchKernelGGL((attend_kernel<DT, DP, false, false>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   if (p.pieces != 1) {  // (no piece at all: every row is empty)
-    // Few rows of many pieces take a workgroup each, many rows share one.
+    // Few rows of many pieces take a workgroup each; many rows share one, a row having as many threads as it has vectors of four sums (up to 128
+    // elements, so that a workgroup's life, which is that of its loads one after the other, is spent on eight rows).
+    constexpr uint32_t kLines = DP > 128 ? 4 : 8;
     const uint32_t lines = p.batch.n_new * p.H * p.G;
     if (lines <= 2048)
       hipLaunchKernelGGL((join_kernel<DT, DP, 1>), dim3(lines), dim3(256), p.pieces * 4, stream, p);
     else
-      hipLaunchKernelGGL((join_kernel<DT, DP, 4>), dim3((lines + 3) / 4), dim3(256), p.pieces * 16, stream, p);
+      hipLaunchKernelGGL((join_kernel<DT, DP, kLines>), dim3((lines + kLines - 1) / kLines), dim3(256), p.pieces * kLines * 4, stream, p);
   }
   return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_RUNTIME;
 }
