@@ -687,44 +687,56 @@ __global__ void __launch_bounds__(256) append_kernel(AppendParams p) {
       c += (uint32_t)__popcll(__ballot(r < p.batch.n_requests && (uint32_t)p.batch.starts[r] <= t));
     r0 = c ? c - 1 : 0;
   }
+  // Each of a vector's questions (request, row, length, page) waits for the one before: those of a thread's vectors are asked side by side, with
+  // indexes that are in range whatever the answers were.
+  const uint64_t most = begin + 256 * U < all ? begin + 256 * U - 1 : all - 1;
+  bool several = false;
+  if (p.batch.starts && r0 + 1 < p.batch.n_requests) several = (uint32_t)p.batch.starts[r0 + 1] <= (uint32_t)(most / per_token);
   u32x4 value[U];
-  uint8_t* to[U];
+  uint32_t t[U], kind[U], atom[U], r[U], back[U], row[U], len[U], page[U], slot[U];
+  bool live[U];
   uint32_t bad = 0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint64_t at = begin + (uint32_t)u * 256 + threadIdx.x;
-    to[u] = nullptr;
-    if (at >= all) continue;
-    uint32_t t, atom, twice;
-    if (all >> 31) twice = (uint32_t)(at / p.atoms), atom = (uint32_t)(at - (uint64_t)twice * p.atoms);
-    else fd_divmod(p.datoms, (uint32_t)at, twice, atom);
-    t = twice / 2;
-    const uint32_t kind = twice % 2;
-    uint32_t r = t, back = 1;  // the token is its request's last but back - 1
-    if (p.batch.starts) {
-      r = request_from(p.batch, t, r0);
-      const uint32_t end = (uint32_t)p.batch.starts[r + 1];
-      back = end - t;
-    }
-    const uint32_t row = p.batch.rows ? (uint32_t)p.batch.rows[r] : r;
-    const uint32_t len = row < p.pool.n_rows ? (uint32_t)p.pool.lens[row] : ~0u;
-    if (len > p.pool.capacity || back - 1 >= len) {
-      bad |= KVC_FAULT_LIST;
-      continue;
-    }
-    uint32_t block, slot;
-    fd_divmod(p.pool.dbs, len - back, block, slot);
-    const uint32_t page = (uint32_t)p.pool.tables[(uint64_t)row * p.pool.table_len + block];
-    if (page >= p.pool.num_blocks) {
-      bad |= KVC_FAULT_PAGE;
-      continue;
-    }
-    value[u] = *(const KVC_GLOBAL u32x4*)((kind ? p.v : p.k) + (int64_t)t * p.token_stride + atom * 8);
-    to[u] = page_at(p.pool, p.layer, kind, page) + (uint64_t)slot * p.pool.token_bytes + atom * 16;
+    const uint64_t here = begin + (uint32_t)u * 256 + threadIdx.x, at = here < all ? here : all - 1;
+    live[u] = here < all;
+    uint32_t twice;
+    if (all >> 31) twice = (uint32_t)(at / p.atoms), atom[u] = (uint32_t)(at - (uint64_t)twice * p.atoms);
+    else fd_divmod(p.datoms, (uint32_t)at, twice, atom[u]);
+    t[u] = twice / 2;
+    kind[u] = twice % 2;
+    value[u] = *(const KVC_GLOBAL u32x4*)((kind[u] ? p.v : p.k) + (int64_t)t[u] * p.token_stride + atom[u] * 8);
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (to[u]) *(KVC_GLOBAL u32x4*)to[u] = value[u];
+  for (int u = 0; u < U; ++u) {  // the token is its request's last but back - 1
+    r[u] = p.batch.starts ? r0 : t[u];
+    if (several) r[u] = request_from(p.batch, t[u], u ? r[u - 1] : r0);
+    back[u] = p.batch.starts ? (uint32_t)p.batch.starts[r[u] + 1] - t[u] : 1u;
+    row[u] = p.batch.rows ? (uint32_t)p.batch.rows[r[u]] : r[u];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool known = row[u] < p.pool.n_rows;
+    len[u] = (uint32_t)p.pool.lens[known ? row[u] : 0];
+    if (live[u] && (!known || len[u] > p.pool.capacity || back[u] - 1 >= len[u])) {
+      bad |= KVC_FAULT_LIST;
+      live[u] = false;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    uint32_t block;
+    fd_divmod(p.pool.dbs, live[u] ? len[u] - back[u] : 0u, block, slot[u]);
+    page[u] = (uint32_t)p.pool.tables[(uint64_t)(live[u] ? row[u] : 0u) * p.pool.table_len + block];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!live[u]) continue;
+    if (page[u] < p.pool.num_blocks)
+      *(KVC_GLOBAL u32x4*)(page_at(p.pool, p.layer, kind[u], page[u]) + (uint64_t)slot[u] * p.pool.token_bytes + atom[u] * 16) = value[u];
+    else
+      bad |= KVC_FAULT_PAGE;
+  }
   fault(p.pool, bad);
 }
 
