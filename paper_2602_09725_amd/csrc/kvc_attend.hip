@@ -4,7 +4,8 @@
 //   out = sum_j w_j v_j / sum_j w_j,  w_j = exp2(scale_log2 * (s_j - m)),  m any number near the largest s_j,
 // and results over disjoint sets of tokens join by their m and sums.  So the work is cut into pieces: the shared prefix is
 // one sequence for the rows of all requests (read once for 32 or 128 of them), each row's own tokens another for the rows
-// of its request, and both are cut along the tokens until the chip is full.  A second, small launch joins the pieces.
+// of its request, and both are cut along the tokens until the chip is full.  A second, small launch joins the pieces.  Where many new tokens
+// meet a short prefix the pieces' sums would be most of the work: then each row's tokens are one sequence, the prefix's and its own.
 //
 // A wave holds 32 rows.  It computes S^T = K Q^T and O^T += V^T W^T with 32x32x16 matrix instructions, so that a lane has
 // one row (lane % 32) in all of its registers: the softmax needs one exchange between the halves of a wave for a
@@ -174,7 +175,21 @@ struct Unit {
   uint32_t t0, t1, bound;  // tokens of the unit that are there; none that the host knows of lies at or beyond `bound`
   uint32_t limit, least;   // those below `limit` are seen by the lane's row, below `least` by all of them
   bool bad_pages;          // a page outside the pool has been met: an error of the caller's, and only then looked for token by token
+  bool page_fault;
+  // Four waves side by side may have the prefix before a row's own tokens: those below `front` are read through this table, and are there below `known`.
+  const int32_t* front_table;
+  uint32_t front, known;
 };
+
+// Page of a position, and whether it is one of the prefix's that are not there.
+template <int TT>
+__device__ __forceinline__ uint32_t page_of(const AttendParams& p, const Unit& u, uint32_t pos) {
+  const int32_t* table = u.table;
+  if (TT == 64 && pos < u.front) table = u.front_table;
+  return (uint32_t)table[fd_div(p.pool.dbs, pos)];
+}
+template <int TT>
+__device__ __forceinline__ bool in_hole(const Unit& u, uint32_t pos) { return TT == 64 && pos < u.front && pos >= u.known; }
 
 // Running state of a lane's row: a number near the largest product so far, sum of this half's weights, sums of values.
 template <int DP>
@@ -205,7 +220,7 @@ __device__ __forceinline__ void wait_reads() {
 template <int TT>
 __device__ __forceinline__ uint32_t page_of_lane(const AttendParams& p, const Unit& u, uint32_t at) {
   const uint32_t pos = at + (threadIdx.x & (uint32_t)(TT - 1));
-  return (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.bound - 1))];
+  return page_of<TT>(p, u, min(pos, u.bound - 1));
 }
 
 // What has been loaded is not looked at before this point, so that no wait is put in front of it.
@@ -228,8 +243,11 @@ __device__ __forceinline__ Sources<DP, R, BIG> sources_of(const AttendParams& p,
   const uint32_t self = R == 1 ? threadIdx.x & 63u : threadIdx.x, first = self / S::CH, lane = threadIdx.x & 63u;
   const uint32_t pos = at + (lane & (uint32_t)(S::TT - 1));
   const uint32_t slot = page * p.pool.block_size + (pos - fd_div(p.pool.dbs, pos) * p.pool.block_size);
-  const bool bad = page >= p.pool.num_blocks, gone = pos >= u.t1;
-  u.bad_pages |= __any((int)bad & (int)!gone);
+  const bool hole = in_hole<S::TT>(u, pos), bad = (int)(page >= p.pool.num_blocks) | (int)hole, gone = pos >= u.t1;
+  if (__any((int)bad & (int)!gone)) {
+    u.bad_pages = true;
+    u.page_fault |= __any((int)bad & (int)!gone & (int)!hole);
+  }
   uint32_t offset, base = 0;
   if constexpr (BIG) {
     const uint64_t all = (uint64_t)slot * p.pool.token_bytes;
@@ -310,7 +328,7 @@ __device__ __forceinline__ void products(const u32x4 KVC_LDS* k, const u32x4 (&q
 }
 
 // -inf in the place of products that the lane's row does not see, in a tile at position `at`.
-template <int NS>
+template <int NS, int TT>
 __device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint32_t at, f32x16 (&s)[NS]) {
   const uint32_t half = (threadIdx.x >> 5) & 1u;
 #pragma unroll
@@ -319,7 +337,7 @@ __device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint3
     for (int i = 0; i < 16; ++i) {
       const uint32_t pos = at + n * 32 + (i / 4) * 8 + half * 4 + i % 4;
       bool seen = pos < u.limit && pos < u.t1;
-      if (u.bad_pages) seen = seen && (uint32_t)u.table[fd_div(p.pool.dbs, min(pos, u.t1 - 1))] < p.pool.num_blocks;
+      if (u.bad_pages) seen = seen && !in_hole<TT>(u, pos) && page_of<TT>(p, u, min(pos, u.t1 - 1)) < p.pool.num_blocks;
       if (!seen) s[n][i] = kNone;
     }
 }
@@ -528,7 +546,7 @@ template <int DT, int DP>
 __device__ __forceinline__ void take_masked(const AttendParams& p, const Unit& u, uint32_t at, State<DP>& x, const f32x16& products, const u32x4 KVC_LDS* v) {
   f32x16 s[1] = {products};
   u32x4 w[1][2];
-  mask<1>(p, u, at, s);
+  mask<1, 64>(p, u, at, s);
   weights<DT, DP, 1>(p, x, s, w);
   if (hides_tokens<32>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
   else add_values<DT, DP, 1>(x, v, w);
@@ -567,7 +585,7 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   load_tile(u, keys, from, k);
   asm volatile("" ::: "memory");
   page = page_of_lane<S::TT>(p, u, at + 2 * next);  // (between this line and the wait below: it is one of the loads counted there)
-  if constexpr (!PLAIN) mask<1>(p, u, at, s);
+  if constexpr (!PLAIN) mask<1, S::TT>(p, u, at, s);
   weights<DT, DP, 1>(p, x, s, w);
   wait_loads<N + 1>();  // V is there; the next K and its successor's page follow
   if (!PLAIN && hides_tokens<S::TT>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
@@ -694,8 +712,16 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   Unit u;
   Request q{};
   if (!shared) q = request_at(p, at_work.request);
+  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
+  if (!shared && at_work.block * (R * 32) >= wave_uniform(new_tokens) * p.G) {  // (a request with fewer new tokens than others)
+    if (threadIdx.x == 0) fault(p, q.faults);
+    return;
+  }
   u.bound = shared ? p.prefix : p.most_tokens;
-  u.t0 = (shared ? 0 : p.prefix) + at_work.split * part.tokens;
+  u.t0 = (shared ? 0 : p.own_from) + at_work.split * part.tokens;
+  u.front = shared || p.own_from ? 0 : p.prefix;
+  u.front_table = p.pool.tables + (uint64_t)p.prefix_row * p.pool.table_len;
+  u.page_fault = false;
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
   constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a wave to its next
   const uint32_t start = u.t0 + (R == 1 ? wave_uniform(wave) * TT : 0);
@@ -704,7 +730,6 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   for (int i = 0; i < (R == 1 ? 2 : 3); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
 
   const uint32_t base_row = (at_work.block * R + (R == 1 ? 0 : wave)) * 32;
-  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
   uint32_t token;
   u32x4 query[KK];
   const bool there = load_query<DP>(p, q, shared, new_tokens, base_row + col, at_work.head, token, query);
@@ -713,7 +738,8 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   u.span = (uint32_t)((uint64_t)p.pool.num_blocks * p.pool.page_bytes - (uint64_t)at_work.head * p.D * 2);
   if (shared) q = request_at(p, request_of(p.batch, token));
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
-  if (shared ? u.t1 < p.prefix && threadIdx.x == 0 : false) fault(p, KVC_FAULT_LIST);
+  u.known = u.front ? prefix_there(p) : 0;
+  if ((shared ? u.t1 < p.prefix : u.known < u.front) && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
   u.t1 = min(u.t1, u.t0 + part.tokens);
   u.bad_pages = false;
   u.limit = u.least = 0;
@@ -795,7 +821,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     }
   }
   wait_loads<0>();  // (of tiles that nobody reads: they may not land on the sums, nor after the workgroup's end)
-  if (u.bad_pages && lane == 0) fault(p, KVC_FAULT_PAGE);
+  if (u.page_fault && lane == 0) fault(p, KVC_FAULT_PAGE);
   if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   __syncthreads();
@@ -884,7 +910,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
   uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;
-  uint32_t n = p.part[1].splits && limit > p.prefix && token - q.first < p.batch.most_new ? fd_div(p.part[1].dtokens, limit - p.prefix + p.part[1].tokens - 1) : 0;
+  uint32_t n = p.part[1].splits && limit > p.own_from && token - q.first < p.batch.most_new ? fd_div(p.part[1].dtokens, limit - p.own_from + p.part[1].tokens - 1) : 0;
   if (!there) a = n = 0;
   const uint32_t split = p.part[0].splits, end = split + n;
   auto holds = [&](uint32_t i) { return i < a || (i >= split && i < end); };
@@ -979,15 +1005,25 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 
 }  // namespace
 
+// Whether the prefix is read anew for each request.  It costs the products of about 64 rows of a block that a request does not fill, over the
+// prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s; and there have to be blocks enough
+// for the chip without cutting along the tokens.
+bool one_sequence(const AttendParams& p) {
+  const uint64_t rows = (uint64_t)p.batch.n_new * p.G;
+  if (p.prefix == 0 || p.most_tokens == p.prefix || (uint64_t)p.batch.most_new * p.G <= 32) return false;
+  return rows * p.H >= 128 * 256 && (uint64_t)p.batch.n_requests * p.prefix < 14 * rows;
+}
+
 kvc_status plan_attend(AttendParams& p) {
   p.pieces = 0;
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = 8.0f / p.scale_log2 < 1e30f ? 8.0f / p.scale_log2 : 1e30f;
   const uint64_t chip = p.D <= 128 ? 512 : 256;  // workgroups that run at a time
+  p.own_from = one_sequence(p) ? 0 : p.prefix;
   for (int i = 0; i < 2; ++i) {
     AttendPart& a = p.part[i];
     a = AttendPart{};
-    const uint64_t tokens = i == 0 ? p.prefix : p.most_tokens - p.prefix;
+    const uint64_t tokens = i == 0 ? p.own_from : p.most_tokens - p.own_from;
     const uint64_t rows = (uint64_t)(i == 0 ? p.batch.n_new : p.batch.most_new) * p.G;
     a.waves = rows <= 32 ? 1 : 4;
     const uint64_t each_block = a.waves == 1 ? 32 : 128, blocks = (rows + each_block - 1) / each_block;

@@ -85,6 +85,7 @@ struct AttendParams {
   int64_t q_token, q_head, o_token, o_head;
   uint32_t layer, H, G, D, dtype;
   uint32_t prefix, prefix_row, most_tokens;
+  uint32_t own_from;    // first token of the rows' own part: the prefix's end, or 0 where each row's tokens are one sequence
   FastDiv dG, dheads;   // dheads: query heads
   AttendPart part[2];   // prefix, own
   float scale, scale_log2;

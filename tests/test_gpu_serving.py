@@ -721,3 +721,56 @@ def test_offsets_beyond_32_bits(kvc_lib):
     kvc.kvc_pages_copy(a.device.pool, src.data_ptr(), dst.data_ptr(), 1, hz.stream_handle())
     torch.cuda.synchronize()
     assert torch.equal(a.caches[0][:, 0], a.caches[0][:, a.books.tables[0][0]])
+
+
+# ---- many new tokens over a short prefix: each row's tokens are one sequence, and no pieces are joined
+
+ONE_SEQUENCE = [
+    (8, 8, 128, 16, 100, [320, 260, 140, 290], [200, 150, 0, 170]),
+    (4, 16, 64, 5, 33, [300, 280, 33, 40], [260, 240, 3, 20]),
+    (8, 8, 128, 16, 128, [60, 300, 290, 0], [60, 250, 210, 5]),  # rows that end inside the prefix
+    (8, 8, 256, 32, 70, [300, 330], [250, 270]),
+    (8, 8, 72, 1, 64, [200, 450], [130, 390]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", ONE_SEQUENCE, ids=[f"c{i}" for i in range(len(ONE_SEQUENCE))])
+def test_attention_of_one_sequence(kvc_lib, case, dtype):
+    hz.say(f"[case] one sequence {case} {dtype}")
+    a = Attend(*case[:3], dtype, *case[3:], seed=len(case[5]))
+    assert a.space.numel() == 0
+    a.call()
+    a.check()
+
+
+def test_faults_of_one_sequence(kvc_lib):
+    """Pages outside the pool are not seen, below the prefix those of the prefix's row; nor is what that row lacks."""
+    a = Attend(8, 8, 64, "f16", 16, 100, [320, 290], [270, 250], seed=3)
+    assert a.space.numel() == 0
+    a.books.tables[0][2] = a.books.blocks           # positions 32 .. 47 of the prefix
+    a.books.tables[a.rows[0]][9] = -1               # 144 .. 159 of a row
+    a.books.tables[a.rows[1]][3] = 10 ** 6          # below the prefix: read through row 0
+    a.device.tables.copy_(i32(a.books.tables))
+    a.call()
+    a.check(err=model.FAULT_PAGE, missing=[(None, p) for p in range(32, 48)] + [(a.rows[0], p) for p in range(144, 160)])
+    b = Attend(8, 8, 128, "bf16", 16, 100, [320, 290], [270, 250], seed=4)
+    b.device.lens[0] = 71
+    b.call()
+    b.check(err=model.FAULT_LIST, missing=[(None, p) for p in range(71, 100)])
+
+
+def test_wild_values_of_one_sequence(kvc_lib):
+    """What a query does not see does not reach it, be it infinite."""
+    a, clean = (Attend(8, 8, 128, "f16", 16, 90, [300, 310], [260, 270], seed=6) for _ in range(2))
+    page = a.books.tables[a.rows[0]][280 // 16]
+    a.caches[0][1, page, 280 % 16, :, 5] = math.inf
+    a.call()
+    clean.call()
+    clean.check()
+    torch.cuda.synchronize()
+    first = 280 - 40  # the token at position 280 is the request's 241st
+    assert torch.equal(a.out[:first], clean.out[:first]) and torch.equal(a.out[260:], clean.out[260:])
+    assert bool((a.out[first:260, :, 5] == math.inf).all())
+    rest = [d for d in range(128) if d != 5]
+    assert torch.equal(a.out[first:260][:, :, rest], clean.out[first:260][:, :, rest])
