@@ -126,6 +126,12 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (w & e) == e || ((w >> 16) & e) == e;
 }
 
+// Bits 15 and 31: which of the two values of a word are not finite.
+template <int DT>
+__device__ __forceinline__ uint32_t wild_bits(uint32_t w) {
+  return DT == KVC_F16 ? (w & 0x7c007c00u) + 0x04000400u : (w & 0x7f807f80u) + 0x00800080u;
+}
+
 // The two values of a word, 0 in the place of those that are not finite.
 template <int DT>
 __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
@@ -327,19 +333,22 @@ __device__ __forceinline__ void products(const u32x4 KVC_LDS* k, const u32x4 (&q
   }
 }
 
-// -inf in the place of products that the lane's row does not see, in a tile at position `at`.
-template <int NS, int TT>
-__device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint32_t at, f32x16 (&s)[NS]) {
-  const uint32_t half = (threadIdx.x >> 5) & 1u;
+// -inf in the place of products that the lane's row does not see, in 32 tokens at position `at`.  TT: of a tile of the body.
+template <int TT>
+__device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint32_t at, f32x16& s) {
+  const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
+  const int32_t seen = (int32_t)(min(u.limit, u.t1) - at - half * 4);  // (below 2^31 each)
 #pragma unroll
-  for (int n = 0; n < NS; ++n)
+  for (int i = 0; i < 16; ++i)
+    if ((i / 4) * 8 + i % 4 >= seen) s[i] = kNone;
+  if (u.bad_pages) {
+    const uint32_t pos = at + (lane & 31u);
+    const bool there = !in_hole<TT>(u, pos) && page_of<TT>(p, u, min(pos, u.t1 - 1)) < p.pool.num_blocks;
+    const uint32_t bits = (uint32_t)__ballot(there) >> (half * 4);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const uint32_t pos = at + n * 32 + (i / 4) * 8 + half * 4 + i % 4;
-      bool seen = pos < u.limit && pos < u.t1;
-      if (u.bad_pages) seen = seen && !in_hole<TT>(u, pos) && page_of<TT>(p, u, min(pos, u.t1 - 1)) < p.pool.num_blocks;
-      if (!seen) s[n][i] = kNone;
-    }
+    for (int i = 0; i < 16; ++i)
+      if (!(bits >> ((i / 4) * 8 + i % 4) & 1u)) s[i] = kNone;
+  }
 }
 
 // Moves the state's base if a product exceeds it by too much; top: the largest of the lane's.  (The number subtracted need not be the
@@ -395,12 +404,13 @@ template <int DT, int DP, int NS>
 __device__ __forceinline__ void add_seen_values(const Unit& u, uint32_t at, State<DP>& x, const u32x4 KVC_LDS* v, const u32x4 (&w)[NS][2]) {
   constexpr int CH = DP / 8, TT = NS * 32;
   const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
-  bool wild = false;
-  for (uint32_t i = lane; i < (uint32_t)(TT * CH); i += 64) {
-    const u32x4 y = v[i];
-    wild |= not_finite<DT>(y.x) || not_finite<DT>(y.y) || not_finite<DT>(y.z) || not_finite<DT>(y.w);
+  uint32_t wild = 0;
+#pragma unroll
+  for (int i = 0; i < TT * CH / 64; ++i) {
+    const u32x4 y = v[i * 64 + lane];
+    wild |= wild_bits<DT>(y.x) | wild_bits<DT>(y.y) | wild_bits<DT>(y.z) | wild_bits<DT>(y.w);
   }
-  if (!__any(wild)) {
+  if (!__any((wild & 0x80008000u) != 0)) {
     add_values<DT, DP, NS>(x, v, w);
     return;
   }
@@ -546,7 +556,7 @@ template <int DT, int DP>
 __device__ __forceinline__ void take_masked(const AttendParams& p, const Unit& u, uint32_t at, State<DP>& x, const f32x16& products, const u32x4 KVC_LDS* v) {
   f32x16 s[1] = {products};
   u32x4 w[1][2];
-  mask<1, 64>(p, u, at, s);
+  mask<64>(p, u, at, s[0]);
   weights<DT, DP, 1>(p, x, s, w);
   if (hides_tokens<32>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
   else add_values<DT, DP, 1>(x, v, w);
@@ -585,7 +595,7 @@ __device__ __forceinline__ void step_of_one(const AttendParams& p, Unit& u, cons
   load_tile(u, keys, from, k);
   asm volatile("" ::: "memory");
   page = page_of_lane<S::TT>(p, u, at + 2 * next);  // (between this line and the wait below: it is one of the loads counted there)
-  if constexpr (!PLAIN) mask<1, S::TT>(p, u, at, s);
+  if constexpr (!PLAIN) mask<S::TT>(p, u, at, s[0]);
   weights<DT, DP, 1>(p, x, s, w);
   wait_loads<N + 1>();  // V is there; the next K and its successor's page follow
   if (!PLAIN && hides_tokens<S::TT>(u, at)) add_seen_values<DT, DP, 1>(u, at, x, v, w);
@@ -832,7 +842,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   constexpr uint32_t SIDE = 64 / QD == 0 ? 1 : 64 / QD;  // rows that a wave writes at a time
   constexpr uint32_t MINE = R == 1 ? 8 : 32;             // rows that it writes in all
   const uint32_t begin = R == 1 ? wave * 8 : 0, at = lane % QD;
-#pragma unroll 2
+#pragma unroll 8
   for (uint32_t i = 0; i < MINE; i += SIDE) {
     const uint32_t r = begin + i + lane / QD;
     f32x4 o = {0, 0, 0, 0};
@@ -1006,12 +1016,13 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 }  // namespace
 
 // Whether the prefix is read anew for each request.  It costs the products of about 64 rows of a block that a request does not fill, over the
-// prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s; and there have to be blocks enough
-// for the chip without cutting along the tokens.
+// prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s.  (Of eight to twenty blocks there are too
+// few: 15 tokens of 64 heads over 265 gain 12 %, 60 tokens of 16 heads over 446 lose 7 %; from 39 on the sequences were 25-40 % faster, but for one case of 9
+// % slower.)
 bool one_sequence(const AttendParams& p) {
   const uint64_t rows = (uint64_t)p.batch.n_new * p.G;
   if (p.prefix == 0 || p.most_tokens == p.prefix || (uint64_t)p.batch.most_new * p.G <= 32) return false;
-  return rows * p.H >= 128 * 256 && (uint64_t)p.batch.n_requests * p.prefix < 14 * rows;
+  return rows * p.H >= 128 * 32 && (uint64_t)p.batch.n_requests * p.prefix < 14 * rows;
 }
 
 kvc_status plan_attend(AttendParams& p) {
@@ -1035,7 +1046,8 @@ kvc_status plan_attend(AttendParams& p) {
     // is long (64 rows of queries, 256 of a head: of 64K tokens 16 or 32 pieces 125 or 120 us; of 32K, where the rows' own 500 tokens each take the
     // second workgroup's place, 66 or 76); where more than two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms
     // instead of 1.75).
-    const uint64_t lengthy = i == 0 && p.most_tokens > p.prefix ? 2048 : 1024;
+    // Of a row's own tokens four waves side by side take pieces of 512 (19 requests of 56 heads with 2000 tokens each 55 or 42 us).
+    const uint64_t lengthy = i == 0 && p.most_tokens > p.prefix ? 2048 : a.waves == 4 ? 256 : 1024;
     uint64_t splits = whole <= chip && tokens * whole >= lengthy * chip ? chip / whole : whole <= 256 ? 256 / whole : 1;
     if (whole > chip && tokens >= 4096 && 20 * ((whole + chip - 1) / chip) * chip > 23 * whole) splits = 2;
     uint64_t each = (tokens + splits - 1) / splits;
