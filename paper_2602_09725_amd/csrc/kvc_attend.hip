@@ -685,29 +685,6 @@ __device__ __forceinline__ void put_sums(const AttendParams& p, const State<DP>&
   }
 }
 
-// Four sums of a row, the at-th vector of them: to the pieces, or divided to the result.
-template <int DT>
-__device__ __forceinline__ void write_row(const AttendParams& p, bool shared, const Place& w, const Request& q, uint32_t new_tokens, uint32_t row, uint32_t at,
-                                          f32x4 o, float top, float total) {
-  uint32_t t, g;
-  fd_divmod(p.dG, row, t, g);
-  if (t >= new_tokens) return;
-  const uint32_t token = shared ? t : q.first + t, head = w.head * p.G + g;
-  const uint32_t piece = shared ? w.split : p.part[0].splits + w.split;
-  const uint64_t slot = ((uint64_t)piece * p.batch.n_new + token) * (p.H * p.G) + head;
-  if (p.pieces > 1) {
-    if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
-    if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
-    return;
-  }
-  const float y = total == 0.0f ? 0.0f : 1.0f / total;
-  if (at * 4 < p.D) {
-    const u32x2 r = {narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
-    *(KVC_GLOBAL u32x2*)(p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4) = r;
-  }
-  if (at == 0 && p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
-}
-
 // One workgroup's unit: rows x head x piece of the tokens.
 template <int DT, int DP, int R, bool BIG>
 __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, const Lds& lds, Tops& tops) {
@@ -841,28 +818,51 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   constexpr uint32_t QD = DP / 4;                         // vectors of four sums of a row
   constexpr uint32_t SIDE = 64 / QD == 0 ? 1 : 64 / QD;  // rows that a wave writes at a time
   constexpr uint32_t MINE = R == 1 ? 8 : 32;             // rows that it writes in all
+  constexpr int PARTS = R == 1 ? 4 : 1;                  // waves that have a sum of a row
+  // A lane knows where its row goes and what the waves' sums of it weigh; those who write it ask the lane.
+  float share[PARTS];  // below 0: the wave saw nothing
+  uint64_t to = 0;
+  {
+    float m[PARTS], top = kNone, total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) m[k] = tops.m[R == 1 ? k : wave][col], top = fmaxf(top, m[k]);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      share[k] = R == 1 ? weight(m[k], top) : 1.0f;
+      total += share[k] * tops.l[R == 1 ? k : wave][col];
+    }
+    const float y = p.pieces > 1 ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) share[k] = m[k] == kNone ? -1.0f : share[k] * y;
+    uint32_t t, g;
+    fd_divmod(p.dG, base_row + col, t, g);
+    if (t < new_tokens) {
+      const uint32_t at_token = shared ? t : q.first + t, head = at_work.head * p.G + g;
+      const uint32_t piece = shared ? at_work.split : p.part[0].splits + at_work.split;
+      const uint64_t slot = ((uint64_t)piece * p.batch.n_new + at_token) * (p.H * p.G) + head;
+      to = p.pieces > 1 ? (uint64_t)(p.sums + slot * p.D) : (uint64_t)(p.out + (int64_t)at_token * p.o_token + (int64_t)head * p.o_head);
+      if (half == 0 && (R == 4 || wave == 0)) {
+        if (p.pieces > 1) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
+        else if (p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+      }
+    }
+  }
   const uint32_t begin = R == 1 ? wave * 8 : 0, at = lane % QD;
 #pragma unroll 8
   for (uint32_t i = 0; i < MINE; i += SIDE) {
     const uint32_t r = begin + i + lane / QD;
+    auto of_row = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(r * 4), (int)v); };
+    uint8_t* const there_to = (uint8_t*)((uint64_t)of_row((uint32_t)(to >> 32)) << 32 | of_row((uint32_t)to));
     f32x4 o = {0, 0, 0, 0};
-    float top = kNone, total = 0.0f;
-    if constexpr (R == 1) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) top = fmaxf(top, tops.m[k][r]);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float y = weight(tops.m[k][r], top);
-        total += y * tops.l[k][r];
-        const f32x4 v = ((const f32x4 KVC_LDS*)lds.of(k))[r * QD + (at ^ (r & 15u))];
-        if (tops.m[k][r] != kNone) o += y * v;
-      }
-    } else {
-      top = tops.m[wave][r];
-      total = tops.l[wave][r];
-      o = mine[r * QD + (at ^ (r & 15u))];
+    for (int k = 0; k < PARTS; ++k) {
+      const float x = __builtin_bit_cast(float, of_row(__builtin_bit_cast(uint32_t, share[k])));
+      const f32x4 v = (R == 1 ? (const f32x4 KVC_LDS*)lds.of(k) : (const f32x4 KVC_LDS*)mine)[r * QD + (at ^ (r & 15u))];
+      if (!(x < 0.0f)) o += x * v;
     }
-    write_row<DT>(p, shared, at_work, q, new_tokens, base_row + r, at, o, top, total);
+    if (!there_to || at * 4 >= p.D) continue;
+    if (p.pieces > 1) *(KVC_GLOBAL f32x4*)(there_to + at * 16) = o;
+    else *(KVC_GLOBAL u32x2*)(there_to + at * 8) = u32x2{narrow_pair<DT>(o.x, o.y), narrow_pair<DT>(o.z, o.w)};
   }
 }
 
