@@ -685,12 +685,14 @@ __device__ __forceinline__ void put_sums(const AttendParams& p, const State<DP>&
   }
 }
 
-// One workgroup's unit: rows x head x piece of the tokens.
-template <int DT, int DP, int R, bool BIG>
+// One unit: rows x head x piece of the tokens; a workgroup's, or (LONE) a wave's.
+template <int DT, int DP, int R, bool BIG, bool LONE = false>
 __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, const Lds& lds, Tops& tops) {
   using S = Shape<DP, R>;
   constexpr int TT = S::TT, KK = DP / 16, DD = DP / 32;
+  constexpr bool JOINED = R == 1 && !LONE;  // the waves of a workgroup have tokens of the same rows
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u, half = lane >> 5;
+  const uint32_t speaker = LONE ? lane : threadIdx.x;
 
   const Place at_work = place_of_unit(p, part, shared, unit);
 
@@ -701,7 +703,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   if (!shared) q = request_at(p, at_work.request);
   const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
   if (!shared && at_work.block * (R * 32) >= wave_uniform(new_tokens) * p.G) {  // (a request with fewer new tokens than others)
-    if (threadIdx.x == 0) fault(p, q.faults);
+    if (speaker == 0) fault(p, q.faults);
     return;
   }
   u.bound = shared ? p.prefix : p.most_tokens;
@@ -710,8 +712,8 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   u.front_table = p.pool.tables + (uint64_t)p.prefix_row * p.pool.table_len;
   u.page_fault = false;
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
-  constexpr uint32_t NEXT = S::GROUPS * TT;  // from a tile of a wave to its next
-  const uint32_t start = u.t0 + (R == 1 ? wave_uniform(wave) * TT : 0);
+  constexpr uint32_t NEXT = LONE ? TT : S::GROUPS * TT;  // from a tile of a wave to its next
+  const uint32_t start = u.t0 + (JOINED ? wave_uniform(wave) * TT : 0);
   uint32_t page[3];
 #pragma unroll
   for (int i = 0; i < (R == 1 ? 2 : 3); ++i) page[i] = page_of_lane<TT>(p, u, start + i * NEXT);
@@ -726,7 +728,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   if (shared) q = request_at(p, request_of(p.batch, token));
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
   u.known = u.front ? prefix_there(p) : 0;
-  if ((shared ? u.t1 < p.prefix : u.known < u.front) && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
+  if ((shared ? u.t1 < p.prefix : u.known < u.front) && speaker == 0) fault(p, KVC_FAULT_LIST);
   u.t1 = min(u.t1, u.t0 + part.tokens);
   u.bad_pages = false;
   u.limit = u.least = 0;
@@ -737,8 +739,13 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   Sources<DP, 4, BIG> next;
   if constexpr (R == 1) {
     const uint32_t self = wave_uniform(wave);
-    k0 = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
-    v0 = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
+    if constexpr (LONE) {
+      k0 = lds.of(self);  // (its sums follow there)
+      v0 = k0 + S::TILE;
+    } else {
+      k0 = (self < 2 ? lds.a : lds.b) + (self & 1u) * S::TILE;
+      v0 = (self < 2 ? lds.c : lds.d) + (self & 1u) * S::TILE;
+    }
     if (has_tile) {
       const Sources<DP, 1, BIG> from = sources_of<DP, 1, BIG>(p, u, start, page[0]);
       load_tile(u, u.keys, from, k0);
@@ -759,7 +766,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   }
 
   // How far the rows see.
-  if (shared ? there && at_work.split == 0 && at_work.head == 0 && half == 0 : threadIdx.x == 0) fault(p, q.faults);
+  if (shared ? there && at_work.split == 0 && at_work.head == 0 && half == 0 : speaker == 0) fault(p, q.faults);
   u.limit = there ? limit_of(p, q, token) : 0;
   uint32_t most = u.limit, least = there ? u.limit : ~0u;
   if constexpr (R == 1) lanes_see(most, least);
@@ -811,25 +818,27 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   if (u.page_fault && lane == 0) fault(p, KVC_FAULT_PAGE);
   if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
   // Results: sums go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
-  __syncthreads();
+  if constexpr (LONE) wait_reads();
+  else __syncthreads();
   f32x4 KVC_LDS* const mine = (f32x4 KVC_LDS*)lds.of(wave_uniform(wave));
   put_sums<DP>(p, x, mine, tops.m[wave], tops.l[wave]);
-  __syncthreads();
+  if constexpr (LONE) wait_reads();
+  else __syncthreads();
   constexpr uint32_t QD = DP / 4;                         // vectors of four sums of a row
   constexpr uint32_t SIDE = 64 / QD == 0 ? 1 : 64 / QD;  // rows that a wave writes at a time
-  constexpr uint32_t MINE = R == 1 ? 8 : 32;             // rows that it writes in all
-  constexpr int PARTS = R == 1 ? 4 : 1;                  // waves that have a sum of a row
+  constexpr uint32_t MINE = JOINED ? 8 : 32;             // rows that it writes in all
+  constexpr int PARTS = JOINED ? 4 : 1;                  // waves that have a sum of a row
   // A lane knows where its row goes and what the waves' sums of it weigh; those who write it ask the lane.
   float share[PARTS];  // below 0: the wave saw nothing
   uint64_t to = 0;
   {
     float m[PARTS], top = kNone, total = 0.0f;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) m[k] = tops.m[R == 1 ? k : wave][col], top = fmaxf(top, m[k]);
+    for (int k = 0; k < PARTS; ++k) m[k] = tops.m[JOINED ? k : wave][col], top = fmaxf(top, m[k]);
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
-      share[k] = R == 1 ? weight(m[k], top) : 1.0f;
-      total += share[k] * tops.l[R == 1 ? k : wave][col];
+      share[k] = JOINED ? weight(m[k], top) : 1.0f;
+      total += share[k] * tops.l[JOINED ? k : wave][col];
     }
     const float y = p.pieces > 1 ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
@@ -841,15 +850,16 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       const uint32_t piece = shared ? at_work.split : p.part[0].splits + at_work.split;
       const uint64_t slot = ((uint64_t)piece * p.batch.n_new + at_token) * (p.H * p.G) + head;
       to = p.pieces > 1 ? (uint64_t)(p.sums + slot * p.D) : (uint64_t)(p.out + (int64_t)at_token * p.o_token + (int64_t)head * p.o_head);
-      if (half == 0 && (R == 4 || wave == 0)) {
+      if (half == 0 && (!JOINED || wave == 0)) {
         if (p.pieces > 1) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
         else if (p.lse) p.lse[slot] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
       }
     }
   }
-  const uint32_t begin = R == 1 ? wave * 8 : 0, at = lane % QD;
-#pragma unroll 8
-  for (uint32_t i = 0; i < MINE; i += SIDE) {
+  const uint32_t begin = JOINED ? wave * 8 : 0, at = lane % QD;
+  const uint32_t rows = LONE ? min(MINE, wave_uniform(new_tokens) * p.G - base_row) : MINE;
+#pragma unroll LONE ? 1 : 8
+  for (uint32_t i = 0; i < rows; i += SIDE) {
     const uint32_t r = begin + i + lane / QD;
     auto of_row = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(r * 4), (int)v); };
     uint8_t* const there_to = (uint8_t*)((uint64_t)of_row((uint32_t)(to >> 32)) << 32 | of_row((uint32_t)to));
@@ -857,7 +867,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
       const float x = __builtin_bit_cast(float, of_row(__builtin_bit_cast(uint32_t, share[k])));
-      const f32x4 v = (R == 1 ? (const f32x4 KVC_LDS*)lds.of(k) : (const f32x4 KVC_LDS*)mine)[r * QD + (at ^ (r & 15u))];
+      const f32x4 v = (JOINED ? (const f32x4 KVC_LDS*)lds.of(k) : (const f32x4 KVC_LDS*)mine)[r * QD + (at ^ (r & 15u))];
       if (!(x < 0.0f)) o += x * v;
     }
     if (!there_to || at * 4 >= p.D) continue;
@@ -886,7 +896,10 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendPar
   uint32_t unit;
   if (!unit_of(p, shared, unit)) return;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  if (ONES || part.waves == 1) attend_unit<DT, DP, 1, BIG>(p, part, shared, unit, lds, tops);
+  if (part.lone) {
+    unit = unit * 4 + wave_uniform(threadIdx.x >> 6);
+    if (unit < part.lone) attend_unit<DT, DP, 1, BIG, true>(p, part, shared, unit, lds, tops);
+  } else if (ONES || part.waves == 1) attend_unit<DT, DP, 1, BIG>(p, part, shared, unit, lds, tops);
   else if constexpr (!ONES) attend_unit<DT, DP, 4, BIG>(p, part, shared, unit, lds, tops);
 }
 
@@ -1059,6 +1072,13 @@ kvc_status plan_attend(AttendParams& p) {
     a.splits = (uint32_t)splits;
     a.tokens = (uint32_t)each;
     a.units = (uint32_t)(whole * splits);
+    // A wave each has a unit of few tokens where there are many: a workgroup's life is mostly that of memory's answers one after the other, and it has four
+    // at a time so (91 requests of 32 heads with 6 tokens 67 -> 41 us, 128 of 8 heads with 60 or 250: 37.8 -> 30.4, 41.7 -> 35.2, 32 with 20: 21.7 -> 20.8;
+    // 64 with 500 beside a prefix of 32K, from memory, 77 -> 81, and with 1000 48.8 -> 53.1, so these keep a workgroup).
+    if (i == 1 && a.waves == 1 && each <= 256 && 2 * whole * splits >= chip) {
+      a.lone = a.units;
+      a.units = (a.units + 3) / 4;
+    }
     a.drows = make_fastdiv(a.row_blocks);
     a.dsplits = make_fastdiv(a.splits);
     a.drequests = make_fastdiv(p.batch.n_requests);

@@ -73,6 +73,7 @@ struct AttendPart {
   uint32_t splits;      // pieces of the tokens, 0: the part is empty
   uint32_t tokens;      // of a piece
   uint32_t units;       // workgroups
+  uint32_t lone;        // units in all, a wave each; 0: a workgroup each
   FastDiv drows, dsplits, drequests, dtokens;
 };
 

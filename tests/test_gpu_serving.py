@@ -774,3 +774,26 @@ def test_wild_values_of_one_sequence(kvc_lib):
     assert bool((a.out[first:260, :, 5] == math.inf).all())
     rest = [d for d in range(128) if d != 5]
     assert torch.equal(a.out[first:260][:, :, rest], clean.out[first:260][:, :, rest])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", [
+    (32, 1, 128, 16, 70, [71 + (5 * i) % 60 for i in range(20)], None),           # a wave each has a head of a request
+    (32, 3, 64, 5, 33, [40 + (7 * i) % 90 for i in range(17)], [1 + i % 4 for i in range(17)]),
+    (16, 8, 256, 32, 100, [101 + (i * 31) % 128 if i % 5 else 90 + i % 3 for i in range(33)], None),  # some end inside the prefix
+    (40, 1, 72, 1, 0, [(3 * i) % 129 for i in range(15)], [min((3 * i) % 129, i % 6) for i in range(15)]),
+    (32, 1, 128, 16, 64, [64, 64, 65, 192, 0, 1] + [70] * 11, None),
+], ids=[f"c{i}" for i in range(5)])
+def test_many_rows_of_few_tokens(kvc_lib, case, dtype):
+    hz.say(f"[case] few tokens {case} {dtype}")
+    a = Attend(*case[:3], dtype, *case[3:], seed=len(case[5]))
+    a.call()
+    a.check()
+    a.books.tables[a.rows[3]][case[4] // case[3]] = -1  # the page of the first own token, and of what the prefix has in it
+    a.device.tables.copy_(i32(a.books.tables))
+    a.call()
+    block = case[3]
+    first = case[4] // block * block
+    lost = [(a.rows[3], p) for p in range(max(first, case[4]), first + block)]
+    seen = a.lens[3] > case[4] and a.new[3] > 0
+    a.check(err=model.FAULT_PAGE if seen else 0, missing=lost)
