@@ -798,7 +798,8 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       // (whether a page is bad is known two tiles ahead)
       for (; pos + 2 * TT <= plain && !u.bad_pages; pos += 2 * TT) {
         step_of_four<DT, DP, BIG>(p, u, pos, next, page[2], query, x, s[0], lds.a, lds.b, lds.c, lds.d, true);
-        step_of_four<DT, DP, BIG>(p, u, pos + TT, next, page[2], query, x, s[0], lds.c, lds.d, lds.a, lds.b, pos + 3 * TT <= plain);
+        // (the first step has seen the pages of the tile whose products the second one begins)
+        step_of_four<DT, DP, BIG>(p, u, pos + TT, next, page[2], query, x, s[0], lds.c, lds.d, lds.a, lds.b, pos + 3 * TT <= plain && !u.bad_pages);
       }
       if (pos + TT <= plain && !u.bad_pages) {
         step_of_four<DT, DP, BIG>(p, u, pos, next, page[2], query, x, s[0], lds.a, lds.b, lds.c, lds.d, false);
