@@ -614,12 +614,14 @@ typedef struct {
   uint32_t struct_size; /* sizeof(kvc_batch)                                    */
   uint32_t abi_version; /* KVC_ABI_VERSION                                      */
   int32_t n_requests;   /* >= 0                                                 */
-  int32_t most_new;     /* no request has more new tokens (a bound for the launch; later ones get no result, KVC_FAULT_LIST) */
+  int32_t most_new;     /* no request has more new tokens (a bound for the launch)                  */
   int64_t n_new;        /* new tokens of all requests, below 2^31               */
   const int32_t* d_rows;   /* DEVICE int32 [n_requests]; NULL: row r            */
   const int32_t* d_starts; /* DEVICE int32 [n_requests + 1], ascending from 0 to n_new: request r has the tokens
                               [starts[r], starts[r+1]); NULL: one token each (n_new == n_requests, most_new == 1) */
 } kvc_batch;
+/* Tokens that no request covers -- before starts[0], from starts[n_requests] on, or a request's beyond its first most_new -- are
+ * KVC_FAULT_LIST: attention writes 0 for them and a logarithm of -inf. */
 
 /* Writes keys and values of the batch's new tokens to their slots in one layer.
  *   k, v          DEVICE in: [n_new][H][D], 16-byte aligned, the [H][D] of a token contiguous

@@ -76,6 +76,7 @@ __device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r)
     const uint32_t end = b < p.batch.n_new ? b : p.batch.n_new;
     q.n = end > q.first ? end - q.first : 0;
     if (a > b || b > p.batch.n_new || q.n > p.batch.most_new) q.faults |= KVC_FAULT_LIST;
+    if ((r == 0 && a != 0) || (r + 1 == p.batch.n_requests && b != p.batch.n_new)) q.faults |= KVC_FAULT_LIST;
   }
   const bool known = q.row < p.pool.n_rows;
   q.row = known ? q.row : 0;
@@ -85,8 +86,12 @@ __device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r)
   return q;
 }
 
-// Positions that new token t of a request sees: those below this.
+// New tokens of a request that have a result.
+__device__ __forceinline__ uint32_t covered(const AttendParams& p, const Request& q) { return min(q.n, p.batch.most_new); }
+
+// Positions that new token t of a request sees: those below this.  (A token whose request does not cover it sees none.)
 __device__ __forceinline__ uint32_t limit_of(const AttendParams& p, const Request& q, uint32_t t) {
+  if (t - q.first >= covered(p, q)) return 0;
   const int64_t seen = (int64_t)q.len - q.n + (t - q.first) + 1;
   return seen < 0 ? 0 : seen < (int64_t)p.most_tokens ? (uint32_t)seen : p.most_tokens;
 }
@@ -101,6 +106,26 @@ __device__ __forceinline__ uint32_t request_of(const BatchView& b, uint32_t t) {
     else high = mid;
   }
   return low;
+}
+
+// Writes the result of new tokens [from, to) for a KV head's query heads: that of rows that see nothing.  self: one of so many threads.
+__device__ __forceinline__ void write_none(const AttendParams& p, uint32_t from, uint32_t to, uint32_t head, uint32_t self, uint32_t threads) {
+  const uint32_t rows = from < to ? (to - from) * p.G : 0;
+  for (uint32_t row = self; row < rows; row += threads) {
+    uint32_t t, g;
+    fd_divmod(p.dG, row, t, g);
+    const uint32_t token = from + t, h = head * p.G + g;
+    uint16_t* const out = p.out + (int64_t)token * p.o_token + (int64_t)h * p.o_head;
+    for (uint32_t at = 0; at < p.D; at += 8) *(KVC_GLOBAL u32x4*)(out + at) = u32x4{0, 0, 0, 0};
+    if (p.lse) p.lse[(uint64_t)token * (p.H * p.G) + h] = kNone;
+  }
+}
+
+// The new tokens around a request's that no request covers: its own beyond the bound, and those before the first request's and after the last one's.
+__device__ __forceinline__ void write_uncovered(const AttendParams& p, const Request& q, uint32_t request, uint32_t head, uint32_t self, uint32_t threads) {
+  const uint32_t end = q.first + q.n;
+  write_none(p, q.first + covered(p, q), request + 1 == p.batch.n_requests ? p.batch.n_new : end, head, self, threads);
+  if (request == 0) write_none(p, 0, q.first, head, self, threads);
 }
 
 // Tokens of the shared prefix that there are.
@@ -701,7 +726,9 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   Unit u;
   Request q{};
   if (!shared) q = request_at(p, at_work.request);
-  const uint32_t new_tokens = shared ? p.batch.n_new : q.n < p.batch.most_new ? q.n : p.batch.most_new;
+  const uint32_t new_tokens = shared ? p.batch.n_new : covered(p, q);
+  if (!shared && p.pieces == 1 && at_work.block == 0 && q.faults)  // (of several pieces the join writes what these rows hold)
+    write_uncovered(p, q, at_work.request, at_work.head, speaker, LONE ? 64 : 256);
   if (!shared && at_work.block * (R * 32) >= wave_uniform(new_tokens) * p.G) {  // (a request with fewer new tokens than others)
     if (speaker == 0) fault(p, q.faults);
     return;
@@ -934,7 +961,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
   uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;
-  uint32_t n = p.part[1].splits && limit > p.own_from && token - q.first < p.batch.most_new ? fd_div(p.part[1].dtokens, limit - p.own_from + p.part[1].tokens - 1) : 0;
+  uint32_t n = p.part[1].splits && limit > p.own_from ? fd_div(p.part[1].dtokens, limit - p.own_from + p.part[1].tokens - 1) : 0;
   if (!there) a = n = 0;
   const uint32_t split = p.part[0].splits, end = split + n;
   auto holds = [&](uint32_t i) { return i < a || (i >= split && i < end); };

@@ -1,10 +1,13 @@
 """Serving calls where books, lists and pages are not what a call may rely on, and attention at the ends of its types and addresses."""
+import math
+
 import pytest
 import torch
 
 import kvc_harness as hz
+import paper_2602_09725_amd as kvc
 import serving_model as model
-from test_gpu_serving import Attend, i32
+from test_gpu_serving import Attend, i32, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +49,72 @@ def test_a_page_outside_the_pool_takes_nothing_from_those_before(kvc_lib, case, 
     a.device.tables.copy_(i32(a.books.tables))
     a.call()
     a.check(err=model.FAULT_PAGE)
+
+
+# ---- new tokens that no request covers
+
+
+def rows_near(a, request, tokens, seen):
+    """The results of these tokens of a request are those of the first seen[i] positions of its row."""
+    r, n = a.rows[request], max(seen)
+    got, got_lse = a.out[tokens].double().cpu(), a.lse[tokens].double().cpu()
+    positions = torch.arange(n)
+    own, front = torch.tensor(a.books.tables[r])[positions // a.block], torch.tensor(a.books.tables[0])[positions // a.block]
+    slots = torch.where(positions < a.prefix, front, own) * a.block + positions % a.block
+    flat = a.caches[a.layer].flatten(1, 2)[:, slots.cuda()].cpu()
+    visible = positions[None] < torch.tensor(seen)[:, None]
+    for h in range(a.H):
+        heads = slice(h * a.G, h * a.G + a.G)
+        want = model.attention(a.q[tokens, heads].cpu(), flat[0, :, h], flat[1, :, h], visible, a.scale)
+        far, far_lse = model.attention_bounds(*want, n, a.D, a.dtype)
+        a.near(f"out of request {request}, head {h}", got[:, heads], want[0], far)
+        a.near(f"lse of request {request}, head {h}", got_lse[:, heads], want[1], far_lse)
+
+
+UNCOVERED = {
+    "pieces": (2, 4, 128, 16, 700, [760, 720, 900], [6, 5, 9]),
+    "one wave": (2, 2, 64, 16, 0, [40, 60, 100], [6, 5, 9]),
+    "four waves": (2, 16, 128, 16, 0, [40, 60, 100], [6, 5, 9]),
+    "a wave each": (32, 1, 128, 16, 0, [40 + i for i in range(20)], [6, 5] + [4] * 17 + [9]),
+    "prefix alone": (2, 4, 128, 16, 90, [90, 80, 85], [6, 5, 9]),
+    "one sequence": (8, 8, 64, 16, 100, [320, 290, 300], [270, 250, 280]),
+}
+
+
+@pytest.mark.parametrize("wrong", ["tail", "head", "many", "descending"])
+@pytest.mark.parametrize("form", UNCOVERED)
+def test_tokens_that_no_request_covers_have_no_result(kvc_lib, form, wrong):
+    """They get 0 and -inf, whatever the workspace and the results held before, and the list is told to be at fault."""
+    hz.say(f"[case] uncovered {form} {wrong}")
+    case = UNCOVERED[form]
+    a = Attend(*case[:3], "f16", *case[3:], seed=7)
+    starts, most = starts_of(a.new), max(a.new)
+    if wrong == "tail":
+        starts[-1] -= 3
+    elif wrong == "head":
+        starts[0] = 2
+    elif wrong == "many":
+        most -= 2
+    else:
+        starts[1], starts[2] = starts[2], starts[1]
+    a.starts.copy_(i32(starts))
+    a.batch = kvc.Batch(len(a.new), sum(a.new), most, a.where.data_ptr(), a.starts.data_ptr())
+    a.space = torch.empty(kvc.attention_workspace(a.device.pool, a.batch, a.attention), dtype=torch.uint8, device="cuda")
+    a.space.view(torch.float32).fill_(1.5)
+    a.call()
+    torch.cuda.synchronize()
+    assert int(a.device.err.item()) == model.FAULT_LIST
+    assert bool((a.out_store[:, :, a.D:] == 7.0).all()) and bool((a.lse[-1] == 7.0).all())
+    if wrong == "descending":  # the requests overlap: their tokens' results are open, but they are results
+        assert not bool((a.out == 7.0).any()) and not bool((a.lse[:-1] == 7.0).any())
+        return
+    covered = torch.zeros(sum(a.new), dtype=torch.bool)
+    for request, (first, end) in enumerate(zip(starts, starts[1:])):
+        n = end - first
+        tokens = list(range(first, first + min(n, most)))
+        covered[tokens] = True
+        length = a.books.lens[a.rows[request]]
+        if request in (0, 1, len(a.new) - 1):
+            rows_near(a, request, tokens, [length - n + i + 1 for i in range(len(tokens))])
+    assert int((~covered).sum()) >= 2
+    assert bool((a.out[~covered.cuda()] == 0).all()) and bool((a.lse[:-1][~covered.cuda()] == -math.inf).all())
