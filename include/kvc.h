@@ -621,7 +621,7 @@ typedef struct {
                               [starts[r], starts[r+1]); NULL: one token each (n_new == n_requests, most_new == 1) */
 } kvc_batch;
 /* Tokens that no request covers -- before starts[0], from starts[n_requests] on, or a request's beyond its first most_new -- are
- * KVC_FAULT_LIST: attention writes 0 for them and a logarithm of -inf. */
+ * KVC_FAULT_LIST: attention writes 0 for them and a logarithm of -inf, kvc_append_paged leaves them out. */
 
 /* Writes keys and values of the batch's new tokens to their slots in one layer.
  *   k, v          DEVICE in: [n_new][H][D], 16-byte aligned, the [H][D] of a token contiguous

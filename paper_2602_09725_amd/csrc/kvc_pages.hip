@@ -693,7 +693,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendParams p) {
   bool several = false;
   if (p.batch.starts && r0 + 1 < p.batch.n_requests) several = (uint32_t)p.batch.starts[r0 + 1] <= (uint32_t)(most / per_token);
   u32x4 value[U];
-  uint32_t t[U], kind[U], atom[U], r[U], back[U], row[U], len[U], page[U], slot[U];
+  uint32_t t[U], kind[U], atom[U], r[U], first[U], back[U], row[U], len[U], page[U], slot[U];
   bool live[U];
   uint32_t bad = 0;
 #pragma unroll
@@ -711,6 +711,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendParams p) {
   for (int u = 0; u < U; ++u) {  // the token is its request's last but back - 1
     r[u] = p.batch.starts ? r0 : t[u];
     if (several) r[u] = request_from(p.batch, t[u], u ? r[u - 1] : r0);
+    first[u] = p.batch.starts ? (uint32_t)p.batch.starts[r[u]] : t[u];
     back[u] = p.batch.starts ? (uint32_t)p.batch.starts[r[u] + 1] - t[u] : 1u;
     row[u] = p.batch.rows ? (uint32_t)p.batch.rows[r[u]] : r[u];
   }
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendParams p) {
   for (int u = 0; u < U; ++u) {
     const bool known = row[u] < p.pool.n_rows;
     len[u] = (uint32_t)p.pool.lens[known ? row[u] : 0];
-    if (live[u] && (!known || len[u] > p.pool.capacity || back[u] - 1 >= len[u])) {
+    if (live[u] && (!known || len[u] > p.pool.capacity || back[u] - 1 >= len[u] || t[u] - first[u] >= p.batch.most_new)) {
       bad |= KVC_FAULT_LIST;
       live[u] = false;
     }

@@ -7,7 +7,7 @@ import torch
 import kvc_harness as hz
 import paper_2602_09725_amd as kvc
 import serving_model as model
-from test_gpu_serving import Attend, i32, starts_of
+from test_gpu_serving import Attend, DevicePool, filled, i32, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,30 @@ def test_tokens_that_no_request_covers_have_no_result(kvc_lib, form, wrong):
             rows_near(a, request, tokens, [length - n + i + 1 for i in range(len(tokens))])
     assert int((~covered).sum()) >= 2
     assert bool((a.out[~covered.cuda()] == 0).all()) and bool((a.lse[:-1][~covered.cuda()] == -math.inf).all())
+
+
+@pytest.mark.parametrize("H,D", [(1, 8), (40, 128)])  # (a vector a thread, and four)
+@pytest.mark.parametrize("wrong", ["head", "tail", "many"])
+def test_append_leaves_out_what_no_request_covers(kvc_lib, wrong, H, D):
+    books = filled(3, 80, 4, 200, [280, 290, 9], seed=6)
+    d = DevicePool(books, 1, H, D, refs=False)
+    before = d.copy()
+    new, most = [250, 200, 4], 250
+    starts = starts_of(new)
+    if wrong == "head":
+        starts[0] = 5
+    elif wrong == "tail":
+        starts[-1] -= 2
+    else:
+        most = 230
+    n, where = sum(new), i32(starts)
+    x = torch.randint(-32768, 32768, (n, H * D), device="cuda", dtype=torch.int16)
+    kvc.kvc_append_paged(d.pool, kvc.Batch(3, n, most, None, where.data_ptr()), 0, x.data_ptr(), x.data_ptr(), H * D, hz.stream_handle())
+    want = before[0].clone()
+    for r, (first, end) in enumerate(zip(starts, starts[1:])):
+        for t in range(first, min(end, first + most)):
+            at = books.lens[r] - end + t
+            want[:, books.tables[r][at // 4], at % 4] = x[t]
+    books.err = model.FAULT_LIST
+    d.check()
+    assert torch.equal(d.caches[0], want)
