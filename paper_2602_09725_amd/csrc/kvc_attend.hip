@@ -958,6 +958,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   f32x2 first = {kNone, 0.0f};
   if (self < p.pieces) first = *(const KVC_GLOBAL f32x2*)(p.tops + slot(self) * 2);
   const Request q = request_at(p, request_of(p.batch, token));
+  if (p.pieces == 0 && there && head == 0 && self == 0) fault(p, q.faults);  // (no other kernel has looked at it)
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
   uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;

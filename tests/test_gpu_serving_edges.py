@@ -120,6 +120,18 @@ def test_tokens_that_no_request_covers_have_no_result(kvc_lib, form, wrong):
     assert bool((a.out[~covered.cuda()] == 0).all()) and bool((a.lse[:-1][~covered.cuda()] == -math.inf).all())
 
 
+def test_books_at_fault_are_told_where_nothing_may_be_seen(kvc_lib):
+    """No position lies below a bound of 0 tokens: all rows are empty, and those that are not are told."""
+    for lens, err in (([0, 0, 0], 0), ([0, 9, 0], model.FAULT_LIST)):
+        a = Attend(2, 2, 64, "f16", 16, 0, lens, None, seed=2)
+        a.most = 0
+        a.attention = kvc.Attention(4, a.scale, 0, 0, 0, a.q.stride()[:2], a.out.stride()[:2])
+        a.call()
+        torch.cuda.synchronize()
+        assert int(a.device.err.item()) == err
+        assert bool((a.out == 0).all()) and bool((a.lse[:-1] == -math.inf).all())
+
+
 @pytest.mark.parametrize("H,D", [(1, 8), (40, 128)])  # (a vector a thread, and four)
 @pytest.mark.parametrize("wrong", ["head", "tail", "many"])
 def test_append_leaves_out_what_no_request_covers(kvc_lib, wrong, H, D):
