@@ -585,7 +585,7 @@ kvc_status kvc_pages_fork(const kvc_pool* pool, const int32_t* d_parents, const 
  *   d_rows    DEVICE in: int32 [n], n <= n_rows, no row twice
  *   d_counts  DEVICE in: int32 [n], >= 0; NULL: one token each
  * KVC_FAULT_LIST too where a last page that is filled in part and would be written
- * to is held by another row. */
+ * to is held by another row, or is free; other pages of the rows are not looked at. */
 kvc_status kvc_pages_grow(const kvc_pool* pool, const int32_t* d_rows, const int32_t* d_counts, int64_t n, void* workspace,
                           size_t workspace_bytes, void* stream);
 

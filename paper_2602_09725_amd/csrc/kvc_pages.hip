@@ -96,9 +96,9 @@ __device__ __forceinline__ Entry entry_of(const PoolView& p, uint32_t row, int32
   } else {
     e.more = (uint32_t)more;
     e.need = pages_of(p, len + e.more) - e.held;
-    if (part && more > 0) {  // its last page will be written to
+    if (part && more > 0) {  // its last page will be written to: it has to be this row's alone
       if (e.last >= p.num_blocks) fault(p, KVC_FAULT_PAGE);
-      else if (p.refs[e.last] > 1) bad |= KVC_FAULT_LIST;
+      else if (p.refs[e.last] != 1) bad |= KVC_FAULT_LIST;
     }
   }
   return e;

@@ -157,3 +157,35 @@ def test_append_leaves_out_what_no_request_covers(kvc_lib, wrong, H, D):
     books.err = model.FAULT_LIST
     d.check()
     assert torch.equal(d.caches[0], want)
+
+
+# ---- tables that hold free pages
+
+
+def books_of(blocks, lens, seed):
+    books = filled(8, 6, 4, blocks, lens, seed=seed)
+    return books
+
+
+@pytest.mark.parametrize("blocks", [40, 20000])
+@pytest.mark.parametrize("count", [0, -2])
+def test_a_grow_into_a_free_page_changes_nothing(kvc_lib, blocks, count):
+    """A last page that is filled in part and held by nobody could be another row's by now."""
+    books = books_of(blocks, [9, 8, 6, 0], blocks)
+    books.refs[books.tables[2][1]] = count
+    books.refs[books.tables[1][1]] = 0  # filled to its end: nobody writes to it
+    d = DevicePool(books, 1, 1, 8)
+    before = d.copy()
+    for more in ([3, 1, 5], [3, 2, 0]):
+        rows, counts = i32([0, 2, 3]), i32(more)
+        kvc.kvc_pages_grow(d.pool, rows.data_ptr(), counts.data_ptr(), 3, *d.room())
+        books.err = model.FAULT_LIST
+        d.check(before)
+    if count == 0:
+        d.err.zero_()
+        books.err = 0
+        rows, counts = i32([2, 0]), i32([0, 5])  # a row that gets no token is not written to
+        kvc.kvc_pages_grow(d.pool, rows.data_ptr(), counts.data_ptr(), 2, *d.room())
+        books.grow([2, 0], [0, 5])
+        assert books.err == 0
+        d.check(before)
