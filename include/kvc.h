@@ -529,7 +529,7 @@ kvc_status kvc_tiling_costs(const kvc_layout* layout, const void* kv, kvc_stride
  * Faults that only the device can see are ORed into *d_err (KVC_FAULT_*).  A
  * fork or grow whose list is at fault (KVC_FAULT_LIST) or lacks room
  * (KVC_FAULT_NO_ROOM) changes nothing at all; a count of holders below 0 is
- * taken for 0; what a single bad page id does is said at each call. */
+ * taken for 0; what a single bad page id or free page does is said at each call. */
 enum {
   KVC_FAULT_PAGE = 1,    /* a table entry or page id outside [0, num_blocks): what it would touch is left out  */
   KVC_FAULT_LIST = 2,    /* a list or book that contradicts itself: a row outside [0, n_rows), a length outside
@@ -575,8 +575,9 @@ size_t kvc_pages_workspace(const kvc_pool* pool);
  *   d_parents, d_children  DEVICE in: int32 [n], n <= n_rows.  A child's length must be 0;
  *                          a parent may have many children, a child may not be a
  *                          parent or a child twice in one call
- * A parent's entry outside the pool is copied as it is and shared with nobody
- * (KVC_FAULT_PAGE). */
+ * A whole page of a parent's that is outside the pool or free is copied to the child's table as it is and
+ * shared with nobody (KVC_FAULT_PAGE, KVC_FAULT_LIST); the call goes on.  A last page that is filled in part
+ * and free is a list at fault; one outside the pool leaves the child's page as it was (KVC_FAULT_PAGE). */
 kvc_status kvc_pages_fork(const kvc_pool* pool, const int32_t* d_parents, const int32_t* d_children, int64_t n,
                           void* workspace, size_t workspace_bytes, void* stream);
 

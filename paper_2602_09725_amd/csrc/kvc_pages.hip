@@ -128,7 +128,9 @@ __device__ void plan_list(const PoolView& p, const PageSpace& w, const int32_t* 
     if (i < n) {
       const uint32_t row = (uint32_t)a[i];
       if (LIST == PageList::kFork) bad |= parent_noted(p, row, seen);
-      need = entry_of<LIST>(p, row, LIST == PageList::kGrow && b ? b[i] : 1, bad).need;
+      const Entry e = entry_of<LIST>(p, row, LIST == PageList::kGrow && b ? b[i] : 1, bad);
+      need = e.need;
+      if (LIST == PageList::kFork && need && e.last < p.num_blocks && p.refs[e.last] <= 0) bad |= KVC_FAULT_LIST;  // (its tokens are nobody's)
     }
     uint64_t total;
     const uint64_t before = group_scan(need, sums, &total);
@@ -304,6 +306,8 @@ __device__ __forceinline__ OnePlan plan_one(const PoolView& p, OneBooks& s, cons
   if (__any(below) && lane_id() == 0) fault(p, KVC_FAULT_LIST);
   __syncthreads();
   if (mine) bad |= note_row<LIST>(p, LIST == PageList::kFork ? (uint32_t)other : row, other_len, seen);
+  if (LIST == PageList::kFork && plan.e.need && plan.e.last < p.num_blocks && (s.words[plan.e.last / 32] >> plan.e.last % 32 & 1u))
+    bad |= KVC_FAULT_LIST;  // (its tokens are nobody's)
   const uint64_t v = (uint64_t)(self < kOneWords ? __popc(s.words[self]) : 0) << 44 | plan.e.need;
   const uint64_t inclusive = wave_scan<unsigned long long>(v);
   if (lane_id() == 63) s.sums[wave] = inclusive;
@@ -350,6 +354,7 @@ __global__ void __launch_bounds__(kOneThreads) plan_fork_kernel(PoolView p, Page
   const OnePlan plan = plan_one<PageList::kFork>(p, s, parents, children, n, seen);
   const Entry& e = plan.e;
   if (i == 0) w.head[kPlanFaults] = plan.faults;
+  if (i < w.segments * kSegmentWords) w.bits[i] = s.words[i];  // (kOneWords at most)
   __syncthreads();
   if (i >= n || plan.faults) return;
   ForkJob job = {0, 0, 0, e.len};
@@ -461,6 +466,7 @@ __global__ void __launch_bounds__(256) copy_kernel(PoolView p, const int32_t* sr
 }
 
 // Workgroup: one kind of one layer of one fork.  KNOWN: plan_fork_kernel has written the books but for the pages that are shared.
+// Whether a page was free before the call is asked of the survey's bits: the call itself may have taken it since.
 template <bool KNOWN>
 __global__ void __launch_bounds__(256) fork_kernel(PoolView p, PageSpace w, const int32_t* parents, const int32_t* children, FastDiv dkinds) {
   uint32_t i, layer_kind;
@@ -482,8 +488,9 @@ __global__ void __launch_bounds__(256) fork_kernel(PoolView p, PageSpace w, cons
       for (uint32_t j = threadIdx.x; j < whole; j += 256) {
         const uint32_t page = (uint32_t)from[j];
         to[j] = (int32_t)page;
-        if (page < p.num_blocks) atomicAdd(p.refs + page, 1);
-        else fault(p, KVC_FAULT_PAGE);
+        if (page >= p.num_blocks) fault(p, KVC_FAULT_PAGE);
+        else if (w.bits[page / 32] >> page % 32 & 1u) fault(p, KVC_FAULT_LIST);
+        else atomicAdd(p.refs + page, 1);
       }
     }
     if constexpr (!KNOWN) {

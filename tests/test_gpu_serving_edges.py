@@ -162,8 +162,27 @@ def test_append_leaves_out_what_no_request_covers(kvc_lib, wrong, H, D):
 # ---- tables that hold free pages
 
 
+class Books(model.Books):
+    """A fork whose parent holds a free page: of a last page filled in part the list is at fault, a whole one is copied as it is and shared
+    with nobody."""
+
+    def fork(self, parents, children):
+        free = set(self.free_list())
+        lost = [self.tables[p][j] for p in parents for j in range(self.lens[p] // self.block) if self.tables[p][j] in free]
+        if any(self.lens[p] % self.block and self.tables[p][self.lens[p] // self.block] in free for p in parents):
+            self.err |= model.FAULT_LIST
+            return
+        taken = self.free_list()[:sum(self.lens[p] % self.block != 0 for p in parents)]
+        was = list(self.refs)
+        super().fork(parents, children)
+        for page in lost:
+            self.refs[page] = 1 if page in taken else was[page]
+            self.err |= model.FAULT_LIST
+
+
 def books_of(blocks, lens, seed):
     books = filled(8, 6, 4, blocks, lens, seed=seed)
+    books.__class__ = Books
     return books
 
 
@@ -189,3 +208,24 @@ def test_a_grow_into_a_free_page_changes_nothing(kvc_lib, blocks, count):
         books.grow([2, 0], [0, 5])
         assert books.err == 0
         d.check(before)
+
+
+@pytest.mark.parametrize("blocks", [40, 20000])
+@pytest.mark.parametrize("count", [0, -2])
+@pytest.mark.parametrize("what", ["part", "whole"])
+def test_a_fork_of_a_free_page(kvc_lib, blocks, count, what):
+    books = books_of(blocks, [9, 12, 6, 0, 0, 0, 0], blocks + 1)
+    if what == "part":
+        books.refs[books.tables[2][1]] = count
+    else:  # the lowest free page, which the call takes for a child too
+        books.refs[books.tables[0][0]] = books.refs[books.tables[1][1]] = 0
+        books.tables[1][1] = books.free_list()[0]
+        books.refs[books.tables[1][1]] = count
+    d = DevicePool(books, 2, 1, 16)
+    before = d.copy()
+    parents, children = [1, 0, 1, 2], [3, 4, 6, 5]
+    a, b = i32(parents), i32(children)
+    kvc.kvc_pages_fork(d.pool, a.data_ptr(), b.data_ptr(), 4, *d.room())
+    books.fork(parents, children)
+    assert books.err == model.FAULT_LIST and (books.lens[3] == 12) == (what == "whole")
+    d.check(before)
