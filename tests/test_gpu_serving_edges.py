@@ -229,3 +229,37 @@ def test_a_fork_of_a_free_page(kvc_lib, blocks, count, what):
     books.fork(parents, children)
     assert books.err == model.FAULT_LIST and (books.lens[3] == 12) == (what == "whole")
     d.check(before)
+
+
+# ---- weights far below a row's largest
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("G,new,tokens", [(1, 1, 300), (3, 20, 300), (2, 1, 20), (40, 1, 3000)])
+def test_small_weights_count(kvc_lib, dtype, G, new, tokens):
+    """One token outweighs each of the others 2^26 times and has the value 0: what is left is theirs.  Weights are held with a relative
+    error of half a step of the type down to 2^-21 of the largest, and to 2^-32 of it below that."""
+    a = Attend(2, G, 64, dtype, 16, 0, [tokens], [new], seed=3, scale=math.log(2.0))
+    keys, values = a.caches[0][0].flatten(0, 1), a.caches[0][1].flatten(0, 1)
+    positions = torch.arange(tokens)
+    slots = (torch.tensor(a.books.tables[a.rows[0]])[positions // 16] * 16 + positions % 16).cuda()
+    a.q.zero_()
+    a.q[..., 0] = 1.0
+    keys[slots] = 0
+    keys[slots[1:], :, 0] = -26.0
+    values[slots[:1]] = 0
+    values[slots[1:]] = (512.0 + torch.arange(64, device="cuda")).to(a.dtype)
+    a.call()
+    torch.cuda.synchronize()
+    assert int(a.device.err.item()) == 0
+    seen = torch.arange(tokens - new + 1, tokens + 1, dtype=torch.float64)[:, None, None]  # tokens that each query sees
+    others = (seen - 1) * 2.0 ** -26
+    value = values[slots[-1]].double().cpu()[0]
+    want = (others / (1 + others) * value).expand(new, 2 * G, 64)
+    u, e = torch.finfo(a.dtype).eps / 2, 2.0 ** -24
+    size, smallest = 26.0 * math.log(2.0), 2.0 ** -25 if dtype == "f16" else 2.0 ** -134
+    held = (seen - 1) * 2.0 ** -32 * value if dtype == "f16" else 0.0
+    far = (2 * u + 2 * u * u + 2 * e * (68 * size + 4) + (tokens + 16) * e) * want + held + smallest
+    assert bool(((a.out.double().cpu() - want).abs() <= far).all())
+    want_lse = torch.log1p(others)[..., 0].expand(new, 2 * G)
+    assert bool(((a.lse[:-1].double().cpu() - want_lse).abs() <= e * (68 * size + 4) + (tokens + 20) * e).all())
