@@ -1,5 +1,6 @@
 """Serving calls where books, lists and pages are not what a call may rely on, and attention at the ends of its types and addresses."""
 import math
+import random
 
 import pytest
 import torch
@@ -263,3 +264,54 @@ def test_small_weights_count(kvc_lib, dtype, G, new, tokens):
     assert bool(((a.out.double().cpu() - want).abs() <= far).all())
     want_lse = torch.log1p(others)[..., 0].expand(new, 2 * G)
     assert bool(((a.lse[:-1].double().cpu() - want_lse).abs() <= e * (68 * size + 4) + (tokens + 20) * e).all())
+
+
+# ---- caches whose K and V pass 32 bits of offsets
+
+
+@pytest.fixture(scope="module")
+def large():
+    """Memory of a layer whose K and V have 4.6 GB each."""
+    yield torch.full((2 * 4600 << 20,), 0x7E, dtype=torch.uint8, device="cuda")  # (NaN in both types)
+
+
+LARGE = [  # H, G, block, prefix, lens, new
+    (2, 4, 16, 900, [901 + 30 * i for i in range(3)], None),              # one wave along the rows, for both parts
+    (4, 4, 16, 0, [700, 90, 1500], None),
+    (32, 1, 16, 70, [71 + (5 * i) % 60 for i in range(20)], None),        # a wave each for a head of a request
+    (32, 3, 8, 33, [40 + (7 * i) % 90 for i in range(17)], [1 + i % 4 for i in range(17)]),
+    (2, 4, 32, 640, [641 + 7 * i for i in range(40)], None),              # four waves over the prefix
+    (2, 4, 16, 300, [600, 450], [40, 90]),                                # and over the rows' own tokens
+    (8, 8, 16, 100, [320, 260, 140, 290], [200, 150, 0, 170]),            # one sequence a row
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256, 40])
+@pytest.mark.parametrize("case", LARGE, ids=[f"c{i}" for i in range(len(LARGE))])
+def test_every_body_beyond_32_bits(kvc_lib, large, case, D, dtype):
+    """Pages all over 4.6 GB of K and of V, so that neighbours lie on both sides of 2 and 4 GiB: results are those of the same pages side by side."""
+    hz.say(f"[case] large {case} {D} {dtype}")
+    H, G, block, prefix, lens, new = case
+    a = Attend(H, G, D, dtype, block, prefix, lens, new, seed=9)
+    a.call()
+    torch.cuda.synchronize()
+    near, near_lse = a.out.clone(), a.lse.clone()
+    page_bytes = block * H * D * 2
+    blocks = large.numel() // 2 // page_bytes
+    assert blocks * page_bytes > 1 << 32
+    rng = random.Random(D)
+    to = [0, blocks - 1] + [edge // page_bytes + i for edge in (1 << 31, 1 << 32) for i in (-1, 0, 1)]
+    to += rng.sample([page for page in range(1, blocks - 1, 7) if page not in to], a.books.blocks - len(to))
+    rng.shuffle(to)
+    cache = large[:2 * blocks * page_bytes].view(a.dtype).unflatten(0, (2, blocks, block, H, D))
+    cache[:, torch.tensor(to, device="cuda")] = a.caches[0]
+    a.device.tables.copy_(i32([[to[page] if page >= 0 else -1 for page in t] for t in a.books.tables]))
+    a.device.ptrs.fill_(large.data_ptr())
+    a.device.pool.num_blocks = blocks
+    a.out_store.fill_(7.0)
+    a.lse.fill_(7.0)
+    a.call()
+    torch.cuda.synchronize()
+    assert int(a.device.err.item()) == 0
+    assert torch.equal(a.out, near) and torch.equal(a.lse, near_lse)
