@@ -526,6 +526,9 @@ kvc_status kvc_tiling_costs(const kvc_layout* layout, const void* kv, kvc_stride
  * Pages are taken lowest id first, in the order of the list that a call is
  * given, so the same books always become the same books.
  *
+ * A call whose work is more than a launch can hold (2^24 workgroups: 105 000 pages of 80
+ * layers copied at a time) is KVC_ERR_UNSUPPORTED.
+ *
  * Faults that only the device can see are ORed into *d_err (KVC_FAULT_*).  A
  * fork or grow whose list is at fault (KVC_FAULT_LIST) or lacks room
  * (KVC_FAULT_NO_ROOM) changes nothing at all; a count of holders below 0 is

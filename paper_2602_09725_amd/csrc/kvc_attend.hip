@@ -1040,9 +1040,16 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   if (at == 0 && p.lse) p.lse[line] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
+// Workgroups of the attention's launch.
+uint64_t attend_groups(const AttendParams& p) { return ((uint64_t)p.part[0].units + 7) / 8 * 8 + ((uint64_t)p.part[1].units + 7) / 8 * 8; }
+
+// Rows that share a workgroup of the join.  Few rows of many pieces take a workgroup each; many rows share one, a row having as many threads as it has
+// vectors of four sums (up to 128 elements, so that a workgroup's life, which is that of its loads one after the other, is spent on eight rows).
+constexpr uint32_t join_lines(uint32_t D) { return D > 128 ? 4 : 8; }
+
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
-  const uint32_t groups = (p.part[0].units + 7) / 8 * 8 + (p.part[1].units + 7) / 8 * 8;
+  const uint32_t groups = (uint32_t)attend_groups(p);
   const bool big = (uint64_t)p.pool.num_blocks * p.pool.page_bytes > 0xffff0000u;  // (offsets of what is not there lie above)
   // Few rows have a kernel of the one body alone, with fewer registers (4 rows over 1000 tokens 14.6 -> 13.9 us, 30 rows of 32 heads over 3000 tokens 40.8 ->
   // 39.2); caches beyond 32 bits go without.
@@ -1052,9 +1059,7 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   if (groups && !big && !ones) hipLaunchKernelGGL((attend_kernel<DT, DP, false, false>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   if (p.pieces != 1) {  // (no piece at all: every row is empty)
-    // Few rows of many pieces take a workgroup each; many rows share one, a row having as many threads as it has vectors of four sums (up to 128
-    // elements, so that a workgroup's life, which is that of its loads one after the other, is spent on eight rows).
-    constexpr uint32_t kLines = DP > 128 ? 4 : 8;
+    constexpr uint32_t kLines = join_lines(DP);
     const uint32_t lines = p.batch.n_new * p.H * p.G;
     if (lines <= 2048)
       hipLaunchKernelGGL((join_kernel<DT, DP, 1>), dim3(lines), dim3(256), p.pieces * 4, stream, p);
@@ -1123,7 +1128,8 @@ kvc_status plan_attend(AttendParams& p) {
     a.dtokens = make_fastdiv(a.tokens);
     p.pieces += a.splits;
   }
-  if ((uint64_t)p.part[0].units + p.part[1].units > 0x7ffffff0u) return KVC_ERR_UNSUPPORTED;
+  const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = join_lines(p.D);
+  if (attend_groups(p) > kMostGroups || (p.pieces != 1 && (lines + each - 1) / each > kMostGroups)) return KVC_ERR_UNSUPPORTED;
   return KVC_OK;
 }
 

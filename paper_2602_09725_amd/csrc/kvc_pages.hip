@@ -771,7 +771,7 @@ kvc_status launch_survey(const PoolView& pool, const PageSpace& w, PageList list
 kvc_status launch_fork(const PoolView& pool, const PageSpace& w, const int32_t* parents, const int32_t* children, uint32_t n,
                        hipStream_t stream) {
   const uint32_t kinds = 2 * pool.L;
-  if ((uint64_t)n * kinds >> 31) return KVC_ERR_UNSUPPORTED;
+  if ((uint64_t)n * kinds > kMostGroups) return KVC_ERR_UNSUPPORTED;
   if (one_group(pool, n)) {
     hipLaunchKernelGGL(plan_fork_kernel, dim3(1), dim3(kOneThreads), (pool.n_rows + 31) / 32 * 4, stream, pool, w, parents, children, n);
     if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
@@ -797,6 +797,7 @@ kvc_status launch_grow(const PoolView& pool, const PageSpace& w, const int32_t* 
 }
 
 kvc_status launch_free(const PoolView& pool, const int32_t* rows, uint32_t n, hipStream_t stream) {
+  if ((n + 3) / 4 > kMostGroups) return KVC_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(free_kernel, dim3((n + 3) / 4), dim3(256), 0, stream, pool, rows, n);
   return launched();
 }
@@ -821,7 +822,7 @@ kvc_status launch_compact(const PoolView& pool, const PageSpace& w, int32_t* map
 
 kvc_status launch_copy_pages(const PoolView& pool, const int32_t* src, const int32_t* dst, uint32_t n, hipStream_t stream) {
   const uint64_t pieces = (pool.page_bytes + kPiece - 1) / kPiece;
-  if (2 * pool.L * pieces >> 31 || (uint64_t)n * (2 * pool.L * pieces) >> 31) return KVC_ERR_UNSUPPORTED;
+  if (2 * pool.L * pieces > kMostGroups || (uint64_t)n * (2 * pool.L * pieces) > kMostGroups) return KVC_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(copy_kernel, dim3((uint32_t)(n * 2 * pool.L * pieces)), dim3(256), 0, stream, pool, src, dst, make_fastdiv((uint32_t)pieces),
                      make_fastdiv(2 * pool.L));
   return launched();
@@ -831,7 +832,7 @@ kvc_status launch_append(const AppendParams& p, hipStream_t stream) {
   const uint64_t vectors = (uint64_t)p.batch.n_new * 2 * p.atoms;
   const bool many = vectors >= 256 * 4 * 512;
   const uint64_t groups = (vectors + (many ? 1023 : 255)) / (many ? 1024 : 256);
-  if (groups >> 31) return KVC_ERR_UNSUPPORTED;
+  if (groups > kMostGroups) return KVC_ERR_UNSUPPORTED;
   if (many) hipLaunchKernelGGL(append_kernel<4>, dim3((uint32_t)groups), dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(append_kernel<1>, dim3((uint32_t)groups), dim3(256), 0, stream, p);
   return launched();

@@ -7,6 +7,9 @@
 
 namespace kvc {
 
+// Workgroups of 256 threads that a launch can have: fewer than 2^32 threads.
+constexpr uint64_t kMostGroups = (1ull << 24) - 1;
+
 // The pool as the kernels see it.
 struct PoolView {
   void* const* layers;
