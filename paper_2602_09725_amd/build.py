@@ -28,9 +28,8 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
 ]
-# Flags that a source is compiled without or with: attention's scores may be anything that a cache holds.
+# Flags that a source is compiled without: attention's scores may be anything that a cache holds.
 WITHOUT = {"kvc_attend.hip": ["-fno-honor-nans"]}
-WITH = {}
 
 
 def source_id(extra_flags=()):
@@ -41,7 +40,7 @@ def source_id(extra_flags=()):
         h.update(os.path.basename(f).encode() + b"\0")
         with open(f, "rb") as fh:
             h.update(fh.read())
-    h.update("\0".join([*FLAGS, *extra_flags, repr(sorted(WITHOUT.items())), repr(sorted(WITH.items()))]).encode())
+    h.update("\0".join([*FLAGS, *extra_flags, repr(sorted(WITHOUT.items()))]).encode())
     return h.hexdigest()[:16]
 
 
@@ -65,7 +64,7 @@ def build(out=LIB, extra_flags=()):
     with tempfile.TemporaryDirectory() as objects:
         def compiled(source):
             obj = os.path.join(objects, source + ".o")
-            flags = [f for f in FLAGS if f not in WITHOUT.get(source, ())] + WITH.get(source, [])
+            flags = [f for f in FLAGS if f not in WITHOUT.get(source, ())]
             subprocess.run(["hipcc", *flags, *common, "-c", os.path.join(CSRC, source), "-o", obj], check=True)
             return obj
 

@@ -175,17 +175,15 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   return w;
 }
 
-// Sizes of a body: R waves side by side along the rows; tokens of a tile; LDS of a tile's K (and V).
+// Sizes of a body: R waves side by side along the rows; tokens of a tile; vectors of a tile's K (and V).
 template <int DP, int R>
 struct Shape {
   static constexpr int CH = DP / 8;                          // vectors of a token's row
   static constexpr int TT = R == 1 ? 32 : 64;                // tokens of a tile
   static constexpr int GROUPS = 4 / R;                       // waves along the tokens, each with tiles of its own
-  static constexpr int BUFFERS = R == 1 ? 1 : 2;
   static constexpr int LOADS = TT * CH / (R * 64);           // vectors of K (and of V) that a thread loads
   static constexpr int STEP = R * 64 / CH;                   // tokens from one of them to the next
   static constexpr int TILE = TT * CH;                       // vectors of a tile
-  static constexpr int LDS = GROUPS * BUFFERS * 2 * TILE;    // vectors in all
 };
 
 // LDS of a workgroup: four arrays of this many vectors, so that the compiler sees which reads a load does not touch.  Four waves

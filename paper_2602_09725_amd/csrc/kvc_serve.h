@@ -92,7 +92,7 @@ struct AttendParams {
   uint32_t own_from;    // first token of the rows' own part: the prefix's end, or 0 where each row's tokens are one sequence
   FastDiv dG, dheads;   // dheads: query heads
   AttendPart part[2];   // prefix, own
-  float scale, scale_log2;
+  float scale_log2;
   float slack;          // products that exceed the running maximum by no more than this leave it as it is
   uint32_t pieces;      // results of a row that are joined afterwards; 1: the row is written at once; 0: nobody sees anything
   float *sums, *tops;   // [pieces][n_new][heads][D] unnormalized sums, [pieces][n_new][heads][2] {maximum (log2), sum of weights}

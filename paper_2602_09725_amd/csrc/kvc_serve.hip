@@ -109,7 +109,6 @@ kvc_status plan_of(const kvc_pool* pool, const kvc_batch* batch, const kvc_atten
   p->prefix_row = (uint32_t)a->prefix_row;
   p->most_tokens = (uint32_t)a->most_tokens;
   p->dG = make_fastdiv(p->G);
-  p->scale = a->scale;
   p->scale_log2 = (float)((double)a->scale * 1.4426950408889634);
   return batch->n_new == 0 ? KVC_OK : plan_attend(*p);
 }
