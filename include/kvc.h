@@ -640,10 +640,12 @@ kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_
  *   out = sum_j softmax_j(scale * q.k_j) v_j,   lse = log sum_j exp(scale * q.k_j)
  * and out = 0, lse = -inf where it sees none.  Query head h reads KV head
  * h / (num_q_heads / H).  The rows share their first prefix_tokens positions, which are
- * read through row prefix_row's table: once for all queries, or, where many queries meet a
- * short prefix, once for each request's.
+ * read through row prefix_row's table: once for each 128 rows of queries (a token and one of the num_q_heads / H
+ * query heads of a KV head; 32 of them if there are no more), or, where many queries meet a short prefix, once
+ * for each 128 rows of a request's.
  * Arithmetic: products of 16-bit values summed in fp32, softmax and sums in fp32,
- * probabilities rounded to the cache's type before they meet V, one rounding at the end. */
+ * probabilities rounded to the cache's type before they meet V (those of fp16 down to 2^-32 of a
+ * row's largest count), one rounding at the end. */
 typedef struct {
   uint32_t struct_size; /* sizeof(kvc_attention)                                */
   uint32_t abi_version; /* KVC_ABI_VERSION                                      */

@@ -399,7 +399,8 @@ __device__ __forceinline__ void move_base(const AttendParams& p, State<DP>& x, f
   }
 }
 
-// Weights of a tile, rounded to the type, from its products; the state is moved to them.
+// Weights of a tile, rounded to the type, from its products; the state is moved to them.  (The matrix unit takes 16 bits: half a step a weight, as the inputs
+// themselves have.  Their sum is of the weights before that: its logarithm is a result in fp32, which rounded weights would leave with 2^-12 or 2^-9.)
 template <int DT, int DP, int NS>
 __device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, const f32x16 (&s)[NS], u32x4 (&w)[NS][2]) {
   float top = kNone;
@@ -1070,9 +1071,9 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 }  // namespace
 
 // Whether the prefix is read anew for each request.  It costs the products of about 64 rows of a block that a request does not fill, over the
-// prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s.  (Of eight to twenty blocks there are too
-// few: 15 tokens of 64 heads over 265 gain 12 %, 60 tokens of 16 heads over 446 lose 7 %; from 39 on the sequences were 25-40 % faster, but for one case of 9
-// % slower.)
+// prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s, and the join's launch.  (Calls of 2 or 8
+// requests over 60 to 500 tokens, 16 to 64 query heads: from 32 blocks of 128 rows on the sequences are 34 % faster to 13 % slower, the median 6 % faster; of 8
+// to 32 blocks, where most of the gain is the launch, 25 % faster to 6 % slower, 4 %: no border shows, and these keep the pieces.)
 bool one_sequence(const AttendParams& p) {
   const uint64_t rows = (uint64_t)p.batch.n_new * p.G;
   if (p.prefix == 0 || p.most_tokens == p.prefix || (uint64_t)p.batch.most_new * p.G <= 32) return false;
@@ -1096,11 +1097,11 @@ kvc_status plan_attend(AttendParams& p) {
     a.drows = a.dsplits = a.drequests = make_fastdiv(1);
     if (tokens == 0) continue;
     if (whole >> 31) return KVC_ERR_UNSUPPORTED;
-    // One workgroup a CU where a piece is short (of 32K tokens and 32 rows 32 or 64 pieces of 8 heads 51 or 59 us), two of them where it
-    // is long (64 rows of queries, 256 of a head: of 64K tokens 16 or 32 pieces 125 or 120 us; of 32K, where the rows' own 500 tokens each take the
-    // second workgroup's place, 66 or 76); where more than two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms
+    // One workgroup a CU where a piece is short (32 query heads of 8 KV heads, one or two workgroups: 8 requests over 32K tokens 34 or 39 us, over 64K 60 or
+    // 65), two of them where it is long (64 requests over 64K 123 or 112 us; over 32K 73 or 69, but where the rows' own 500 tokens each take the
+    // second workgroup's place 83 or 86); where more than two a CU wait, in halves if the last round would be mostly empty (79 blocks of 8 heads 1.51 ms
     // instead of 1.75).
-    // Of a row's own tokens four waves side by side take pieces of 512 (19 requests of 56 heads with 2000 tokens each 55 or 42 us).
+    // Of a row's own tokens four waves side by side take pieces of 512 (19 requests of 56 heads with up to 2000 tokens each 55 or 47 us).
     const uint64_t lengthy = i == 0 && p.most_tokens > p.prefix ? 2048 : a.waves == 4 ? 256 : 1024;
     uint64_t splits = whole <= chip && tokens * whole >= lengthy * chip ? chip / whole : whole <= 256 ? 256 / whole : 1;
     if (whole > chip && tokens >= 4096 && 20 * ((whole + chip - 1) / chip) * chip > 23 * whole) splits = 2;
@@ -1114,8 +1115,8 @@ kvc_status plan_attend(AttendParams& p) {
     a.tokens = (uint32_t)each;
     a.units = (uint32_t)(whole * splits);
     // A wave each has a unit of few tokens where there are many: a workgroup's life is mostly that of memory's answers one after the other, and it has four
-    // at a time so (91 requests of 32 heads with 6 tokens 67 -> 41 us, 128 of 8 heads with 60 or 250: 37.8 -> 30.4, 41.7 -> 35.2, 32 with 20: 21.7 -> 20.8;
-    // 64 with 500 beside a prefix of 32K, from memory, 77 -> 81, and with 1000 48.8 -> 53.1, so these keep a workgroup).
+    // at a time so (over a prefix of 1000: 91 requests of 32 heads with up to 6 tokens 56 -> 30 us, 128 of 8 heads with up to 60 or 250: 36 -> 32, 42 -> 36, 32
+    // with 20: 23.6 -> 22.6; 64 with up to 500 beside a prefix of 32K 81 -> 85, and with 1000 46 -> 53, so these keep a workgroup).
     if (i == 1 && a.waves == 1 && each <= 256 && 2 * whole * splits >= chip) {
       a.lone = a.units;
       a.units = (a.units + 3) / 4;

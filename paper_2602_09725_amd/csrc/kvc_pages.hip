@@ -755,8 +755,8 @@ kvc_status launched() { return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ER
 namespace {
 
 // Whether one workgroup looks after a call's books: of pools of kOnePages pages, and lists of an entry a thread.  (One layer, lists of 4 to 1024
-// entries, pools of 500 to 16384 pages: a grow 4.1-5.5 us, by many workgroups 6.6-11.4; a fork and a free 10.4-12.7, 10.9-14.7; a compact that moves
-// nothing 8.9-13.3, 11.4-15.6.)
+// entries, pools of 500 to 16384 pages, kernels: a grow 4.4-7.2 us, by many workgroups 12-18; a fork 8.1-10.2, 7.8-13.0; a compact of few pages 7.0-15.4,
+// 10-23.)
 bool one_group(const PoolView& pool, uint32_t n) { return pool.num_blocks <= kOnePages && n <= kOneThreads; }
 
 kvc_status launch_survey(const PoolView& pool, const PageSpace& w, PageList list, const int32_t* a, const int32_t* b, uint32_t n,
