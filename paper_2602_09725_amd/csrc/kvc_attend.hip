@@ -53,15 +53,6 @@ __device__ __forceinline__ float half_sum(float v) {
 
 constexpr float kNone = -__builtin_inff();
 
-// Weights are held 2^kLift times as large as their base says: 16 bits of fp16 hold numbers down to 2^-24, and what lies below is lost to the values'
-// sum.  With weights of up to 2^8 (see slack) this is as high as they can go, and keeps those down to 2^-32 of the base's.
-template <int DT>
-constexpr float kLift = DT == KVC_F16 ? 7.0f : 0.0f;
-
-// What is subtracted from a scaled product before exp2, of a row with base m.
-template <int DT>
-__device__ __forceinline__ float shift_of(float m, float scale_log2) { return m == kNone ? 0.0f : m * scale_log2 - kLift<DT>; }
-
 // exp2(a - b) where a is -inf if b is: 0 then.
 __device__ __forceinline__ float weight(float a, float b) { return a == kNone ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
 
@@ -384,12 +375,13 @@ __device__ __forceinline__ void mask(const AttendParams& p, const Unit& u, uint3
 }
 
 // Moves the state's base if a product exceeds it by too much; top: the largest of the lane's.  (The number subtracted need not be the
-// maximum: as long as no weight exceeds 2^8 (2^15 with kLift), sums and types hold them as well.)
+// maximum: as long as no weight exceeds 2^8, or 2^15 of fp16, sums and types hold them as well.  fp16 holds numbers down to 2^-24, and a weight below
+// that is lost to the values' sum: so its base lies 2^7 below the product that moves it, and weights down to 2^-32 of the largest count.)
 template <int DP>
 __device__ __forceinline__ void move_base(const AttendParams& p, State<DP>& x, float top) {
   top = half_max(top);
   if (__any(top > x.m + p.slack)) {
-    const float now = fmaxf(x.m, top), keep = weight(x.m * p.scale_log2, now * p.scale_log2);
+    const float now = fmaxf(x.m, top - p.lift), keep = weight(x.m * p.scale_log2, now * p.scale_log2);
     x.m = now;
     x.l *= keep;
 #pragma unroll
@@ -409,7 +401,7 @@ __device__ __forceinline__ void weights(const AttendParams& p, State<DP>& x, con
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
   move_base<DP>(p, x, top);
-  const float shift = shift_of<DT>(x.m, p.scale_log2);
+  const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
 #pragma unroll
   for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -506,7 +498,7 @@ __device__ __forceinline__ void take_tokens(const AttendParams& p, State<DP>& x,
   u32x4 w[2], f[A + 1];
 #pragma unroll
   for (int e = 0; e < A; ++e) f[e] = first[e];
-  const float shift = shift_of<DT>(x.m, p.scale_log2);
+  const float shift = x.m == kNone ? 0.0f : x.m * p.scale_log2;
 #pragma unroll
   for (int e = 0; e < KK; ++e) {
     f[(e + A) % (A + 1)] = e + A < KK ? key_at<DP>(k, e + A) : values_at<DP / 8>(v, (e + A - KK) / DD, (e + A - KK) % DD);
@@ -700,7 +692,7 @@ __device__ __forceinline__ void rows_see(Tops& tops, uint32_t& most, uint32_t& l
 }
 
 // A wave's 32 rows of sums into LDS, in vectors of four, and their bases and sums of weights.
-template <int DT, int DP>
+template <int DP>
 __device__ __forceinline__ void put_sums(const AttendParams& p, const State<DP>& x, f32x4 KVC_LDS* sums, float* m, float* l) {
   constexpr uint32_t QD = DP / 4;
   const uint32_t lane = threadIdx.x & 63u, col = lane & 31u, half = lane >> 5;
@@ -713,7 +705,7 @@ __device__ __forceinline__ void put_sums(const AttendParams& p, const State<DP>&
     }
   const float total = half_sum(x.l);
   if (half == 0) {
-    m[col] = x.m != kNone || total != 0.0f ? shift_of<DT>(x.m, p.scale_log2) : kNone;  // (a row that saw NaN alone is not empty)
+    m[col] = x.m != kNone ? x.m * p.scale_log2 : total == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
     l[col] = total;
   }
 }
@@ -857,7 +849,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   if constexpr (LONE) wait_reads();
   else __syncthreads();
   f32x4 KVC_LDS* const mine = (f32x4 KVC_LDS*)lds.of(wave_uniform(wave));
-  put_sums<DT, DP>(p, x, mine, tops.m[wave], tops.l[wave]);
+  put_sums<DP>(p, x, mine, tops.m[wave], tops.l[wave]);
   if constexpr (LONE) wait_reads();
   else __syncthreads();
   constexpr uint32_t QD = DP / 4;                         // vectors of four sums of a row
@@ -1084,6 +1076,8 @@ kvc_status plan_attend(AttendParams& p) {
   p.pieces = 0;
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = 8.0f / p.scale_log2 < 1e30f ? 8.0f / p.scale_log2 : 1e30f;
+  p.lift = p.dtype == KVC_F16 ? p.slack * 0.875f : 0.0f;
+  p.slack += p.lift;
   const uint64_t chip = p.D <= 128 ? 512 : 256;  // workgroups that run at a time
   p.own_from = one_sequence(p) ? 0 : p.prefix;
   for (int i = 0; i < 2; ++i) {

@@ -93,7 +93,8 @@ struct AttendParams {
   FastDiv dG, dheads;   // dheads: query heads
   AttendPart part[2];   // prefix, own
   float scale_log2;
-  float slack;          // products that exceed the running maximum by no more than this leave it as it is
+  float slack;          // products that exceed a row's base by no more than this leave it as it is
+  float lift;           // a base that is moved comes to lie this much below the product that moved it
   uint32_t pieces;      // results of a row that are joined afterwards; 1: the row is written at once; 0: nobody sees anything
   float *sums, *tops;   // [pieces][n_new][heads][D] unnormalized sums, [pieces][n_new][heads][2] {maximum (log2), sum of weights}
 };
