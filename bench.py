@@ -28,7 +28,7 @@ HBM_PEAK_GBPS = 8000.0  # MI355X HBM3E, published peak
 # this command, not in this one, and are keyed by the identifier the library carries (a hash of its sources,
 # header and compiler flags): for any other build the figure is reported as null.
 MEASURED_TRAFFIC = {
-    "d45a06e0c4f7cb1c": {"pack": 6582100685, "restore": 6513976115},
+    "6a57455e2f272ba0": {"pack": 6582058803, "restore": 6513971507},
 }
 TRAFFIC_PROFILE = "profiles/pack_restore_llama3_8b_32k_paged.txt"
 
