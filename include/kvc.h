@@ -541,11 +541,27 @@ enum {
   KVC_FAULT_NO_ROOM = 4  /* fewer pages are free than the call needs, or a row's table is full            */
 };
 
+/* A pool may hold its tokens in 4 bits instead of 16: dtype is then KVC_F16 or KVC_BF16, the type of tokens as they come and
+ * go, with KVC_HELD_Q4.  Every serving call takes such a pool; a prefix is restored into a pool of 16 bits and moved by
+ * kvc_pages_convert.  A token's head (the D elements of a kind, layer, token and head, as KVC_Q_PER_TOKEN) is held as
+ *   mn = min + 0.0f, step = (max - mn) / 15, scale = step rounded up to the type, inv = 1 / scale (0 if scale is 0),
+ *   code = min(rint((x - mn) * inv), 15)
+ * in fp32, each step rounded, and stands for x_hat = fma(code, scale, mn), which is within half a scale of x.  mn is one of the
+ * values, so the type has it; a scale rounded up loses no range (2^-10 or 2^-7 of a step at most).  Read back, x_hat
+ * is rounded to nearest even in the type, and held to its largest number.  Values must be finite, and max - min 0 or >= 2^-100; a head
+ * with a value that is not finite (or a max - min that is not, in fp32) reads back as NaN, all of it.
+ * A page of one layer and kind has kvc_page_bytes() = block_size * H * (D / 2 + 4) bytes, in 32-bit words
+ *   codes [H][block_size / 4][D / 8][4]: word w of a token and head has elements 8 w .. 8 w + 7, element 8 w + 2 i in bits
+ *         4 i .. 4 i + 3, element 8 w + 2 i + 1 in bits 16 + 4 i .. 19 + 4 i; four tokens of a block lie side by side
+ *   pairs [H][block_size]: scale in the low half, mn in the high one
+ * and a layer's cache is [2][num_blocks] of them.  block_size a multiple of 4 and D at most 256, else KVC_ERR_UNSUPPORTED. */
+#define KVC_HELD_Q4 0x10
+
 typedef struct {
   uint32_t struct_size; /* sizeof(kvc_pool)                                     */
   uint32_t abi_version; /* KVC_ABI_VERSION                                      */
   int32_t num_layers, num_kv_heads, head_dim; /* head_dim a multiple of 8, else KVC_ERR_UNSUPPORTED */
-  int32_t dtype;        /* kvc_dtype                                            */
+  int32_t dtype;        /* kvc_dtype, with KVC_HELD_Q4 or not                   */
   int64_t num_blocks;   /* pages; num_blocks * block_size below 2^32, else KVC_ERR_UNSUPPORTED      */
   int64_t n_rows;       /* rows of the table, below 2^18, else KVC_ERR_UNSUPPORTED                  */
   int32_t block_size;   /* tokens of a page, any number >= 1                    */
@@ -554,12 +570,15 @@ typedef struct {
   int32_t* d_tables;    /* DEVICE int32 [n_rows][table_len]                     */
   int32_t* d_lens;      /* DEVICE int32 [n_rows]: tokens of each row            */
   int32_t* d_refs;      /* DEVICE int32 [num_blocks]: holders of each page; may be NULL for kvc_pages_copy,
-                           kvc_append_paged and kvc_attend_paged                */
+                           kvc_pages_convert, kvc_append_paged, kvc_read_paged and kvc_attend_paged */
   uint32_t* d_err;      /* DEVICE, may be NULL                                  */
 } kvc_pool;
 
 /* Checks a pool on the host (sizes, NULL pointers, alignment). */
 kvc_status kvc_pool_validate(const kvc_pool* pool);
+
+/* Bytes of a page of one layer and kind; 0 on a bad argument. */
+size_t kvc_page_bytes(const kvc_pool* pool);
 
 /* Copies pages: page d_src[i] -> page d_dst[i] in all layers, K and V.
  *   d_src, d_dst  DEVICE in: int32 [n].  No page may be copied to twice, nor be
@@ -574,7 +593,7 @@ size_t kvc_pages_workspace(const kvc_pool* pool);
 /* Forks rows: row d_children[i] becomes a copy of row d_parents[i].  Whole pages
  * are shared (their counts go up by one), the tokens of the parent's last page, where
  * it is filled in part, are copied to a page that is taken for the child, in all
- * layers; no token that either writes from then on is seen by the other.
+ * layers (a page in 4 bits is copied whole); no token that either writes from then on is seen by the other.
  *   d_parents, d_children  DEVICE in: int32 [n], n <= n_rows.  A child's length must be 0;
  *                          a parent may have many children, a child may not be a
  *                          parent or a child twice in one call
@@ -583,6 +602,14 @@ size_t kvc_pages_workspace(const kvc_pool* pool);
  * and free is a list at fault; one outside the pool leaves the child's page as it was (KVC_FAULT_PAGE). */
 kvc_status kvc_pages_fork(const kvc_pool* pool, const int32_t* d_parents, const int32_t* d_children, int64_t n,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Moves pages between a pool of 16 bits and one of 4: page d_src[i] of `from` is quantized into page d_dst[i] of `to`, or read back into
+ * it, all of its slots in all layers, K and V.  The pools are alike in layers, heads, head_dim, block_size and type, and one of them is of KVC_HELD_Q4
+ * (else KVC_ERR_INVALID_ARG).
+ *   d_src, d_dst  DEVICE in: int32 [n].  No page may be written twice
+ * A pair with an id outside its pool is left out (KVC_FAULT_PAGE to that pool).  The books are not touched: a page that has been moved
+ * has the same place in a row's table. */
+kvc_status kvc_pages_convert(const kvc_pool* from, const kvc_pool* to, const int32_t* d_src, const int32_t* d_dst, int64_t n, void* stream);
 
 /* Makes rows longer: lens[d_rows[i]] += d_counts[i], and takes the pages that
  * the row's table then lacks.  Their contents are what was there before.
@@ -635,6 +662,16 @@ typedef struct {
 kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_t layer, const void* k, const void* v,
                             int64_t token_stride, void* stream);
 
+/* Reads keys and values of rows back from one layer: the tokens of the batch, as kvc_append_paged writes them, or, with d_first, n_r
+ * tokens of request r's row from position d_first[r] on.
+ *   d_first       DEVICE in: int32 [n_requests], may be NULL
+ *   k, v          DEVICE out: [n_new][H][D], 16-byte aligned, apart from each other
+ *   token_stride  elements from a token to the next, of k and of v; a multiple of 8, at least H * D
+ * A token whose page is outside the pool (KVC_FAULT_PAGE), whose position is not in its row, or that no request covers (KVC_FAULT_LIST), is
+ * left as it was. */
+kvc_status kvc_read_paged(const kvc_pool* pool, const kvc_batch* batch, const int32_t* d_first, int32_t layer, void* k, void* v,
+                          int64_t token_stride, void* stream);
+
 /* Attention of the batch's new tokens over their rows, in one layer.  The query
  * of a token at position p sees the positions 0 .. p of its row (p < 0: none):
  *   out = sum_j softmax_j(scale * q.k_j) v_j,   lse = log sum_j exp(scale * q.k_j)
@@ -645,7 +682,8 @@ kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_
  * for each 128 rows of a request's.
  * Arithmetic: products of 16-bit values summed in fp32, softmax and sums in fp32,
  * probabilities rounded to the cache's type before they meet V (those of fp16 down to 2^-32 of a
- * row's largest count), one rounding at the end. */
+ * row's largest count), one rounding at the end.  Of a pool of KVC_HELD_Q4 the keys and values are x_hat before it is rounded to the
+ * type; weights times a token's scale are rounded to bf16, or held in twice its bits for fp16. */
 typedef struct {
   uint32_t struct_size; /* sizeof(kvc_attention)                                */
   uint32_t abi_version; /* KVC_ABI_VERSION                                      */

@@ -18,7 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvc.so")
 SOURCES = ["kvc_api.hip", "kvc_restore.hip", "kvc_pack.hip", "kvc_score.hip", "kvc_search.hip", "kvc_probe.hip", "kvc_serve.hip",
-           "kvc_pages.hip", "kvc_attend.hip"]
+           "kvc_pages.hip", "kvc_held.hip", "kvc_attend.hip", "kvc_attend_held.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -28,8 +28,8 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
 ]
-# Flags that a source is compiled without: attention's scores may be anything that a cache holds.
-WITHOUT = {"kvc_attend.hip": ["-fno-honor-nans"]}
+# Flags that a source is compiled without: attention's scores may be anything that a cache holds, and what is held in 4 bits may stand for NaN.
+WITHOUT = {name: ["-fno-honor-nans"] for name in ("kvc_attend.hip", "kvc_attend_held.hip", "kvc_held.hip")}
 
 
 def source_id(extra_flags=()):

@@ -14,6 +14,7 @@
 // transposing reads.
 #include <hip/hip_runtime.h>
 
+#include "kvc_attend.h"
 #include "kvc_device.h"
 #include "kvc_serve.h"
 
@@ -35,10 +36,6 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ void fault(const AttendParams& p, uint32_t bits) {
-  if (p.pool.err && bits) atomicOr(p.pool.err, bits);
-}
-
 // Values of a lane and of its partner 32 lanes away.
 __device__ __forceinline__ float half_max(float v) {
   const uint32_t u = __builtin_bit_cast(uint32_t, v);
@@ -49,90 +46,6 @@ __device__ __forceinline__ float half_sum(float v) {
   const uint32_t u = __builtin_bit_cast(uint32_t, v);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-
-constexpr float kNone = -__builtin_inff();
-
-// exp2(a - b) where a is -inf if b is: 0 then.
-__device__ __forceinline__ float weight(float a, float b) { return a == kNone ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
-
-// ---- who sees what --------------------------------------------------------------------------------------------------------
-
-struct Request {
-  uint32_t row, first, n, len;  // row of the table; first new token, new tokens; tokens (the true length)
-  uint32_t faults;
-};
-
-// All of a request; what is out of range is told and made harmless.
-__device__ __forceinline__ Request request_at(const AttendParams& p, uint32_t r) {
-  Request q;
-  q.faults = 0;
-  q.first = r;
-  q.n = 1;
-  q.row = p.batch.rows ? (uint32_t)p.batch.rows[r] : r;
-  if (p.batch.starts) {
-    const uint32_t a = (uint32_t)p.batch.starts[r], b = (uint32_t)p.batch.starts[r + 1];
-    q.first = a < p.batch.n_new ? a : p.batch.n_new;
-    const uint32_t end = b < p.batch.n_new ? b : p.batch.n_new;
-    q.n = end > q.first ? end - q.first : 0;
-    if (a > b || b > p.batch.n_new || q.n > p.batch.most_new) q.faults |= KVC_FAULT_LIST;
-    if ((r == 0 && a != 0) || (r + 1 == p.batch.n_requests && b != p.batch.n_new)) q.faults |= KVC_FAULT_LIST;
-  }
-  const bool known = q.row < p.pool.n_rows;
-  q.row = known ? q.row : 0;
-  q.len = (uint32_t)p.pool.lens[q.row];
-  if (!known || q.len > p.most_tokens) q.faults |= KVC_FAULT_LIST;
-  if (!known || q.len > 0x7fffffffu) q.len = 0;
-  return q;
-}
-
-// New tokens of a request that have a result.
-__device__ __forceinline__ uint32_t covered(const AttendParams& p, const Request& q) { return min(q.n, p.batch.most_new); }
-
-// Positions that new token t of a request sees: those below this.  (A token whose request does not cover it sees none.)
-__device__ __forceinline__ uint32_t limit_of(const AttendParams& p, const Request& q, uint32_t t) {
-  if (t - q.first >= covered(p, q)) return 0;
-  const int64_t seen = (int64_t)q.len - q.n + (t - q.first) + 1;
-  return seen < 0 ? 0 : seen < (int64_t)p.most_tokens ? (uint32_t)seen : p.most_tokens;
-}
-
-// Request of new token t.
-__device__ __forceinline__ uint32_t request_of(const BatchView& b, uint32_t t) {
-  if (!b.starts) return t;
-  uint32_t low = 0, high = b.n_requests;
-  while (low + 1 < high) {
-    const uint32_t mid = (low + high) / 2;
-    if ((uint32_t)b.starts[mid] <= t) low = mid;
-    else high = mid;
-  }
-  return low;
-}
-
-// Writes the result of new tokens [from, to) for a KV head's query heads: that of rows that see nothing.  self: one of so many threads.
-__device__ __forceinline__ void write_none(const AttendParams& p, uint32_t from, uint32_t to, uint32_t head, uint32_t self, uint32_t threads) {
-  const uint32_t rows = from < to ? (to - from) * p.G : 0;
-  for (uint32_t row = self; row < rows; row += threads) {
-    uint32_t t, g;
-    fd_divmod(p.dG, row, t, g);
-    const uint32_t token = from + t, h = head * p.G + g;
-    uint16_t* const out = p.out + (int64_t)token * p.o_token + (int64_t)h * p.o_head;
-    for (uint32_t at = 0; at < p.D; at += 8) *(KVC_GLOBAL u32x4*)(out + at) = u32x4{0, 0, 0, 0};
-    if (p.lse) p.lse[(uint64_t)token * (p.H * p.G) + h] = kNone;
-  }
-}
-
-// The new tokens around a request's that no request covers: its own beyond the bound, and those before the first request's and after the last one's.
-__device__ __forceinline__ void write_uncovered(const AttendParams& p, const Request& q, uint32_t request, uint32_t head, uint32_t self, uint32_t threads) {
-  const uint32_t end = q.first + q.n;
-  write_none(p, q.first + covered(p, q), request + 1 == p.batch.n_requests ? p.batch.n_new : end, head, self, threads);
-  if (request == 0) write_none(p, 0, q.first, head, self, threads);
-}
-
-// Tokens of the shared prefix that there are.
-__device__ __forceinline__ uint32_t prefix_there(const AttendParams& p) {
-  if (p.prefix == 0) return 0;
-  const uint32_t len = (uint32_t)as_const(p.pool.lens)[p.prefix_row];
-  return len > p.pool.capacity ? 0 : len < p.prefix ? len : p.prefix;
 }
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------------
@@ -638,23 +551,6 @@ __device__ __forceinline__ void plain_step_of_one(const AttendParams& p, Unit& u
   step_of_one<DT, DP, BIG, true>(p, u, keys, values, at, next, page, query, x, k, v);
 }
 
-// Which part of the work a unit is.
-struct Place {
-  uint32_t block, split, head, request;
-};
-
-__device__ __forceinline__ Place place_of_unit(const AttendParams& p, const AttendPart& part, bool shared, uint32_t unit) {
-  Place w;
-  uint32_t rest;
-  fd_divmod(part.drows, unit, rest, w.block);
-  if (!shared) w.block = part.row_blocks - 1 - w.block;  // (of a prompt the last rows see the most, and are begun first)
-  fd_divmod(part.dsplits, rest, rest, w.split);
-  w.head = rest;
-  w.request = 0;
-  if (!shared) fd_divmod(part.drequests, rest, w.head, w.request);
-  return w;
-}
-
 // The query of a row, element 16 k + 8 half of it in the k-th vector; 0 where there is none.  Returns whether there is a row, and its token.
 template <int DP>
 __device__ __forceinline__ bool load_query(const AttendParams& p, const Request& q, bool shared, uint32_t new_tokens, uint32_t row, uint32_t head,
@@ -904,16 +800,6 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   }
 }
 
-// Workgroups go to the XCDs round-robin.  Each XCD has an eighth of a part's units, which follow one another (blocks of rows of the
-// same tokens, then pieces of the same head); the prefix's units, which may be long, are begun first.
-__device__ __forceinline__ bool unit_of(const AttendParams& p, bool& shared, uint32_t& unit) {
-  const uint32_t front = (p.part[0].units + 7) / 8 * 8;
-  shared = blockIdx.x < front;
-  const uint32_t units = p.part[shared ? 0 : 1].units, at = shared ? blockIdx.x : blockIdx.x - front;
-  unit = (at & 7u) * ((units + 7) / 8) + (at >> 3);
-  return unit < units;
-}
-
 // ONES: neither part has four waves side by side.
 template <int DT, int DP, bool BIG, bool ONES>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(AttendParams p) {
@@ -1031,12 +917,20 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   if (at == 0 && p.lse) p.lse[line] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
-// Workgroups of the attention's launch.
-uint64_t attend_groups(const AttendParams& p) { return ((uint64_t)p.part[0].units + 7) / 8 * 8 + ((uint64_t)p.part[1].units + 7) / 8 * 8; }
-
 // Rows that share a workgroup of the join.  Few rows of many pieces take a workgroup each; many rows share one, a row having as many threads as it has
 // vectors of four sums (up to 128 elements, so that a workgroup's life, which is that of its loads one after the other, is spent on eight rows).
 constexpr uint32_t join_lines(uint32_t D) { return D > 128 ? 4 : 8; }
+
+template <int DT, int DP>
+kvc_status join_of(const AttendParams& p, hipStream_t stream) {
+  constexpr uint32_t kLines = join_lines(DP);
+  const uint32_t lines = p.batch.n_new * p.H * p.G;
+  if (lines <= 2048)
+    hipLaunchKernelGGL((join_kernel<DT, DP, 1>), dim3(lines), dim3(256), p.pieces * 4, stream, p);
+  else
+    hipLaunchKernelGGL((join_kernel<DT, DP, kLines>), dim3((lines + kLines - 1) / kLines), dim3(256), p.pieces * kLines * 4, stream, p);
+  return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_RUNTIME;
+}
 
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
@@ -1049,18 +943,24 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   if (groups && !big && ones) hipLaunchKernelGGL((attend_kernel<DT, DP, false, true>), dim3(groups), dim3(256), 0, stream, p);
   if (groups && !big && !ones) hipLaunchKernelGGL((attend_kernel<DT, DP, false, false>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
-  if (p.pieces != 1) {  // (no piece at all: every row is empty)
-    constexpr uint32_t kLines = join_lines(DP);
-    const uint32_t lines = p.batch.n_new * p.H * p.G;
-    if (lines <= 2048)
-      hipLaunchKernelGGL((join_kernel<DT, DP, 1>), dim3(lines), dim3(256), p.pieces * 4, stream, p);
-    else
-      hipLaunchKernelGGL((join_kernel<DT, DP, kLines>), dim3((lines + kLines - 1) / kLines), dim3(256), p.pieces * kLines * 4, stream, p);
-  }
-  return hipGetLastError() == hipSuccess ? KVC_OK : KVC_ERR_RUNTIME;
+  return p.pieces == 1 ? KVC_OK : join_of<DT, DP>(p, stream);  // (no piece at all: every row is empty)
 }
 
 }  // namespace
+
+uint64_t attend_groups(const AttendParams& p) { return ((uint64_t)p.part[0].units + 7) / 8 * 8 + ((uint64_t)p.part[1].units + 7) / 8 * 8; }
+
+bool attend_fits(const AttendParams& p) {
+  const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = join_lines(p.D);
+  return attend_groups(p) <= kMostGroups && (p.pieces == 1 || (lines + each - 1) / each <= kMostGroups);
+}
+
+kvc_status launch_join(const AttendParams& p, hipStream_t stream) {
+  const bool half = p.dtype == KVC_F16;
+  if (p.D <= 64) return half ? join_of<KVC_F16, 64>(p, stream) : join_of<KVC_BF16, 64>(p, stream);
+  if (p.D <= 128) return half ? join_of<KVC_F16, 128>(p, stream) : join_of<KVC_BF16, 128>(p, stream);
+  return half ? join_of<KVC_F16, 256>(p, stream) : join_of<KVC_BF16, 256>(p, stream);
+}
 
 // Whether the prefix is read anew for each request.  It costs the products of about 64 rows of a block that a request does not fill, over the
 // prefix's tokens and at 900 TFLOP/s, and spares the writing and reading of a sum of each part for each row, at 4 TB/s, and the join's launch.  (Calls of 2 or 8
@@ -1121,9 +1021,7 @@ kvc_status plan_attend(AttendParams& p) {
     a.dtokens = make_fastdiv(a.tokens);
     p.pieces += a.splits;
   }
-  const uint64_t lines = (uint64_t)p.batch.n_new * p.H * p.G, each = join_lines(p.D);
-  if (attend_groups(p) > kMostGroups || (p.pieces != 1 && (lines + each - 1) / each > kMostGroups)) return KVC_ERR_UNSUPPORTED;
-  return KVC_OK;
+  return attend_fits(p) ? KVC_OK : KVC_ERR_UNSUPPORTED;
 }
 
 kvc_status launch_attend(const AttendParams& p, hipStream_t stream) {

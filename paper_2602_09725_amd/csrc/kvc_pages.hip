@@ -516,7 +516,8 @@ __global__ void __launch_bounds__(256) fork_kernel(PoolView p, PageSpace w, cons
     }
   }
   if (job.tokens == 0) return;
-  const uint64_t bytes = (uint64_t)job.tokens * p.token_bytes;
+  // (a page in 4 bits has the tokens of a head, not the heads of a token, side by side: it is copied whole)
+  const uint64_t bytes = (uint64_t)(p.held ? p.block_size : job.tokens) * p.token_bytes;
   uint8_t* d = page_at(p, layer_kind / 2, layer_kind % 2, job.to);
   const uint8_t* s = page_at(p, layer_kind / 2, layer_kind % 2, job.from);
   const uint32_t pieces = (uint32_t)((bytes + kPiece - 1) / kPiece);

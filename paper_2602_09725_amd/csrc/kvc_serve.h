@@ -18,6 +18,7 @@ struct PoolView {
   uint32_t num_blocks, n_rows, table_len, block_size, L;
   uint32_t capacity;      // tokens of a row
   uint32_t token_bytes;   // of one token, layer and kind
+  uint32_t held;          // bits that an element is held in: 4, or 0 where pages have the tokens as they are
   uint64_t page_bytes;    // of one page, layer and kind
   FastDiv dbs;
 };
@@ -69,6 +70,30 @@ struct AppendParams {
 };
 kvc_status launch_append(const AppendParams& p, hipStream_t stream);
 
+// Tokens written to, or read from, pages in 4 bits (or read from pages in 16).
+struct HeldParams {
+  PoolView pool;
+  BatchView batch;
+  const uint16_t *k, *v;
+  uint16_t *k_out, *v_out;
+  const int32_t* first;   // position of each request's first token, or null: its row's last ones
+  int64_t token_stride;
+  uint32_t layer, H, W, dtype;  // W: words of a token's head
+  uint32_t quads;               // groups of four tokens that a batch's can touch
+  FastDiv dcolumns, dwords;     // 2 H, W
+};
+kvc_status launch_write_held(const HeldParams& p, hipStream_t stream);
+kvc_status launch_read(const HeldParams& p, hipStream_t stream);
+
+// Pages from a pool in 16 bits to one in 4, or back.
+struct ConvertParams {
+  PoolView wide, held;
+  const int32_t *src, *dst;
+  uint32_t n, back, H, W, dtype;
+  FastDiv deach, dkinds, dheads;  // quads of all heads of a page, 2 L, H
+};
+kvc_status launch_convert(const ConvertParams& p, hipStream_t stream);
+
 // One of the two parts of an attention call: the shared prefix, or the rows' own tokens.
 struct AttendPart {
   uint32_t waves;       // waves of a workgroup that stand side by side along the rows: 1 or 4
@@ -102,5 +127,11 @@ struct AttendParams {
 // Splits the work (everything but the pointers is set); launch_attend needs what it returns.
 kvc_status plan_attend(AttendParams& p);
 kvc_status launch_attend(const AttendParams& p, hipStream_t stream);
+uint64_t attend_groups(const AttendParams& p);  // workgroups of the attention's launch
+bool attend_fits(const AttendParams& p);        // whether a plan's launches hold its workgroups
+// The same of a pool in 4 bits.
+kvc_status plan_attend_held(AttendParams& p);
+kvc_status launch_attend_held(const AttendParams& p, hipStream_t stream);
+kvc_status launch_join(const AttendParams& p, hipStream_t stream);  // joins the pieces of rows
 
 }  // namespace kvc

@@ -13,17 +13,22 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
+// Type of a pool's tokens, and whether its pages hold them in 4 bits.
+int32_t type_of(const kvc_pool* p) { return p->dtype & ~KVC_HELD_Q4; }
+bool is_held(const kvc_pool* p) { return (p->dtype & KVC_HELD_Q4) != 0; }
+
 // Checks a pool and fills the kernels' view of it.
 kvc_status view_of(const kvc_pool* p, bool books, PoolView* v) {
   if (!p || p->struct_size != sizeof(kvc_pool) || p->abi_version != KVC_ABI_VERSION) return KVC_ERR_INVALID_ARG;
   if (p->num_layers < 1 || p->num_kv_heads < 1 || p->head_dim < 1) return KVC_ERR_INVALID_ARG;
   if (p->num_blocks < 1 || p->n_rows < 1 || p->block_size < 1 || p->table_len < 1) return KVC_ERR_INVALID_ARG;
-  if (p->dtype != KVC_F16 && p->dtype != KVC_BF16) return KVC_ERR_INVALID_ARG;
+  if (type_of(p) != KVC_F16 && type_of(p) != KVC_BF16) return KVC_ERR_INVALID_ARG;
   if (!p->d_layer_cache || !p->d_tables || !p->d_lens || (books && !p->d_refs)) return KVC_ERR_INVALID_ARG;
   if (!aligned(p->d_layer_cache, 8) || !aligned(p->d_tables, 4) || !aligned(p->d_lens, 4) || !aligned(p->d_refs, 4) || !aligned(p->d_err, 4))
     return KVC_ERR_INVALID_ARG;
   const int64_t C = (int64_t)p->num_kv_heads * p->head_dim;
   if (p->head_dim % 8 != 0 || C > (1 << 20) || p->num_layers > (1 << 20) || p->n_rows >= (1 << 18)) return KVC_ERR_UNSUPPORTED;
+  if (is_held(p) && (p->head_dim > 256 || p->block_size % 4 != 0)) return KVC_ERR_UNSUPPORTED;
   if (p->num_blocks >= (1ll << 31) || p->num_blocks * p->block_size >= (1ll << 32)) return KVC_ERR_UNSUPPORTED;
   if ((int64_t)p->table_len * p->block_size >= (1ll << 31)) return KVC_ERR_UNSUPPORTED;
   v->layers = p->d_layer_cache;
@@ -37,7 +42,8 @@ kvc_status view_of(const kvc_pool* p, bool books, PoolView* v) {
   v->block_size = (uint32_t)p->block_size;
   v->L = (uint32_t)p->num_layers;
   v->capacity = v->table_len * v->block_size;
-  v->token_bytes = (uint32_t)(2 * C);
+  v->held = is_held(p) ? 4 : 0;
+  v->token_bytes = is_held(p) ? (uint32_t)(C / 2 + 4 * p->num_kv_heads) : (uint32_t)(2 * C);
   v->page_bytes = (uint64_t)v->block_size * v->token_bytes;
   v->dbs = make_fastdiv(v->block_size);
   return KVC_OK;
@@ -104,13 +110,29 @@ kvc_status plan_of(const kvc_pool* pool, const kvc_batch* batch, const kvc_atten
   p->H = (uint32_t)pool->num_kv_heads;
   p->G = (uint32_t)group;
   p->D = (uint32_t)pool->head_dim;
-  p->dtype = (uint32_t)pool->dtype;
+  p->dtype = (uint32_t)type_of(pool);
   p->prefix = (uint32_t)a->prefix_tokens;
   p->prefix_row = (uint32_t)a->prefix_row;
   p->most_tokens = (uint32_t)a->most_tokens;
   p->dG = make_fastdiv(p->G);
   p->scale_log2 = (float)((double)a->scale * 1.4426950408889634);
-  return batch->n_new == 0 ? KVC_OK : plan_attend(*p);
+  if (batch->n_new == 0) return KVC_OK;
+  return p->pool.held ? plan_attend_held(*p) : plan_attend(*p);
+}
+
+// What the calls that write and read tokens in quads have in common.
+kvc_status fill_held(const kvc_pool* pool, int32_t layer, int64_t token_stride, HeldParams* p) {
+  p->token_stride = token_stride;
+  p->layer = (uint32_t)layer;
+  p->H = (uint32_t)pool->num_kv_heads;
+  p->W = (uint32_t)pool->head_dim / 8;
+  p->dtype = (uint32_t)type_of(pool);
+  const uint64_t quads = p->batch.starts ? p->batch.n_new / 4 + 2ull * p->batch.n_requests : p->batch.n_requests;
+  if (quads >> 31) return KVC_ERR_UNSUPPORTED;
+  p->quads = (uint32_t)quads;
+  p->dcolumns = make_fastdiv(2 * p->H);
+  p->dwords = make_fastdiv(p->W);
+  return KVC_OK;
 }
 
 // Bytes of the joined pieces' sums, and in all.
@@ -131,6 +153,11 @@ extern "C" {
 kvc_status kvc_pool_validate(const kvc_pool* pool) {
   PoolView v{};
   return view_of(pool, false, &v);
+}
+
+size_t kvc_page_bytes(const kvc_pool* pool) {
+  PoolView v{};
+  return view_of(pool, false, &v) == KVC_OK ? (size_t)v.page_bytes : 0;
 }
 
 size_t kvc_pages_workspace(const kvc_pool* pool) {
@@ -207,6 +234,15 @@ kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_
   if (batch->n_new == 0) return KVC_OK;
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return KVC_ERR_INVALID_ARG;
   if (token_stride < 0 || token_stride % 8 != 0) return KVC_ERR_INVALID_ARG;
+  if (p.pool.held) {
+    HeldParams h{};
+    h.pool = p.pool;
+    h.batch = p.batch;
+    h.k = static_cast<const uint16_t*>(k);
+    h.v = static_cast<const uint16_t*>(v);
+    st = fill_held(pool, layer, token_stride, &h);
+    return st == KVC_OK ? launch_write_held(h, as_stream(stream)) : st;
+  }
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);
   p.token_stride = token_stride;
@@ -214,6 +250,51 @@ kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_
   p.atoms = p.pool.token_bytes / 16;
   p.datoms = make_fastdiv(p.atoms);
   return launch_append(p, as_stream(stream));
+}
+
+kvc_status kvc_read_paged(const kvc_pool* pool, const kvc_batch* batch, const int32_t* d_first, int32_t layer, void* k, void* v,
+                          int64_t token_stride, void* stream) {
+  HeldParams p{};
+  kvc_status st = view_of(pool, false, &p.pool);
+  if (st != KVC_OK) return st;
+  if ((st = view_of(batch, &p.batch)) != KVC_OK) return st;
+  if (layer < 0 || layer >= pool->num_layers || !aligned(d_first, 4)) return KVC_ERR_INVALID_ARG;
+  if (batch->n_new == 0) return KVC_OK;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return KVC_ERR_INVALID_ARG;
+  if (token_stride % 8 != 0 || token_stride < (int64_t)pool->num_kv_heads * pool->head_dim) return KVC_ERR_INVALID_ARG;
+  p.k_out = static_cast<uint16_t*>(k);
+  p.v_out = static_cast<uint16_t*>(v);
+  p.first = d_first;
+  st = fill_held(pool, layer, token_stride, &p);
+  return st == KVC_OK ? launch_read(p, as_stream(stream)) : st;
+}
+
+kvc_status kvc_pages_convert(const kvc_pool* from, const kvc_pool* to, const int32_t* d_src, const int32_t* d_dst, int64_t n, void* stream) {
+  ConvertParams p{};
+  PoolView a{}, b{};
+  kvc_status st = view_of(from, false, &a);
+  if (st != KVC_OK) return st;
+  if ((st = view_of(to, false, &b)) != KVC_OK) return st;
+  if (from->num_layers != to->num_layers || from->num_kv_heads != to->num_kv_heads || from->head_dim != to->head_dim ||
+      from->block_size != to->block_size || type_of(from) != type_of(to) || a.held == b.held)
+    return KVC_ERR_INVALID_ARG;
+  if (n < 0 || n >= (1ll << 31)) return KVC_ERR_INVALID_ARG;
+  if (n == 0) return KVC_OK;
+  if (!d_src || !d_dst || !aligned(d_src, 4) || !aligned(d_dst, 4)) return KVC_ERR_INVALID_ARG;
+  p.back = a.held != 0;
+  p.wide = p.back ? b : a;
+  p.held = p.back ? a : b;
+  p.src = d_src;
+  p.dst = d_dst;
+  p.n = (uint32_t)n;
+  p.H = (uint32_t)from->num_kv_heads;
+  p.W = (uint32_t)from->head_dim / 8;
+  p.dtype = (uint32_t)type_of(from);
+  if ((uint64_t)p.H * (p.held.block_size / 4) >> 31) return KVC_ERR_UNSUPPORTED;
+  p.deach = make_fastdiv(p.H * (p.held.block_size / 4));
+  p.dkinds = make_fastdiv(2 * p.held.L);
+  p.dheads = make_fastdiv(p.H);
+  return launch_convert(p, as_stream(stream));
 }
 
 size_t kvc_attention_workspace(const kvc_pool* pool, const kvc_batch* batch, const kvc_attention* attention) {
@@ -242,7 +323,7 @@ kvc_status kvc_attend_paged(const kvc_pool* pool, const kvc_batch* batch, const 
   p.q = static_cast<const uint16_t*>(q);
   p.out = static_cast<uint16_t*>(out);
   p.lse = lse;
-  return launch_attend(p, as_stream(stream));
+  return p.pool.held ? launch_attend_held(p, as_stream(stream)) : launch_attend(p, as_stream(stream));
 }
 
 }  // extern "C"

@@ -153,6 +153,10 @@ def load(path=None):
     lib.kvc_pages_free.argtypes = [pp, vp, i64, vp]
     lib.kvc_pages_compact.argtypes = [pp, vp, vp, vp, vp, sz, vp]
     lib.kvc_append_paged.argtypes = [pp, bp, i32, vp, vp, i64, vp]
+    lib.kvc_page_bytes.argtypes = [pp]
+    lib.kvc_page_bytes.restype = sz
+    lib.kvc_read_paged.argtypes = [pp, bp, vp, i32, vp, vp, i64, vp]
+    lib.kvc_pages_convert.argtypes = [pp, pp, vp, vp, i64, vp]
     lib.kvc_attention_workspace.argtypes = [pp, bp, ap]
     lib.kvc_attention_workspace.restype = sz
     lib.kvc_attend_paged.argtypes = [pp, bp, ap, i32, vp, vp, vp, vp, sz, vp]
@@ -387,10 +391,19 @@ def layout_set_resolution(layout, width, height):
 # ---- serving on a restored cache
 
 KVC_FAULT_PAGE, KVC_FAULT_LIST, KVC_FAULT_NO_ROOM = 1, 2, 4
+KVC_HELD_Q4 = 0x10  # with a pool's dtype: its pages hold tokens in 4 bits
 
 
 def pool_validate(pool):
     return load().kvc_pool_validate(C.byref(pool))
+
+
+def page_bytes(pool):
+    """Bytes of a page of one layer and kind."""
+    n = load().kvc_page_bytes(C.byref(pool))
+    if n == 0:
+        raise KvcError(pool_validate(pool), "kvc_page_bytes")
+    return n
 
 
 def pages_workspace(pool):
@@ -425,6 +438,16 @@ def kvc_pages_compact(pool, map_ptr, tables_out_ptr, refs_out_ptr, workspace_ptr
 
 def kvc_append_paged(pool, batch, layer, k_ptr, v_ptr, token_stride, stream=0):
     _check(load().kvc_append_paged(C.byref(pool), C.byref(batch), layer, k_ptr, v_ptr, token_stride, stream), "kvc_append_paged")
+
+
+def kvc_read_paged(pool, batch, first_ptr, layer, k_ptr, v_ptr, token_stride, stream=0):
+    """first_ptr None: the batch's tokens are their rows' last ones."""
+    _check(load().kvc_read_paged(C.byref(pool), C.byref(batch), first_ptr, layer, k_ptr, v_ptr, token_stride, stream), "kvc_read_paged")
+
+
+def kvc_pages_convert(from_pool, to_pool, src_ptr, dst_ptr, n, stream=0):
+    """One of the pools is of KVC_HELD_Q4."""
+    _check(load().kvc_pages_convert(C.byref(from_pool), C.byref(to_pool), src_ptr, dst_ptr, n, stream), "kvc_pages_convert")
 
 
 def attention_workspace(pool, batch, attention):
