@@ -19,6 +19,22 @@ constexpr float kNone = -__builtin_inff();
 // exp2(a - b) where a is -inf if b is: 0 then.
 __device__ __forceinline__ float weight(float a, float b) { return a == kNone ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
 
+// ---- waits ----------------------------------------------------------------------------------------------------------------
+
+// Waits until the wave's reads of LDS have come back.
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
+
+// All waves of a workgroup have come here, and their reads of LDS have come back; loads stay under way.
+__device__ __forceinline__ void meet() {
+  wait_reads();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // ---- who sees what --------------------------------------------------------------------------------------------------------
 
 struct Request {

@@ -150,13 +150,6 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
-// Waits until the wave's reads of LDS have come back.
-__device__ __forceinline__ void wait_reads() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  asm volatile("" ::: "memory");
-}
-
 // Page of token lane % TT of the tile at position `at`, if it is there.  (Always one load: waits count it.  It lies within the table,
 // and need not wait for the row's length.)
 template <int TT>
@@ -382,13 +375,6 @@ __device__ __forceinline__ bool hides_tokens(const Unit& u, uint32_t at) { retur
 
 // Tokens from t0 on that are all there and seen by all rows: tiles among them need no mask.
 __device__ __forceinline__ uint32_t plain_end(const Unit& u) { return max(u.t0, min(u.least, u.t1)); }
-
-// All waves of a workgroup have come here, and their reads of LDS have come back; loads stay under way.
-__device__ __forceinline__ void meet() {
-  wait_reads();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 
 // The e-th vector of 32 tokens of K, the one that a lane has in the product.
 template <int DP>

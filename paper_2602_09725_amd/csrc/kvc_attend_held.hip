@@ -1,18 +1,25 @@
 // Attention of a batch over pages held in 4 bits (kvc_attend_paged on a pool of KVC_HELD_Q4).
 //
 // A token's key is k = s c + m with codes c of 0 .. 15 and a pair (s, m) of its head, so that q . k = s (q . c) + m sum(q); its value likewise, so that
-//   sum_t w_t v_t = sum_t (w_t s_t) c_t + sum_t w_t m_t.
+//   sum_t w_t v_t = sum_t (w_t s_t) (c_t - 8) + sum_t (w_t s_t) z_t,  z = m / s + 8.
 // Codes go into the matrix unit as they are: the products with keys are of exact numbers, and nothing is dequantized element by element.
 //   Keys: four bits in the low mantissa bits of an fp16 number are c 2^-24, a subnormal that the matrix unit takes exactly; the next four bits are c 2^-20.  Queries are
-//   made fp16 numbers of their row's size (a power of two, exact but for elements 2^34 below the row's largest), those that meet the second kind a sixteenth of it.
+//   made fp16 numbers by a power of two that all rows of a workgroup share (exact but for what lies 2^-35 below the largest of their elements), those that meet the
+//   second kind a sixteenth of it.
 //   Values: four bits in the mantissa of 128 are 128 + c in bf16.  Weights w s are rounded to bf16 (half a step, as the inputs of such a pool have), or for a pool
-//   of fp16 to two of them, which hold 16 bits.  A third product, with ones, sums the rounded weights: 136 of these sums are taken off and w (m + 8 s)
-//   is added in fp32, so that a weight's rounding counts by the distance from the middle of the codes, not from 0.
+//   of fp16 to two of them, which hold 16 bits.  One more product has rows of -136 and of z (in two bf16 numbers): what takes the offset off, and the second term,
+//   of the rounded weights.
+// A weight's rounding so counts by the distance from the middle of the codes, not from 0.
 //
-// A tile is 64 tokens of a wave's own.  S^T = K Q^T and O^T += V^T W^T are 16x16x32 products: a lane has one row (lane % 16), and of a tile the 16 tokens from
+// A tile is 64 tokens.  S^T = K Q^T and O^T += V^T W^T are 16x16x32 products: a lane has one row (lane % 16), and of a tile the 16 tokens from
 // 16 (lane / 16) on.  A page has each word of four tokens side by side (a quad), so that a lane's 16 bytes are the operands of four products with keys, and
-// of values, whose operands take two tokens' codes of one element, words of two tokens are merged half by half.  No operand passes through LDS; the pairs do, a token a lane.
+// of values, whose operands take two tokens' codes of one element, words of two tokens are merged half by half.  No operand passes through LDS; what the pairs
+// give does, a token a lane.
 #include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include <type_traits>
 
 #include "kvc_attend.h"
 #include "kvc_device.h"
@@ -30,6 +37,11 @@ __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
 }
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Adds a product to a sum.
+__device__ __forceinline__ void add_product(u32x4 a, u32x4 b, f32x4& sum) {
+  sum = mfma_bf16(a, b, sum);
 }
 
 constexpr uint32_t kTile = 64;  // tokens
@@ -63,26 +75,38 @@ struct Unit {
   uint32_t quad_bytes;     // codes of a quad
 };
 
+// Where a lane's part of a tile lies: the codes and pairs of quad lane % 16.
+template <bool BIG>
+struct Source {
+  typename Unit<BIG>::Offset codes, pairs;
+  uint32_t missing;  // bit: the quad is on no page of the pool
+};
+
 // A tile's loads.
 template <int DP>
 struct Tile {
   u32x4 k[Sizes<DP>::KS], v[Sizes<DP>::VS][4];
-  uint32_t kp, vp;   // pairs of token `lane`
-  uint32_t missing;  // bit: the quad is on no page of the pool
+  uint32_t kp, vp;  // pairs of token `lane`
+};
+
+// What the pairs of a tile's tokens give.
+struct alignas(16) PairSpace {
+  float ks[kTile], km[kTile], vs[kTile];  // scale and least value of keys, times what a product is multiplied with; scale of values
+  uint16_t z[4][kTile];                   // rows of the product that sums weights, bf16: -136, z, what is left of it, 135
 };
 
 template <int DP, int RB>
 struct State {
-  float m[RB], l[RB], low[RB];  // a number near the largest product, sum of this lane's weights, of what they add to all elements
-  f32x4 total[RB];              // sums of the rounded weights
+  float m[RB], l[RB];  // a number near the largest exponent, sum of this lane's weights
+  f32x4 total[RB];     // what the rounded weights add to all elements, in three parts
   f32x4 sum[RB][Sizes<DP>::VS][Sizes<DP>::NJ];
 };
 
 template <int RB>
 struct Rows {
-  float unit[RB], whole[RB];    // log2 of a weight for one step of a product; sum of the query
-  float slack[RB];
-  uint32_t limit[RB];           // positions below it are seen
+  float whole[RB];      // sum of the query
+  uint32_t limit[RB];   // positions below it are seen
+  float unit;           // log2 of a weight for one step of a product
 };
 
 template <bool BIG>
@@ -99,38 +123,80 @@ __device__ __forceinline__ T of_lane(uint32_t lane, T v) {
     return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(lane * 4), (int)v);
 }
 
-// Loads the tile at position `at`; page: that of the lane's quad.  A quad that is not there is read from page 0, which is.
-template <int DP, bool BIG>
-__device__ __forceinline__ void load_tile(const AttendParams& p, const Unit<BIG>& u, uint32_t at, uint32_t page, Tile<DP>& t) {
-  using S = Sizes<DP>;
+// Where the tile at position `at` lies; page: that of the lane's quad.  A quad that is not there is read from page 0, which is.
+template <bool BIG>
+__device__ __forceinline__ Source<BIG> source_of(const AttendParams& p, const Unit<BIG>& u, uint32_t at, uint32_t page) {
   using Offset = typename Unit<BIG>::Offset;
-  const uint32_t lane = threadIdx.x & 63u, quad = lane & 15u, g = lane >> 4, W = p.D / 8;
-  const uint32_t pos = at + quad * 4;
-  const bool gone = pos >= u.t1, bad = page >= p.pool.num_blocks;
-  t.missing = (uint32_t)__ballot(bad && !gone) & 0xffffu;
+  const uint32_t pos = at + (threadIdx.x & 15u) * 4;
+  const bool gone = pos >= u.t1, bad = page >= p.pool.num_blocks, none = bad || gone;
   const uint32_t slot = pos - fd_div(p.pool.dbs, pos) * p.pool.block_size;
-  const bool none = bad || gone;
   const Offset begin = none ? (Offset)0 : (Offset)page * (Offset)p.pool.page_bytes;
-  const Offset codes = begin + (none ? 0u : slot / 4 * u.quad_bytes), pairs = begin + (none ? 0u : slot * 4);
-  const uint8_t KVC_GLOBAL* const value_codes = u.codes + u.values;
-#pragma unroll
-  for (int e = 0; e < S::KS; ++e) {
-    const uint32_t w = min((uint32_t)e * 4 + g, W - 1);  // (words that the head lacks meet a query's zeros)
-    t.k[e] = *(const u32x4 KVC_GLOBAL*)(u.codes + (codes + w * 16));
-  }
-  const Offset pair = of_lane(lane / 4, pairs) + (lane & 3u) * 4;
+  return Source<BIG>{begin + (none ? 0u : slot / 4 * u.quad_bytes), begin + (none ? 0u : slot * 4), (uint32_t)__ballot(bad && !gone) & 0xffffu};
+}
+
+template <int DP, bool BIG>
+__device__ __forceinline__ void load_keys(const AttendParams& p, const Unit<BIG>& u, const Source<BIG>& from, Tile<DP>& t) {
+  const uint32_t lane = threadIdx.x & 63u, g = lane >> 4, W = p.D / 8;
+  const auto pair = of_lane(lane / 4, from.pairs) + (lane & 3u) * 4;
   t.kp = *(const uint32_t KVC_GLOBAL*)(u.pairs + pair);
   t.vp = *(const uint32_t KVC_GLOBAL*)(u.pairs + u.values + pair);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const Offset from = of_lane(g * 4 + i, codes);
+  for (int e = 0; e < Sizes<DP>::KS; ++e)  // (words that the head lacks meet a query's zeros)
+    t.k[e] = *(const u32x4 KVC_GLOBAL*)(u.codes + (from.codes + min((uint32_t)e * 4 + g, W - 1) * 16));
+}
+
+template <int DP, bool BIG>
+__device__ __forceinline__ void load_values(const AttendParams& p, const Unit<BIG>& u, const Source<BIG>& from, Tile<DP>& t) {
+  const uint32_t lane = threadIdx.x & 63u, quad = lane & 15u, g = lane >> 4, W = p.D / 8;
+  const uint8_t KVC_GLOBAL* const codes = u.codes + u.values;
 #pragma unroll
-    for (int s = 0; s < S::VS; ++s) {
-      const uint32_t w = min(DP == 64 ? quad & 7u : quad + 16 * s, W - 1);  // (elements that the head lacks are not written)
-      t.v[s][i] = *(const u32x4 KVC_GLOBAL*)(value_codes + (from + w * 16));
-    }
+  for (int i = 0; i < 4; ++i) {
+    const auto at = of_lane(g * 4 + i, from.codes);
+#pragma unroll
+    for (int s = 0; s < Sizes<DP>::VS; ++s)  // (elements that the head lacks are not written)
+      t.v[s][i] = *(const u32x4 KVC_GLOBAL*)(codes + (at + min(DP == 64 ? quad & 7u : quad + 16 * s, W - 1) * 16));
   }
 }
+
+// A scale, and the least value in steps of it.  A head whose values are all alike has scale 0: it is given its value's size for a scale.
+__device__ __forceinline__ void steps_of(float& s, float m, float& z) {
+  if (s == 0.0f) {
+    s = fabsf(m);
+    z = m == 0.0f ? 0.0f : copysignf(1.0f, m);
+  } else {
+    const float r = __builtin_amdgcn_rcpf(s);
+    z = m * r;
+    z = fmaf(fmaf(-z, s, m), r, z);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void put_key_pair(PairSpace& to, uint32_t token, uint32_t pair, float unit) {
+  float s, m;
+  widen_pair<DT>(pair, s, m);
+  to.ks[token] = s * unit;
+  to.km[token] = m * unit;
+}
+
+// Returns whether the token's scale is 0.  A pair that is not finite makes NaN of the weights that see it, and nothing of the others.
+template <int DT>
+__device__ __forceinline__ bool put_value_pair(PairSpace& to, uint32_t token, uint32_t pair) {
+  constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
+  const bool wild = (pair & kExp) == kExp || (pair >> 16 & kExp) == kExp;
+  float s, m, z;
+  widen_pair<DT>(pair, s, m);
+  const bool flat = s == 0.0f;
+  steps_of(s, m, z);
+  z = wild ? 0.0f : z + 8.0f;
+  to.vs[token] = wild ? __builtin_nanf("") : s;
+  const uint32_t high = narrow_pair<KVC_BF16>(z, 0.0f);
+  to.z[1][token] = (uint16_t)high;
+  to.z[2][token] = (uint16_t)narrow_pair<KVC_BF16>(z - widen_bits<KVC_BF16>(high & 0xffffu), 0.0f);
+  return flat;
+}
+
+// Rows of the pair space that are the same for all tiles.
+__device__ __forceinline__ void begin_pairs(PairSpace& to, uint32_t token) { to.z[0][token] = 0xc308, to.z[3][token] = 0x4307; }
 
 // Eight codes -> an operand of the products with keys.
 __device__ __forceinline__ u32x4 key_operand(uint32_t w) {
@@ -138,20 +204,104 @@ __device__ __forceinline__ u32x4 key_operand(uint32_t w) {
   return u32x4{w & 0x000f000fu, w & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u};
 }
 
-// One tile.  MASKED: not all of it is there and seen by all rows.
-template <int DT, int DP, int RB, bool MASKED>
-__device__ __forceinline__ void take_tile(const AttendParams& p, uint32_t at, uint32_t t1, const Tile<DP>& t, const Rows<RB>& rows,
-                                          const u32x4 (&query)[RB][Sizes<DP>::KS], State<DP, RB>& x, f32x2* kpair, f32x2* vpair) {
+// Words of eight tokens -> two tokens' elements 2 n (or, with the selector's other value, 2 n + 1) side by side.
+__device__ __forceinline__ u32x4 halves(u32x4 y, u32x4 z, uint32_t selector) {
+  return u32x4{__builtin_amdgcn_perm(y.y, y.x, selector), __builtin_amdgcn_perm(y.w, y.z, selector), __builtin_amdgcn_perm(z.y, z.x, selector),
+               __builtin_amdgcn_perm(z.w, z.z, selector)};
+}
+constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+// Tiles take turns: of the even ones operands are 128 + c, of the odd ones c - 143, so that what is not c - 8 of them nearly cancels in the sums, which
+// fp32 would else lose the rest of in long rows.  turned: 0 or 1.
+__device__ __forceinline__ u32x4 value_operand(u32x4 both, int n, uint32_t turned) {
+  const uint32_t with = turned ? 0xc30fc30fu : 0x43004300u;
+  uint32_t mask = 0x000f000fu;
+  asm("" : "+s"(mask));
+  return u32x4{(both.x >> 4 * n & mask) ^ with, (both.y >> 4 * n & mask) ^ with, (both.z >> 4 * n & mask) ^ with, (both.w >> 4 * n & mask) ^ with};
+}
+
+constexpr float kMost = 16.0f;  // exponents of up to this leave the base as it is
+
+// Weights of a tile from its products s[k][i], those of token 16 g + 4 i + k (they are overwritten): operands w[h] of tokens 16 g + 8 h .. + 7, and for fp16
+// what their rounding left.  masked: not all of it is there and seen by all rows (wave-uniform); missing: quads on no page.  The number subtracted from an exponent need not be
+// the largest one: weights of up to 2^16 do no harm to sums in fp32 and to bf16.  (The order is the source's: a few of LDS's numbers at a time.)
+template <int DT, int DP, int RB>
+__device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, uint32_t missing, const PairSpace& pairs, const Rows<RB>& rows, int b, f32x4 (&s)[4],
+                                        State<DP, RB>& x, u32x4 (&w)[2], u32x4 (&fine)[2]) {
+  const uint32_t g = (threadIdx.x & 63u) >> 4;
+  const float shift = x.m[b] == kNone ? 0.0f : x.m[b];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 ks = *(const f32x4*)&pairs.ks[16 * g + 4 * i], km = *(const f32x4*)&pairs.km[16 * g + 4 * i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k][i] = fmaf(s[k][i], ks[k], fmaf(km[k], rows.whole[b], -shift));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (masked) {
+    const int32_t left = (int32_t)(min(rows.limit[b], t1) - at - 16 * g);
+    const uint32_t gone = missing >> (4 * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k][i] = 4 * i + k < left && !(gone >> i & 1u) ? s[k][i] : kNone;
+  }
+  float top = kNone;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, s[k][i]);
+  if (__any(top > kMost || x.m[b] == kNone)) {
+    top = row_max(top);
+    const bool first = x.m[b] == kNone;
+    const float up = first ? (top == kNone ? 0.0f : top) : fmaxf(top, 0.0f), keep = __builtin_amdgcn_exp2f(first ? 0.0f : -up);
+    if (!first || top != kNone) x.m[b] = shift + up;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k][i] -= up;
+    x.l[b] *= keep;  // (a row that had no base has sums of 0)
+    x.total[b] *= keep;
+#pragma unroll
+    for (int v = 0; v < Sizes<DP>::VS; ++v)
+#pragma unroll
+      for (int j = 0; j < Sizes<DP>::NJ; ++j) x.sum[b][v][j] *= keep;
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x4 vs = *(const f32x4*)&pairs.vs[16 * g + 4 * i];
+    if (masked) {  // (what is not seen may be held with anything)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) vs[k] = s[k][i] == kNone ? 0.0f : vs[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      const float y = __builtin_amdgcn_exp2f(s[k][i]), z = __builtin_amdgcn_exp2f(s[k + 1][i]);
+      x.l[b] += y + z;
+      const float a = y * vs[k], c = z * vs[k + 1];
+      const uint32_t r = narrow_pair<KVC_BF16>(a, c);
+      w[i / 2][i % 2 * 2 + k / 2] = r;
+      if constexpr (DT == KVC_F16)
+        fine[i / 2][i % 2 * 2 + k / 2] = narrow_pair<KVC_BF16>(a - widen_bits<KVC_BF16>(r & 0xffffu), c - widen_bits<KVC_BF16>(r >> 16));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// Operand of the product that sums weights: rows 4 i of what takes the codes' offset off, 4 i + 1 of z, 4 i + 2 of its rest; nobody looks at the others.
+__device__ __forceinline__ u32x4 sums_operand(const PairSpace& pairs, int h, uint32_t turned) {
+  const uint32_t lane = threadIdx.x & 63u, row = (lane & 3u) == 0 && turned ? 3u : lane & 3u;
+  return *(const u32x4*)&pairs.z[row][16 * (lane >> 4) + 8 * h];
+}
+
+// One tile of a wave's own.  The next tile's loads follow as soon as this one's have been used.
+template <int DT, int DP, int RB, bool BIG>
+__device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>& u, bool masked, uint32_t turned, uint32_t at, uint32_t missing, const Source<BIG>& next, Tile<DP>& t,
+                                          const Rows<RB>& rows, const u32x4 (&query)[RB][Sizes<DP>::KS], State<DP, RB>& x, PairSpace& pairs) {
   using S = Sizes<DP>;
   const uint32_t lane = threadIdx.x & 63u, g = lane >> 4;
-  {
-    float s, m;
-    widen_pair<DT>(t.kp, s, m);
-    kpair[lane] = f32x2{s, m};
-    widen_pair<DT>(t.vp, s, m);
-    vpair[lane] = f32x2{s, fmaf(8.0f, s, m)};
-  }
-  // products: s[b][k][i] is token 16 g + 4 i + k
+  put_key_pair<DT>(pairs, lane, t.kp, rows.unit);
+  const uint64_t flat = __ballot(put_value_pair<DT>(pairs, lane, t.vp));
+  // (The order is the source's: left to itself the compiler makes all operands first, and has no registers for them.)
   f32x4 s[RB][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -161,157 +311,111 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, uint32_t at, ui
 #pragma unroll
       for (int b = 0; b < RB; ++b) s[b][k] = mfma_f16(a, query[b][e], e ? s[b][k] : f32x4{0, 0, 0, 0});
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const f32x2 pair = kpair[16 * g + 4 * i + k];
-#pragma unroll
-      for (int b = 0; b < RB; ++b) s[b][k][i] = fmaf(pair.x, s[b][k][i], pair.y * rows.whole[b]);
-    }
-  if constexpr (MASKED) {
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const int32_t seen = (int32_t)(min(rows.limit[b], t1) - at - 16 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (4 * i + k >= seen || (t.missing >> (4 * g + i) & 1u)) s[b][k][i] = kNone;
-    }
-  }
-  // bases
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    float top = kNone;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][k][i]);
-    if (__any(top > x.m[b] + rows.slack[b])) {
-      const float now = fmaxf(x.m[b], row_max(top)), keep = weight(x.m[b] * rows.unit[b], now * rows.unit[b]);
-      x.m[b] = now;
-      x.l[b] *= keep;
-      x.low[b] *= keep;
-      x.total[b] *= keep;
-#pragma unroll
-      for (int v = 0; v < S::VS; ++v)
-#pragma unroll
-        for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] *= keep;
-    }
-  }
-  // weights: w[b][h] is the operand of tokens 16 g + 8 h .. + 7
+  load_keys<DP, BIG>(p, u, next, t);
+  __builtin_amdgcn_sched_barrier(0);
   u32x4 w[RB][2], fine[RB][2];
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    const float shift = x.m[b] == kNone ? 0.0f : x.m[b] * rows.unit[b];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float a[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x2 pair = vpair[16 * g + 4 * i + k];
-        const float y = __builtin_amdgcn_exp2f(fmaf(s[b][k][i], rows.unit[b], -shift));
-        x.l[b] += y;
-        a[k] = y * pair.x;
-        const float low = fmaf(y, pair.y, x.low[b]);
-        if constexpr (MASKED) {  // (what is not seen may be held with anything)
-          const bool none = s[b][k][i] == kNone;
-          a[k] = none ? 0.0f : a[k];
-          x.low[b] = none ? x.low[b] : low;
-        } else {
-          x.low[b] = low;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 4; k += 2) {
-        const uint32_t r = narrow_pair<KVC_BF16>(a[k], a[k + 1]);
-        w[b][i / 2][i % 2 * 2 + k / 2] = r;
-        if constexpr (DT == KVC_F16) fine[b][i / 2][i % 2 * 2 + k / 2] = narrow_pair<KVC_BF16>(a[k] - widen_bits<KVC_BF16>(r & 0xffffu), a[k + 1] - widen_bits<KVC_BF16>(r >> 16));
-      }
-    }
+    weights<DT, DP, RB>(masked, at, u.t1, missing, pairs, rows, b, s[b], x, w[b], fine[b]);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  // values
-  const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  if (flat) {  // (codes that a scale of 0 makes nothing of)
+    const uint32_t mine = (uint32_t)(flat >> (16 * g)) & 0xffffu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int v = 0; v < S::VS; ++v) t.v[v][i][k] = mine >> (4 * i + k) & 1u ? 0u : t.v[v][i][k];
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    const u32x4 rows_of_sums = sums_operand(pairs, h, turned);
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      x.total[b] = mfma_bf16(ones, w[b][h], x.total[b]);
-      if constexpr (DT == KVC_F16) x.total[b] = mfma_bf16(ones, fine[b][h], x.total[b]);
+      add_product(rows_of_sums, w[b][h], x.total[b]);
+      if constexpr (DT == KVC_F16) add_product(rows_of_sums, fine[b][h], x.total[b]);
     }
 #pragma unroll
-    for (int v = 0; v < S::VS; ++v) {
-      const u32x4 y = t.v[v][2 * h], z = t.v[v][2 * h + 1];
+    for (int v = 0; v < S::VS; ++v)
 #pragma unroll
       for (int half = 0; half < (DP == 64 ? 1 : 2); ++half) {
         // (of up to 64 elements the lanes from 8 on have the odd elements of the words that the others have)
-        const uint32_t sel = DP == 64 ? ((lane & 8u) ? 0x07060302u : 0x05040100u) : half ? 0x07060302u : 0x05040100u;
-        const u32x4 both = {__builtin_amdgcn_perm(y.y, y.x, sel), __builtin_amdgcn_perm(y.w, y.z, sel), __builtin_amdgcn_perm(z.y, z.x, sel),
-                            __builtin_amdgcn_perm(z.w, z.z, sel)};
+        const u32x4 both = halves(t.v[v][2 * h], t.v[v][2 * h + 1], DP == 64 ? ((lane & 8u) ? kHigh : kLow) : half ? kHigh : kLow);
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const u32x4 a = {(both.x >> 4 * n & 0x000f000fu) | 0x43004300u, (both.y >> 4 * n & 0x000f000fu) | 0x43004300u,
-                           (both.z >> 4 * n & 0x000f000fu) | 0x43004300u, (both.w >> 4 * n & 0x000f000fu) | 0x43004300u};
+          const u32x4 a = value_operand(both, n, turned);
           const int j = DP == 64 ? n : 2 * n + half;
 #pragma unroll
           for (int b = 0; b < RB; ++b) {
-            x.sum[b][v][j] = mfma_bf16(a, w[b][h], x.sum[b][v][j]);
-            if constexpr (DT == KVC_F16) x.sum[b][v][j] = mfma_bf16(a, fine[b][h], x.sum[b][v][j]);
+            add_product(a, w[b][h], x.sum[b][v][j]);
+            if constexpr (DT == KVC_F16) add_product(a, fine[b][h], x.sum[b][v][j]);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
   }
+  load_values<DP, BIG>(p, u, next, t);
 }
 
-// The query of a row as the products take it, and what its weights are computed with.
+// The queries of a wave's rows as the products take them, and what weights are computed with.  Rows that see nothing, whose queries may be anything, do not count.
 template <int DT, int DP, int RB>
-__device__ __forceinline__ void load_queries(const AttendParams& p, const uint16_t* const (&from)[RB], const bool (&there)[RB], u32x4 (&query)[RB][Sizes<DP>::KS],
-                                             Rows<RB>& rows) {
-  using S = Sizes<DP>;
+__device__ __forceinline__ uint32_t load_queries(const AttendParams& p, const uint16_t* const (&from)[RB], u32x4 (&raw)[RB][Sizes<DP>::KS], const Rows<RB>& rows) {
   const uint32_t g = (threadIdx.x & 63u) >> 4, W = p.D / 8;
+  constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
+  uint32_t most = 0;
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+#pragma unroll
+    for (int e = 0; e < Sizes<DP>::KS; ++e) {
+      const uint32_t w = e * 4 + g;
+      raw[b][e] = *(const KVC_GLOBAL u32x4*)(from[b] + min(w, W - 1) * 8);
+      if (rows.limit[b] == 0 || w >= W) raw[b][e] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = raw[b][e][i] & 0x7fffu, y = raw[b][e][i] >> 16 & 0x7fffu;
+        most = max(most, max(x < kExp ? x : 0, y < kExp ? y : 0));
+      }
+    }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+  return most;
+}
+
+// most: the largest of the workgroup's elements (bits).  It comes to lie in [2^14, 2^15); a step beyond 2^115 would pass fp32's range.
+template <int DT, int DP, int RB>
+__device__ __forceinline__ void make_queries(const AttendParams& p, uint32_t most, u32x4 (&query)[RB][Sizes<DP>::KS], Rows<RB>& rows) {
+  const int up = most ? max(15 - __builtin_amdgcn_frexp_expf(widen_bits<DT>(most)), -100) : 0;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    u32x4 raw[S::KS];
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < S::KS; ++e) {
-      const uint32_t w = e * 4 + g;
-      raw[e] = *(const KVC_GLOBAL u32x4*)(from[b] + min(w, W - 1) * 8);
-      if (!there[b] || w >= W) raw[e] = u32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) most = max(most, max(raw[e][i] & 0x7fffu, raw[e][i] >> 16 & 0x7fffu));
-    }
-    const float largest = row_max(widen_bits<DT>(most));
-    // its largest element comes to lie in [2^14, 2^15).  (An infinity or a NaN stays one; beyond 2^115 the step would pass fp32's range.)
-    int up = largest > 0.0f && largest < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(largest) : 0;
-    up = max(up, -100);
     float whole = 0.0f;
 #pragma unroll
-    for (int e = 0; e < S::KS; ++e)
+    for (int e = 0; e < Sizes<DP>::KS; ++e)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x, y;
-        widen_pair<DT>(raw[e][i], x, y);
+        widen_pair<DT>(query[b][e][i], x, y);
         x = __builtin_amdgcn_ldexpf(x, up), y = __builtin_amdgcn_ldexpf(y, up);
         whole += x + y;
         query[b][e][i] = i % 2 ? narrow_pair<KVC_F16>(x * 0.0625f, y * 0.0625f) : narrow_pair<KVC_F16>(x, y);
       }
     rows.whole[b] = row_sum(whole) * 5.9604644775390625e-8f;  // (2^-24, as the codes)
-    rows.unit[b] = __builtin_amdgcn_ldexpf(p.scale_log2, 24 - up);
-    rows.slack[b] = fminf(8.0f / rows.unit[b], 1e30f);
   }
+  rows.unit = __builtin_amdgcn_ldexpf(p.scale_log2, 24 - up);
 }
 
-template <int DP, int RB>
+// ---- up to 16 rows --------------------------------------------------------------------------------------------------------
+
+// LDS of a wave: the pairs of its tile, and in the end its sums.
+template <int DP>
 struct Lds {
-  struct {
-    f32x2 k[kTile], v[kTile];
-  } pairs[4];
-  float sums[4][16 * RB][DP];
-  float m[4][16 * RB], l[4][16 * RB];
+  union Wave {
+    PairSpace pairs;
+    float sums[16][DP];
+  } of[4];
+  float m[4][16], l[4][16];
 };
 
 // Element of a head that sum j of row i of a lane's is.
@@ -324,6 +428,81 @@ __device__ __forceinline__ uint32_t element_of(uint32_t g, int v, int j, int i) 
   return 8 * (16 * v + 4 * g + i) + j;
 }
 
+// A wave's sums into LDS, in vectors of four, and its rows' bases and sums of weights.
+template <int DP, int RB>
+__device__ __forceinline__ void put_sums(const State<DP, RB>& x, float (*sums)[DP], float* m, float* l) {
+  const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, g = lane >> 4;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const float total = row_sum(x.l[b]), off = x.total[b][0] + x.total[b][1] + x.total[b][2];
+    float* const to = sums[b * 16 + col];
+#pragma unroll
+    for (int v = 0; v < Sizes<DP>::VS; ++v)
+#pragma unroll
+      for (int j = 0; j < Sizes<DP>::NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = element_of<DP>(g, v, j, i);
+          to[((at / 4) ^ col) * 4 + at % 4] = x.sum[b][v][j][i] + off;
+        }
+    if (g == 0) {
+      m[b * 16 + col] = x.m[b] != kNone ? x.m[b] : total == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
+      l[b * 16 + col] = total;
+    }
+  }
+}
+
+// Writes a block's rows: PARTS waves have sums of each of them, THREADS threads write.
+template <int DT, int DP, int ROWS, int PARTS, int THREADS>
+__device__ __forceinline__ void write_rows(const AttendParams& p, bool shared, const Place& at_work, const Request& q, uint32_t new_tokens, uint32_t base_row,
+                                           const float (*sums)[ROWS][DP], const float (*m)[ROWS], const float (*l)[ROWS], uint32_t self) {
+  constexpr uint32_t QD = DP / 4, SIDE = THREADS / QD;
+  const uint32_t at = self % QD;
+#pragma unroll 1
+  for (uint32_t r = self / QD; r < ROWS; r += SIDE) {
+    uint32_t t, k;
+    fd_divmod(p.dG, base_row + r, t, k);
+    if (t >= new_tokens) break;
+    float share[PARTS], top = kNone, total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) top = fmaxf(top, m[i][r]);
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      share[i] = m[i][r] == kNone ? -1.0f : weight(m[i][r], top);  // (below 0: the wave saw nothing)
+      if (m[i][r] != kNone) total += share[i] * l[i][r];
+    }
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      const f32x4 v = *(const f32x4*)&sums[i][r][(at ^ (r & 15u)) * 4];
+      if (!(share[i] < 0.0f)) o += share[i] * v;
+    }
+    const uint32_t token = shared ? t : q.first + t, head = at_work.head * p.G + k;
+    if (p.pieces > 1) {
+      const uint32_t piece = shared ? at_work.split : p.part[0].splits + at_work.split;
+      const uint64_t slot = ((uint64_t)piece * p.batch.n_new + token) * (p.H * p.G) + head;
+      if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
+      if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
+    } else {
+      const float y = total == 0.0f ? 0.0f : 1.0f / total;
+      uint16_t* const to = p.out + (int64_t)token * p.o_token + (int64_t)head * p.o_head + at * 4;
+      if (at * 4 < p.D) *(KVC_GLOBAL u32x2*)to = u32x2{narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
+      if (at == 0 && p.lse) p.lse[(uint64_t)token * (p.H * p.G) + head] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+    }
+  }
+}
+
+// Where a head's codes and pairs lie.
+template <bool BIG>
+__device__ __forceinline__ void place_of_head(const AttendParams& p, uint32_t head, Unit<BIG>& u) {
+  const uint64_t block = p.pool.block_size, W = p.D / 8;
+  const uint8_t KVC_GLOBAL* const layer = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer];
+  u.codes = layer + head * block * W * 4;
+  u.pairs = layer + (p.H * W + head) * block * 4;
+  u.values = (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
+  u.quad_bytes = (uint32_t)W * 16;
+}
+
 // From the lanes' rows to all of a block's: the most and the least that one sees.
 __device__ __forceinline__ void lanes_see(uint32_t& most, uint32_t& least) {
 #pragma unroll
@@ -333,11 +512,12 @@ __device__ __forceinline__ void lanes_see(uint32_t& most, uint32_t& least) {
   }
 }
 
-// One unit: 16 RB rows x head x piece of the tokens; a workgroup's, whose waves have every fourth tile, or (LONE) a wave's.
-template <int DT, int DP, int RB, bool BIG, bool LONE>
-__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, Lds<DP, RB>& lds) {
+// One unit: 16 rows x head x piece of the tokens; a workgroup's, whose waves have every fourth tile, or (LONE) a wave's.
+template <int DT, int DP, bool BIG, bool LONE>
+__device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, Lds<DP>& lds) {
   using S = Sizes<DP>;
-  constexpr uint32_t ROWS = 16 * RB;
+  constexpr int RB = 1;
+  constexpr uint32_t ROWS = 16;
   const uint32_t lane = threadIdx.x & 63u, wave = wave_uniform(threadIdx.x >> 6), col = lane & 15u, g = lane >> 4;
   const uint32_t speaker = LONE ? lane : threadIdx.x;
   const Place at_work = place_of_unit(p, part, shared, unit);
@@ -372,22 +552,20 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     token[b] = (there[b] ? t : 0) + (shared ? 0 : min(q.first, p.batch.n_new - 1));
     from[b] = p.q + (int64_t)token[b] * p.q_token + (int64_t)(at_work.head * p.G + k) * p.q_head;
   }
-  const uint64_t block = p.pool.block_size, W = p.D / 8;
-  const uint8_t KVC_GLOBAL* const layer = (const uint8_t KVC_GLOBAL*)as_const(p.pool.layers)[p.layer];
-  u.codes = layer + at_work.head * block * W * 4;
-  u.pairs = layer + (p.H * W + at_work.head) * block * 4;
-  u.values = (uint64_t)p.pool.num_blocks * p.pool.page_bytes;
-  u.quad_bytes = (uint32_t)W * 16;
+  place_of_head(p, at_work.head, u);
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
   if (shared && u.t1 < p.prefix && speaker == 0) fault(p, KVC_FAULT_LIST);
   u.t1 = min(u.t1, u.t0 + part.tokens);
-  Tile<DP> tile[2];
-  if (start < u.t1) load_tile<DP, BIG>(p, u, start, page[0], tile[0]);
+  const bool has_tile = start < u.t1;
+  Tile<DP> tile;
+  Source<BIG> at_tile = source_of<BIG>(p, u, start, page[0]);
+  if (has_tile) {
+    load_keys<DP, BIG>(p, u, at_tile, tile);
+    load_values<DP, BIG>(p, u, at_tile, tile);
+  }
 
   // How far the rows see.
   Rows<RB> rows;
-  u32x4 query[RB][S::KS];
-  load_queries<DT, DP, RB>(p, from, there, query, rows);
   uint32_t most = 0, least = ~0u;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -401,120 +579,410 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   lanes_see(most, least);
   least = wave_uniform(least);
   const uint32_t end = min(u.t1, wave_uniform(most)), plain = min(least, u.t1);
+  u32x4 query[RB][S::KS];
+  make_queries<DT, DP, RB>(p, load_queries<DT, DP, RB>(p, from, query, rows), query, rows);
 
   State<DP, RB> x;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    x.m[b] = kNone;
-    x.l[b] = x.low[b] = 0.0f;
+    x.m[b] = there[b] ? kNone : 0.0f;  // (a row that is not there asks for no base)
+    x.l[b] = 0.0f;
     x.total[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int v = 0; v < S::VS; ++v)
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
   }
-  uint32_t missing = 0;
-  auto step = [&](uint32_t pos, const Tile<DP>& now, Tile<DP>& next, uint32_t& page_of_next) {
-    if (pos + NEXT < end) {
-      load_tile<DP, BIG>(p, u, pos + NEXT, page_of_next, next);
-      page_of_next = page_of_lane<BIG>(p, u, pos + 2 * NEXT);
-    }
-    missing |= now.missing;
-    f32x2 *const kpair = lds.pairs[wave].k, *const vpair = lds.pairs[wave].v;
-    if (pos + kTile <= plain && now.missing == 0) take_tile<DT, DP, RB, false>(p, pos, u.t1, now, rows, query, x, kpair, vpair);
-    else take_tile<DT, DP, RB, true>(p, pos, u.t1, now, rows, query, x, kpair, vpair);
-  };
-  for (uint32_t pos = start; pos < end;) {
-    step(pos, tile[0], tile[1], page[1]);
-    pos += NEXT;
-    tile[0] = tile[1];
+  PairSpace& pairs = lds.of[wave].pairs;
+  begin_pairs(pairs, lane);
+  uint32_t missing = 0, turned = 0;
+#pragma unroll 1
+  for (uint32_t pos = start; pos < end; pos += NEXT, turned ^= 1u) {
+    const uint32_t holes = at_tile.missing;
+    missing |= holes;
+    at_tile = source_of<BIG>(p, u, pos + NEXT, page[1]);  // (one that is not there reads page 0)
+    page[1] = page_of_lane<BIG>(p, u, pos + 2 * NEXT);
+    take_tile<DT, DP, RB, BIG>(p, u, pos + kTile > plain || holes, turned, pos, holes, at_tile, tile, rows, query, x, pairs);
   }
   if (missing && lane == 0) fault(p, KVC_FAULT_PAGE);
   if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
 
   // Results go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
-  if constexpr (!LONE) __syncthreads();
+  put_sums<DP, 1>(x, lds.of[wave].sums, lds.m[wave], lds.l[wave]);
+  if constexpr (LONE) {
+    __builtin_amdgcn_wave_barrier();
+    write_rows<DT, DP, 16, 1, 64>(p, shared, at_work, q, new_tokens, base_row, &lds.of[wave].sums, &lds.m[wave], &lds.l[wave], lane);
+  } else {
+    __syncthreads();
+    write_rows<DT, DP, 16, 4, 256>(p, shared, at_work, q, new_tokens, base_row, &lds.of[0].sums, lds.m, lds.l, threadIdx.x);
+  }
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------------------------
+//
+// Four waves side by side along the rows, 32 each, take the same tiles.  What a tile's codes become as operands is made once: each wave makes a quarter of it,
+// for the tile after the present one, into LDS, where an operand's 16 bytes a lane lie side by side.  One barrier a tile.
+
+template <int DP>
+struct Made {
+  u32x4 k[4][Sizes<DP>::KS][64];                       // operands of keys
+  u32x4 v[2][Sizes<DP>::VS][Sizes<DP>::NJ][64];        // and of values
+  PairSpace pairs;
+};
+
+constexpr int kRB = 2;  // blocks of 16 rows of a wave
+
+template <int DP>
+struct BlockLds {
+  union {
+    Made<DP> made[2];
+    float sums[4][16 * kRB][DP];
+  };
+  float m[4][16 * kRB], l[4][16 * kRB];
+  uint32_t most[4], seen[4];
+};
+
+// A wave's share of a tile's loads: keys' vectors, words of values of two quads, pairs.
+template <int DP>
+struct Share {
+  static constexpr int KE = DP > 128 ? 2 : 1;
+  u32x4 k[KE], v[Sizes<DP>::VS][2];
+  uint32_t kp, vp;
+};
+
+template <int DP, bool BIG>
+__device__ __forceinline__ void load_share(const AttendParams& p, const Unit<BIG>& u, const Source<BIG>& from, uint32_t wave, Share<DP>& t) {
+  const uint32_t lane = threadIdx.x & 63u, quad = lane & 15u, g = lane >> 4, W = p.D / 8;
+  const auto pair = of_lane(lane / 4, from.pairs) + (lane & 3u) * 4;
+  t.kp = *(const uint32_t KVC_GLOBAL*)(u.pairs + pair);
+  t.vp = *(const uint32_t KVC_GLOBAL*)(u.pairs + u.values + pair);
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const float low = row_sum(x.low[b]), total = row_sum(x.l[b]);
-    const float off = fmaf(-136.0f, x.total[b][0], low);
-    float* const to = lds.sums[wave][b * 16 + col];
+  for (int i = 0; i < Share<DP>::KE; ++i) {
+    const uint32_t e = DP == 64 ? wave & 1u : wave * Share<DP>::KE + i;
+    t.k[i] = *(const u32x4 KVC_GLOBAL*)(u.codes + (from.codes + min(e * 4 + g, W - 1) * 16));
+  }
 #pragma unroll
-    for (int v = 0; v < S::VS; ++v)
+  for (int i = 0; i < 2; ++i) {
+    const auto at = of_lane(g * 4 + (wave >> 1) * 2 + i, from.codes);
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j)
+    for (int s = 0; s < Sizes<DP>::VS; ++s)
+      t.v[s][i] = *(const u32x4 KVC_GLOBAL*)(u.codes + u.values + (at + min(DP == 64 ? quad & 7u : quad + 16 * s, W - 1) * 16));
+  }
+}
+
+// Makes a wave's share of a tile's operands.
+template <int DT, int DP>
+__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, float unit, uint32_t turned, Made<DP>& to) {
+  const uint32_t lane = threadIdx.x & 63u, h = wave >> 1;
+  if (wave == 0) put_key_pair<DT>(to.pairs, lane, t.kp, unit);
+  if (wave == 1) put_value_pair<DT>(to.pairs, lane, t.vp);
+  const uint64_t flat = __ballot((t.vp & 0x7fffu) == 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t at = element_of<DP>(g, v, j, i);
-          to[((at / 4) ^ col) * 4 + at % 4] = x.sum[b][v][j][i] + off;
-        }
-    if (g == 0) {
-      lds.m[wave][b * 16 + col] = x.m[b] != kNone ? x.m[b] * rows.unit[b] : total == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
-      lds.l[wave][b * 16 + col] = total;
+  for (int i = 0; i < Share<DP>::KE; ++i) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (DP == 64) {
+        if ((uint32_t)k >> 1 == h) to.k[k][wave & 1u][lane] = key_operand(t.k[0][k]);
+      } else {
+        to.k[k][wave * Share<DP>::KE + i][lane] = key_operand(t.k[i][k]);
+      }
     }
   }
-  if constexpr (!LONE) __syncthreads();
-  else __builtin_amdgcn_wave_barrier();
-  constexpr uint32_t QD = DP / 4, THREADS = LONE ? 64 : 256, SIDE = THREADS / QD, PARTS = LONE ? 1 : 4;
-  const uint32_t self = LONE ? lane : threadIdx.x, at = self % QD;
-  for (uint32_t r = self / QD; r < ROWS; r += SIDE) {
-    uint32_t t, k;
-    fd_divmod(p.dG, base_row + r, t, k);
-    if (t >= new_tokens) break;
-    float share[PARTS], top = kNone, total = 0.0f;
 #pragma unroll
-    for (uint32_t i = 0; i < PARTS; ++i) top = fmaxf(top, lds.m[LONE ? wave : i][r]);
+  for (int s = 0; s < Sizes<DP>::VS; ++s) {
+    u32x4 y = t.v[s][0], z = t.v[s][1];
+    if (flat) {  // (codes that a scale of 0 makes nothing of)
+      const uint32_t mine = (uint32_t)(flat >> (16 * (lane >> 4) + 8 * h));
 #pragma unroll
-    for (uint32_t i = 0; i < PARTS; ++i) {
-      const float m = lds.m[LONE ? wave : i][r];
-      share[i] = m == kNone ? -1.0f : weight(m, top);
-      if (m != kNone) total += share[i] * lds.l[LONE ? wave : i][r];
+      for (int k = 0; k < 4; ++k) {
+        y[k] = mine >> k & 1u ? 0u : y[k];
+        z[k] = mine >> (4 + k) & 1u ? 0u : z[k];
+      }
     }
-    f32x4 o = {0, 0, 0, 0};
+    if constexpr (DP == 64) {
+      const u32x4 both = halves(y, z, (lane & 8u) ? kHigh : kLow);
 #pragma unroll
-    for (uint32_t i = 0; i < PARTS; ++i) {
-      const f32x4 v = *(const f32x4*)&lds.sums[LONE ? wave : i][r][(at ^ (r & 15u)) * 4];
-      if (!(share[i] < 0.0f)) o += share[i] * v;
-    }
-    const uint32_t at_token = shared ? t : q.first + t, head = at_work.head * p.G + k;
-    if (p.pieces > 1) {
-      const uint32_t piece = shared ? at_work.split : p.part[0].splits + at_work.split;
-      const uint64_t slot = ((uint64_t)piece * p.batch.n_new + at_token) * (p.H * p.G) + head;
-      if (at * 4 < p.D) *(KVC_GLOBAL f32x4*)(p.sums + slot * p.D + at * 4) = o;
-      if (at == 0) *(KVC_GLOBAL f32x2*)(p.tops + slot * 2) = f32x2{top, total};
+      for (int n = 0; n < 4; ++n)
+        if ((uint32_t)n >> 1 == (wave & 1u)) to.v[h][s][n][lane] = value_operand(both, n, turned);
     } else {
-      const float y = total == 0.0f ? 0.0f : 1.0f / total;
-      uint16_t* const to = p.out + (int64_t)at_token * p.o_token + (int64_t)head * p.o_head + at * 4;
-      if (at * 4 < p.D) *(KVC_GLOBAL u32x2*)to = u32x2{narrow_pair<DT>(o.x * y, o.y * y), narrow_pair<DT>(o.z * y, o.w * y)};
-      if (at == 0 && p.lse) p.lse[(uint64_t)at_token * (p.H * p.G) + head] = total == 0.0f ? kNone : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+      const u32x4 both = halves(y, z, (wave & 1u) ? kHigh : kLow);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) to.v[h][s][2 * n + (wave & 1u)][lane] = value_operand(both, n, turned);
     }
   }
 }
 
+constexpr int kAhead = 2;  // pairs of operands that are read before the products that take them
+
+// The first pairs of a tile's operands of keys.
+template <int DP>
+__device__ __forceinline__ void read_first(const Made<DP>& made, u32x4 (&a)[kAhead + 1][2]) {
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) a[n][i] = made.k[2 * n / Sizes<DP>::KS][2 * n % Sizes<DP>::KS + i][threadIdx.x & 63u];
+}
+
+// A tile that has been made.  Operands are read from LDS some products ahead of those that take them; the order is the source's.  ask(): a call in between.
+template <int DT, int DP, typename Ask>
+__device__ __forceinline__ void take_made(bool masked, uint32_t turned, uint32_t at, uint32_t t1, uint32_t missing, const Made<DP>& made, const Rows<kRB>& rows,
+                                          const u32x4 (&query)[kRB][Sizes<DP>::KS], State<DP, kRB>& x, u32x4 (&a)[kAhead + 1][2], Ask ask) {
+  using S = Sizes<DP>;
+  constexpr int KS = S::KS, NV = S::VS * S::NJ, RING = kAhead + 1;
+  const uint32_t lane = threadIdx.x & 63u;
+  f32x4 s[kRB][4];
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int n = 0; n < 2 * KS; ++n) {
+    const int k = 2 * n / KS, first = 2 * n % KS, m = n + kAhead;
+    if (m < 2 * KS) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) a[m % RING][i] = made.k[2 * m / KS][2 * m % KS + i][lane];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < kRB; ++b) s[b][k] = mfma_f16(a[n % RING][i], query[b][first + i], first + i ? s[b][k] : f32x4{0, 0, 0, 0});
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __builtin_amdgcn_s_setprio(0);
+  ask();
+  __builtin_amdgcn_sched_barrier(0);
+  u32x4 w[kRB][2], fine[kRB][2];
+#pragma unroll
+  for (int b = 0; b < kRB; ++b) {
+    if (b == kRB - 1) {
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) a[n][i] = ((const u32x4(*)[64])made.v)[2 * n + i][lane];
+    }
+    weights<DT, DP, kRB>(masked, at, t1, missing, made.pairs, rows, b, s[b], x, w[b], fine[b]);
+  }
+  const u32x4(*const values)[64] = (const u32x4(*)[64])made.v;
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int h = 2 * n / NV, first = 2 * n % NV, m = n + kAhead;
+    if (m < NV) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) a[m % RING][i] = values[2 * m + i][lane];
+    }
+    if (first == 0) {
+      const u32x4 rows_of_sums = sums_operand(made.pairs, h, turned);
+#pragma unroll
+      for (int b = 0; b < kRB; ++b) {
+        add_product(rows_of_sums, w[b][h], x.total[b]);
+        if constexpr (DT == KVC_F16) add_product(rows_of_sums, fine[b][h], x.total[b]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < kRB; ++b) {
+        f32x4& sum = x.sum[b][(first + i) / S::NJ][(first + i) % S::NJ];
+        add_product(a[n % RING][i], w[b][h], sum);
+        if constexpr (DT == KVC_F16) add_product(a[n % RING][i], fine[b][h], sum);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __builtin_amdgcn_s_setprio(0);
+}
+
+// One unit: 128 rows x head x piece of the tokens.
 template <int DT, int DP, bool BIG>
-__global__ void __launch_bounds__(256) attend_held_kernel(AttendParams p) {
-  constexpr int MOST = DP > 128 ? 1 : 2;
-  __shared__ Lds<DP, MOST> lds;
+__device__ __forceinline__ void attend_block(const AttendParams& p, const AttendPart& part, const bool shared, uint32_t unit, BlockLds<DP>& lds) {
+  using S = Sizes<DP>;
+  constexpr uint32_t ROWS = 16 * kRB;
+  const uint32_t lane = threadIdx.x & 63u, wave = wave_uniform(threadIdx.x >> 6), col = lane & 15u, g = lane >> 4;
+  const Place at_work = place_of_unit(p, part, shared, unit);
+
+  Request q{};
+  if (!shared) q = request_at(p, at_work.request);
+  const uint32_t new_tokens = shared ? p.batch.n_new : covered(p, q);
+  if (!shared && p.pieces == 1 && at_work.block == 0 && q.faults)  // (of several pieces the join writes what these rows hold)
+    write_uncovered(p, q, at_work.request, at_work.head, threadIdx.x, 256);
+  if (!shared && at_work.block * (4 * ROWS) >= wave_uniform(new_tokens) * p.G) {  // (a request with fewer new tokens than others)
+    if (threadIdx.x == 0) fault(p, q.faults);
+    return;
+  }
+  Unit<BIG> u;
+  u.bound = shared ? p.prefix : p.most_tokens;
+  u.t0 = (shared ? 0 : p.own_from) + at_work.split * part.tokens;
+  u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
+  uint32_t page[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) page[i] = page_of_lane<BIG>(p, u, u.t0 + i * kTile);
+
+  const uint32_t base_row = (at_work.block * 4 + wave) * ROWS;
+  const uint16_t* from[kRB];
+  bool there[kRB];
+  uint32_t token[kRB];
+#pragma unroll
+  for (int b = 0; b < kRB; ++b) {
+    uint32_t t, k;
+    fd_divmod(p.dG, base_row + b * 16 + col, t, k);
+    there[b] = t < new_tokens;
+    token[b] = (there[b] ? t : 0) + (shared ? 0 : min(q.first, p.batch.n_new - 1));
+    from[b] = p.q + (int64_t)token[b] * p.q_token + (int64_t)(at_work.head * p.G + k) * p.q_head;
+  }
+  place_of_head(p, at_work.head, u);
+  u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
+  if (shared && u.t1 < p.prefix && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
+  u.t1 = min(u.t1, u.t0 + part.tokens);
+  // (a tile that is not there is read from page 0)
+  Share<DP> share;
+  Source<BIG> source = source_of<BIG>(p, u, u.t0, page[0]);
+  uint32_t holes = source.missing, next_holes;  // of the present tile and the next one
+  load_share<DP, BIG>(p, u, source, wave, share);
+
+  // How far the rows see.
+  Rows<kRB> rows;
+  uint32_t most = 0, least = ~0u;
+#pragma unroll
+  for (int b = 0; b < kRB; ++b) {
+    Request r = q;
+    if (shared) r = request_at(p, request_of(p.batch, token[b]));
+    if (shared ? there[b] && at_work.split == 0 && at_work.head == 0 && g == 0 : threadIdx.x == 0 && b == 0) fault(p, r.faults);
+    rows.limit[b] = there[b] ? limit_of(p, r, token[b]) : 0;
+    most = max(most, rows.limit[b]);
+    if (there[b]) least = min(least, rows.limit[b]);
+  }
+  lanes_see(most, least);
+  most = wave_uniform(most), least = wave_uniform(least);
+  u32x4 query[kRB][S::KS];
+  uint32_t largest = load_queries<DT, DP, kRB>(p, from, query, rows);
+  if (lane == 0) lds.most[wave] = largest, lds.seen[wave] = most;
+  meet();
+  largest = wave_uniform(max(max(lds.most[0], lds.most[1]), max(lds.most[2], lds.most[3])));
+  const uint32_t end = min(u.t1, wave_uniform(max(max(lds.seen[0], lds.seen[1]), max(lds.seen[2], lds.seen[3]))));
+  const uint32_t mine = min(u.t1, most), plain = min(least, u.t1);
+  make_queries<DT, DP, kRB>(p, largest, query, rows);
+
+  State<DP, kRB> x;
+#pragma unroll
+  for (int b = 0; b < kRB; ++b) {
+    x.m[b] = there[b] ? kNone : 0.0f;  // (a row that is not there asks for no base)
+    x.l[b] = 0.0f;
+    x.total[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int v = 0; v < S::VS; ++v)
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
+  }
+  if (wave == 0) begin_pairs(lds.made[0].pairs, lane), begin_pairs(lds.made[1].pairs, lane);
+  uint32_t missing = 0;
+  if (u.t0 < end) make_share<DT, DP>(share, wave, rows.unit, 0, lds.made[0]);
+  source = source_of<BIG>(p, u, u.t0 + kTile, page[1]);
+  next_holes = source.missing;
+  load_share<DP, BIG>(p, u, source, wave, share);
+  uint32_t turn = 0;
+#pragma unroll 1
+  for (uint32_t pos = u.t0; pos < end; pos += kTile, turn ^= 1u) {
+    const Made<DP>& now = lds.made[turn];
+    meet();  // what is in `now` is there, and the other one has been read
+    u32x4 first[kAhead + 1][2];
+    read_first<DP>(now, first);
+    if (pos + kTile < end) make_share<DT, DP>(share, wave, rows.unit, turn ^ 1u, lds.made[turn ^ 1u]);
+    __builtin_amdgcn_sched_barrier(0);
+    missing |= holes;
+    auto ask = [&]() {
+      source = source_of<BIG>(p, u, pos + 2 * kTile, page[2]);
+      load_share<DP, BIG>(p, u, source, wave, share);
+      page[2] = page_of_lane<BIG>(p, u, pos + 3 * kTile);
+    };
+    if (pos >= mine) ask();
+    else take_made<DT, DP>(pos + kTile > plain || holes, turn, pos, u.t1, holes, now, rows, query, x, first, ask);
+    holes = next_holes;
+    next_holes = source.missing;
+  }
+  if (missing && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
+  if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
+  meet();  // the sums lie where the operands were
+  put_sums<DP, kRB>(x, lds.sums[wave], lds.m[wave], lds.l[wave]);
+  __builtin_amdgcn_wave_barrier();
+  write_rows<DT, DP, ROWS, 1, 64>(p, shared, at_work, q, new_tokens, base_row, &lds.sums[wave], &lds.m[wave], &lds.l[wave], lane);
+}
+
+// BLOCKS: a part has four waves side by side.
+template <int DT, int DP, bool BIG, bool BLOCKS>
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : BLOCKS ? 2 : 3) attend_held_kernel(AttendParams p) {
+  union Both {
+    Lds<DP> few;
+    typename std::conditional<BLOCKS, BlockLds<DP>, uint32_t>::type many;
+  };
+  __shared__ __align__(16) uint8_t memory[sizeof(Both)];
+  Both& lds = *reinterpret_cast<Both*>(memory);
   bool shared;
   uint32_t unit;
   if (!unit_of(p, shared, unit)) return;
   const AttendPart& part = p.part[shared ? 0 : 1];
-  Lds<DP, 1>& small = *reinterpret_cast<Lds<DP, 1>*>(&lds);
+  if constexpr (BLOCKS) {
+    if (part.waves == 4) {
+      attend_block<DT, DP, BIG>(p, part, shared, unit, lds.many);
+      return;
+    }
+  }
   if (part.lone) {
     unit = unit * 4 + wave_uniform(threadIdx.x >> 6);
-    if (unit < part.lone) attend_unit<DT, DP, 1, BIG, true>(p, part, shared, unit, small);
-  } else if (MOST == 1 || part.waves == 1) attend_unit<DT, DP, 1, BIG, false>(p, part, shared, unit, small);
-  else attend_unit<DT, DP, MOST, BIG, false>(p, part, shared, unit, lds);
+    if (unit < part.lone) attend_unit<DT, DP, BIG, true>(p, part, shared, unit, lds.few);
+  } else {
+    attend_unit<DT, DP, BIG, false>(p, part, shared, unit, lds.few);
+  }
 }
 
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   const uint32_t groups = (uint32_t)attend_groups(p);
   const bool big = (uint64_t)p.pool.num_blocks * p.pool.page_bytes >> 32;
-  if (groups && big) hipLaunchKernelGGL((attend_held_kernel<DT, DP, true>), dim3(groups), dim3(256), 0, stream, p);
-  if (groups && !big) hipLaunchKernelGGL((attend_held_kernel<DT, DP, false>), dim3(groups), dim3(256), 0, stream, p);
+  const bool blocks = p.part[0].waves == 4 || p.part[1].waves == 4;
+  if (groups && big && blocks) hipLaunchKernelGGL((attend_held_kernel<DT, DP, true, true>), dim3(groups), dim3(256), 0, stream, p);
+  else if (groups && big) hipLaunchKernelGGL((attend_held_kernel<DT, DP, true, false>), dim3(groups), dim3(256), 0, stream, p);
+  else if (groups && blocks) hipLaunchKernelGGL((attend_held_kernel<DT, DP, false, true>), dim3(groups), dim3(256), 0, stream, p);
+  else if (groups) hipLaunchKernelGGL((attend_held_kernel<DT, DP, false, false>), dim3(groups), dim3(256), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return KVC_ERR_RUNTIME;
   return p.pieces == 1 ? KVC_OK : launch_join(p, stream);
+}
+
+}  // namespace
+
+namespace {
+
+// What a part of the work takes in units of 16 or 128 rows and of so many tokens each.
+struct Shape {
+  uint32_t waves;  // that stand side by side along the rows: 1 or 4
+  uint64_t blocks, splits, each;
+  double time;  // us, roughly
+};
+
+// The times are a fit to calls of 1 to 128 requests over 50 to 32K tokens: with c workgroups to a CU a unit takes `start` and, for each token, `alone` and `shared` c times.
+// (Which body is taken is worth up to a factor of two: 24 rows over 4000 tokens of 32 heads 26 us in units of 16 rows, 39 in units of 128; 10 000 rows over 32K of 8
+// heads 2.00 and 1.69 ms.  How the tokens are cut: one row over 32K tokens of 8 heads in 14 or 42 pieces 27 or 22.7 us.)
+Shape shape_of(const AttendParams& p, uint32_t waves, uint64_t tokens, uint64_t rows, uint64_t requests, bool joined) {
+  Shape best{};
+  if (tokens == 0) return best;
+  const bool many = waves == 4;
+  const double size = p.D <= 64 ? 0.7 : p.D <= 128 ? 1.0 : 2.0, start = many ? 3.0 : 4.0;
+  const double alone = size * (many ? 0.0048 : 0.0018), shared = size * (many ? (p.dtype == KVC_F16 ? 0.0218 : 0.019) : 0.0025);
+  const uint64_t most = p.D > 128 ? 1 : many ? 2 : 3;  // workgroups to a CU
+  const uint64_t step = many ? kTile : 4 * kTile, block = many ? 64 * kRB : 16;
+  best.waves = waves;
+  best.time = 1e300;
+  best.blocks = (rows + block - 1) / block;
+  const double whole = (double)best.blocks * p.H * requests, lines = (double)p.batch.n_new * p.H * p.G;
+  for (uint64_t splits = 1, last = 0; splits <= 256; ++splits) {
+    const uint64_t each = ((tokens + splits - 1) / splits + step - 1) / step * step, pieces = (tokens + each - 1) / each;
+    if (each == last) continue;
+    last = each;
+    // (rows of their own are of all lengths: little more than half of the units' tokens are there)
+    const double units = whole * pieces * (requests > 1 ? 0.6 : 1.0), slots = 256.0 * most;
+    const double full = floor(units / slots), rest = units - full * slots;
+    double time = full * (each * (alone + shared * most) + start);
+    if (rest > 0 || full == 0) time += each * (alone + shared * ceil(rest > 0 ? rest / 256 : 1)) + start;
+    if (pieces > 1 || joined) time += (joined ? 0 : 3) + lines * pieces * p.D * 8 / 6e6;  // sums of pieces, written and read
+    if (time < best.time) best.time = time, best.each = each, best.splits = pieces;
+  }
+  return best;
 }
 
 }  // namespace
@@ -523,31 +991,39 @@ kvc_status plan_attend_held(AttendParams& p) {
   p.pieces = 0;
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = p.lift = 0.0f;
-  const uint64_t chip = 512;  // workgroups that run at a time
   // Tiles lie on quads of the pages: up to three last tokens of a prefix that ends inside one are read through each row's own table, which has them too.
   p.prefix &= ~3u;
   p.own_from = p.prefix;
+  const uint64_t tokens[2] = {p.own_from, p.most_tokens - p.own_from}, requests[2] = {1, p.batch.n_requests};
+  const uint64_t rows[2] = {(uint64_t)p.batch.n_new * p.G, (uint64_t)p.batch.most_new * p.G};
+  Shape few[2], many[2];
+  for (int i = 0; i < 2; ++i) {
+    if (tokens[i] && (rows[i] + 15) / 16 * p.H * requests[i] >> 31) return KVC_ERR_UNSUPPORTED;
+    few[i] = shape_of(p, 1, tokens[i], rows[i], requests[i], tokens[1 - i] > 0);
+    many[i] = rows[i] > 16 ? shape_of(p, 4, tokens[i], rows[i], requests[i], tokens[1 - i] > 0) : few[i];
+    // (in a kernel that has both bodies the first one has fewer waves to a CU)
+    if (few[i].time * 1.2 < many[i].time) many[i] = few[i], many[i].time *= 1.2;
+  }
+  const bool both = many[0].time + many[1].time < few[0].time + few[1].time;
   for (int i = 0; i < 2; ++i) {
     AttendPart& a = p.part[i];
     a = AttendPart{};
-    const uint64_t tokens = i == 0 ? p.own_from : p.most_tokens - p.own_from;
-    const uint64_t rows = (uint64_t)(i == 0 ? p.batch.n_new : p.batch.most_new) * p.G;
-    a.waves = rows <= 16 || p.D > 128 ? 1 : 2;  // blocks of 16 rows
-    const uint64_t each_block = a.waves * 16, blocks = (rows + each_block - 1) / each_block;
-    const uint64_t whole = blocks * p.H * (i == 0 ? 1 : p.batch.n_requests);
     a.drows = a.dsplits = a.drequests = make_fastdiv(1);
-    if (tokens == 0) continue;
-    if (whole >> 31) return KVC_ERR_UNSUPPORTED;
-    uint64_t splits = whole <= chip ? chip / whole : 1;
-    uint64_t each = (tokens + splits - 1) / splits;
-    const uint64_t least = 4 * kTile;
-    each = (each + least - 1) / least * least;
-    splits = (tokens + each - 1) / each;
-    if (whole * splits >> 31) return KVC_ERR_UNSUPPORTED;
-    a.row_blocks = (uint32_t)blocks;
-    a.splits = (uint32_t)splits;
-    a.tokens = (uint32_t)each;
-    a.units = (uint32_t)(whole * splits);
+    if (tokens[i] == 0) continue;
+    const Shape s = both ? many[i] : few[i];
+    const uint64_t units = s.blocks * p.H * requests[i] * s.splits;
+    if (units >> 31) return KVC_ERR_UNSUPPORTED;
+    a.waves = s.waves;
+    a.row_blocks = (uint32_t)s.blocks;
+    a.splits = (uint32_t)s.splits;
+    a.tokens = (uint32_t)s.each;
+    a.units = (uint32_t)units;
+    // A wave each has a unit of few tokens where there are many (64 rows of 32 heads with up to 300 tokens over a prefix of 500: 45 -> 35 us; with pieces of 1024, 128 rows
+    // of 8 heads 31 -> 36, so these keep a workgroup).
+    if (i == 1 && a.waves == 1 && s.each <= 512 && units >= 512) {
+      a.lone = a.units;
+      a.units = (a.units + 3) / 4;
+    }
     a.drows = make_fastdiv(a.row_blocks);
     a.dsplits = make_fastdiv(a.splits);
     a.drequests = make_fastdiv(p.batch.n_requests);
