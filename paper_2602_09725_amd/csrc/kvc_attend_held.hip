@@ -1,15 +1,16 @@
 // Attention of a batch over pages held in 4 bits (kvc_attend_paged on a pool of KVC_HELD_Q4).
 //
-// A token's key is k = s c + m with codes c of 0 .. 15 and a pair (s, m) of its head, so that q . k = s (q . c) + m sum(q); its value likewise, so that
-//   sum_t w_t v_t = sum_t (w_t s_t) (c_t - 8) + sum_t (w_t s_t) z_t,  z = m / s + 8.
-// Codes go into the matrix unit as they are: the products with keys are of exact numbers, and nothing is dequantized element by element.
-//   Keys: four bits in the low mantissa bits of an fp16 number are c 2^-24, a subnormal that the matrix unit takes exactly; the next four bits are c 2^-20.  Queries are
-//   made fp16 numbers by a power of two that all rows of a workgroup share (exact but for what lies 2^-35 below the largest of their elements), those that meet the
-//   second kind a sixteenth of it.
-//   Values: four bits in the mantissa of 128 are 128 + c in bf16.  Weights w s are rounded to bf16 (half a step, as the inputs of such a pool have), or for a pool
-//   of fp16 to two of them, which hold 16 bits.  One more product has rows of -136 and of z (in two bf16 numbers): what takes the offset off, and the second term,
-//   of the rounded weights.
-// A weight's rounding so counts by the distance from the middle of the codes, not from 0.
+// A token's key is k = s (c - 8) + (m + 8 s) with codes c of 0 .. 15 and a pair (s, m) of its head, so that q . k = s (q . (c - 8)) + (m + 8 s) sum(q); its value
+// likewise, so that, with z = m / s + 8,
+//   sum_t w_t v_t = sum_t (w_t s_t) (c_t - 8) + sum_t (w_t s_t) z_t.
+// Codes go into the matrix unit as they are: nothing is dequantized element by element, and the products with keys are of exact numbers, whose sums are
+// no larger than the products that they stand for.
+//   Four bits in the low mantissa bits of 1024 are 1024 + c in fp16, the next four bits 1024 + 16 c; one instruction takes 1032 or 1152 off two of them.
+//   (Without the 1024 they are c 2^-24, subnormals that the matrix unit takes as well; but sums of such products have been seen to hold some 14 bits only.)
+//   Queries are made fp16 numbers by a power of two that all rows of a workgroup share (exact but for what lies 2^-35 below the largest of their elements), those that
+//   meet the second kind a sixteenth of it.
+//   Weights w s, with s in the exponent, are rounded to fp16 (an eighth of the step that a bf16 pool's results have), or for a pool of fp16 to two such numbers, which
+//   hold 22 bits.  One more product has rows of z (in two numbers): it sums the second term of the same rounded weights.
 //
 // A tile is 64 tokens.  S^T = K Q^T and O^T += V^T W^T are 16x16x32 products: a lane has one row (lane % 16), and of a tile the 16 tokens from
 // 16 (lane / 16) on.  A page has each word of four tokens side by side (a quad), so that a lane's 16 bytes are the operands of four products with keys, and
@@ -30,20 +31,11 @@ namespace kvc {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+__device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Adds a product to a sum.
-__device__ __forceinline__ void add_product(u32x4 a, u32x4 b, f32x4& sum) {
-  sum = mfma_bf16(a, b, sum);
-}
-
 constexpr uint32_t kTile = 64;  // tokens
 
 // Sizes of a body: DP elements of a head at most, RB blocks of 16 rows.
@@ -91,14 +83,15 @@ struct Tile {
 
 // What the pairs of a tile's tokens give.
 struct alignas(16) PairSpace {
-  float ks[kTile], km[kTile], vs[kTile];  // scale and least value of keys, times what a product is multiplied with; scale of values
-  uint16_t z[4][kTile];                   // rows of the product that sums weights, bf16: -136, z, what is left of it, 135
+  float ks[kTile], km[kTile];  // scale and m + 8 s of keys, times what a product is multiplied with
+  float lv[kTile], rv[kTile];  // logarithm and reciprocal of the scale of values
+  uint16_t z[2][kTile];        // rows of the product that sums weights, fp16: z, what is left of it
 };
 
 template <int DP, int RB>
 struct State {
-  float m[RB], l[RB];  // a number near the largest exponent, sum of this lane's weights
-  f32x4 total[RB];     // what the rounded weights add to all elements, in three parts
+  float m[RB], l[RB];  // a number near the largest exponent of a weight times its value's scale, sum of this lane's weights
+  f32x4 total[RB];     // what the rounded weights add to all elements, in two parts
   f32x4 sum[RB][Sizes<DP>::VS][Sizes<DP>::NJ];
 };
 
@@ -158,16 +151,16 @@ __device__ __forceinline__ void load_values(const AttendParams& p, const Unit<BI
   }
 }
 
-// A scale, and the least value in steps of it.  A head whose values are all alike has scale 0: it is given its value's size for a scale.
+// A head whose values are all alike has scale 0.  It is given a scale of its value's size, and codes of 0 (as one whose least value is beyond 2^15 steps, which no
+// values of 16 bits have).
+__device__ __forceinline__ bool is_flat(float s, float m) { return fabsf(m) * 3.0517578125e-5f >= s; }
+
+// The least value in steps of the scale.
 __device__ __forceinline__ void steps_of(float& s, float m, float& z) {
-  if (s == 0.0f) {
-    s = fabsf(m);
-    z = m == 0.0f ? 0.0f : copysignf(1.0f, m);
-  } else {
-    const float r = __builtin_amdgcn_rcpf(s);
-    z = m * r;
-    z = fmaf(fmaf(-z, s, m), r, z);
-  }
+  if (is_flat(s, m)) s = fmaxf(fabsf(m), 8.67361738e-19f);  // (2^-60: its reciprocal, and sums of it, are numbers)
+  const float r = __builtin_amdgcn_rcpf(s);
+  z = m * r;
+  z = fmaf(fmaf(-z, s, m), r, z);
 }
 
 template <int DT>
@@ -175,33 +168,47 @@ __device__ __forceinline__ void put_key_pair(PairSpace& to, uint32_t token, uint
   float s, m;
   widen_pair<DT>(pair, s, m);
   to.ks[token] = s * unit;
-  to.km[token] = m * unit;
+  to.km[token] = fmaf(8.0f, s, m) * unit;
 }
 
-// Returns whether the token's scale is 0.  A pair that is not finite makes NaN of the weights that see it, and nothing of the others.
+// Tokens of a tile whose values are flat; pair: token `lane`'s.
 template <int DT>
-__device__ __forceinline__ bool put_value_pair(PairSpace& to, uint32_t token, uint32_t pair) {
+__device__ __forceinline__ uint64_t flat_tokens(uint32_t pair) {
+  float s, m;
+  widen_pair<DT>(pair, s, m);
+  return __ballot(is_flat(s, m));
+}
+
+// A pair that is not finite makes NaN of the weights that see it, and nothing of the others.
+template <int DT>
+__device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, uint32_t pair) {
   constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
   const bool wild = (pair & kExp) == kExp || (pair >> 16 & kExp) == kExp;
   float s, m, z;
   widen_pair<DT>(pair, s, m);
-  const bool flat = s == 0.0f;
   steps_of(s, m, z);
   z = wild ? 0.0f : z + 8.0f;
-  to.vs[token] = wild ? __builtin_nanf("") : s;
-  const uint32_t high = narrow_pair<KVC_BF16>(z, 0.0f);
-  to.z[1][token] = (uint16_t)high;
-  to.z[2][token] = (uint16_t)narrow_pair<KVC_BF16>(z - widen_bits<KVC_BF16>(high & 0xffffu), 0.0f);
-  return flat;
+  to.lv[token] = wild ? __builtin_nanf("") : __builtin_amdgcn_logf(s);
+  to.rv[token] = __builtin_amdgcn_rcpf(s);
+  const uint32_t high = narrow_pair<KVC_F16>(z, 0.0f);
+  to.z[0][token] = (uint16_t)high;
+  to.z[1][token] = (uint16_t)narrow_pair<KVC_F16>(z - widen_bits<KVC_F16>(high & 0xffffu), 0.0f);
 }
 
-// Rows of the pair space that are the same for all tiles.
-__device__ __forceinline__ void begin_pairs(PairSpace& to, uint32_t token) { to.z[0][token] = 0xc308, to.z[3][token] = 0x4307; }
+// Codes c in the low mantissa bits of two halves, or c 16 in those above -> c - 8 or 16 (c - 8): 1024 and more, less 1032 or 1152.
+template <int SHIFT>
+__device__ __forceinline__ uint32_t centred(uint32_t w) {
+  uint32_t mask = SHIFT ? 0x00f000f0u : 0x000f000fu, big = 0x64006400u;  // (in registers, so that one instruction takes both)
+  asm("" : "+s"(mask));
+  asm("" : "+v"(big));
+  const uint32_t codes = (w & mask) | big, less = SHIFT ? 0x64806480u : 0x64086408u;
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2v, codes) - __builtin_bit_cast(f16x2v, less));
+}
 
 // Eight codes -> an operand of the products with keys.
 __device__ __forceinline__ u32x4 key_operand(uint32_t w) {
   const uint32_t h = w >> 8;
-  return u32x4{w & 0x000f000fu, w & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u};
+  return u32x4{centred<0>(w), centred<4>(w), centred<0>(h), centred<4>(h)};
 }
 
 // Words of eight tokens -> two tokens' elements 2 n (or, with the selector's other value, 2 n + 1) side by side.
@@ -210,30 +217,30 @@ __device__ __forceinline__ u32x4 halves(u32x4 y, u32x4 z, uint32_t selector) {
                __builtin_amdgcn_perm(z.w, z.z, selector)};
 }
 constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-// Tiles take turns: of the even ones operands are 128 + c, of the odd ones c - 143, so that what is not c - 8 of them nearly cancels in the sums, which
-// fp32 would else lose the rest of in long rows.  turned: 0 or 1.
-__device__ __forceinline__ u32x4 value_operand(u32x4 both, int n, uint32_t turned) {
-  const uint32_t with = turned ? 0xc30fc30fu : 0x43004300u;
-  uint32_t mask = 0x000f000fu;
-  asm("" : "+s"(mask));
-  return u32x4{(both.x >> 4 * n & mask) ^ with, (both.y >> 4 * n & mask) ^ with, (both.z >> 4 * n & mask) ^ with, (both.w >> 4 * n & mask) ^ with};
+// (Elements of odd n come 16 times too large.)
+__device__ __forceinline__ u32x4 value_operand(u32x4 both, int n) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = n % 2 ? centred<4>(both[i] >> n / 2 * 8) : centred<0>(both[i] >> n / 2 * 8);
+  return r;
 }
-
-constexpr float kMost = 16.0f;  // exponents of up to this leave the base as it is
+template <int DP>
+constexpr float size_of(int j) { return (DP == 64 ? j : j / 2) % 2 ? 0.0625f : 1.0f; }
 
 // Weights of a tile from its products s[k][i], those of token 16 g + 4 i + k (they are overwritten): operands w[h] of tokens 16 g + 8 h .. + 7, and for fp16
 // what their rounding left.  masked: not all of it is there and seen by all rows (wave-uniform); missing: quads on no page.  The number subtracted from an exponent need not be
-// the largest one: weights of up to 2^16 do no harm to sums in fp32 and to bf16.  (The order is the source's: a few of LDS's numbers at a time.)
+// the largest one, as long as no weight leaves fp16; so that small ones stay in it too it lies 2^8 below the product that moves it for a pool of fp16.  (The order is the source's: a few of LDS's numbers at a time.)
 template <int DT, int DP, int RB>
 __device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, uint32_t missing, const PairSpace& pairs, const Rows<RB>& rows, int b, f32x4 (&s)[4],
                                         State<DP, RB>& x, u32x4 (&w)[2], u32x4 (&fine)[2]) {
   const uint32_t g = (threadIdx.x & 63u) >> 4;
+  constexpr float kLift = DT == KVC_F16 ? 8.0f : 0.0f, kMost = DT == KVC_F16 ? 15.0f : 6.0f;
   const float shift = x.m[b] == kNone ? 0.0f : x.m[b];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const f32x4 ks = *(const f32x4*)&pairs.ks[16 * g + 4 * i], km = *(const f32x4*)&pairs.km[16 * g + 4 * i];
+    const f32x4 ks = *(const f32x4*)&pairs.ks[16 * g + 4 * i], km = *(const f32x4*)&pairs.km[16 * g + 4 * i], lv = *(const f32x4*)&pairs.lv[16 * g + 4 * i];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[k][i] = fmaf(s[k][i], ks[k], fmaf(km[k], rows.whole[b], -shift));
+    for (int k = 0; k < 4; ++k) s[k][i] = fmaf(s[k][i], ks[k], fmaf(km[k], rows.whole[b], lv[k] - shift));
     __builtin_amdgcn_sched_barrier(0);
   }
   if (masked) {
@@ -252,7 +259,7 @@ __device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, u
   if (__any(top > kMost || x.m[b] == kNone)) {
     top = row_max(top);
     const bool first = x.m[b] == kNone;
-    const float up = first ? (top == kNone ? 0.0f : top) : fmaxf(top, 0.0f), keep = __builtin_amdgcn_exp2f(first ? 0.0f : -up);
+    const float up = top == kNone ? 0.0f : first ? top - kLift : fmaxf(top - kLift, 0.0f), keep = __builtin_amdgcn_exp2f(first ? 0.0f : -up);
     if (!first || top != kNone) x.m[b] = shift + up;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -268,39 +275,39 @@ __device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, u
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    f32x4 vs = *(const f32x4*)&pairs.vs[16 * g + 4 * i];
+    f32x4 rv = *(const f32x4*)&pairs.rv[16 * g + 4 * i];
     if (masked) {  // (what is not seen may be held with anything)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) vs[k] = s[k][i] == kNone ? 0.0f : vs[k];
+      for (int k = 0; k < 4; ++k) rv[k] = s[k][i] == kNone ? 0.0f : rv[k];
     }
 #pragma unroll
     for (int k = 0; k < 4; k += 2) {
       const float y = __builtin_amdgcn_exp2f(s[k][i]), z = __builtin_amdgcn_exp2f(s[k + 1][i]);
-      x.l[b] += y + z;
-      const float a = y * vs[k], c = z * vs[k + 1];
-      const uint32_t r = narrow_pair<KVC_BF16>(a, c);
+      x.l[b] = fmaf(y, rv[k], fmaf(z, rv[k + 1], x.l[b]));
+      const uint32_t r = narrow_pair<KVC_F16>(y, z);
       w[i / 2][i % 2 * 2 + k / 2] = r;
       if constexpr (DT == KVC_F16)
-        fine[i / 2][i % 2 * 2 + k / 2] = narrow_pair<KVC_BF16>(a - widen_bits<KVC_BF16>(r & 0xffffu), c - widen_bits<KVC_BF16>(r >> 16));
+        fine[i / 2][i % 2 * 2 + k / 2] = narrow_pair<KVC_F16>(y - widen_bits<KVC_F16>(r & 0xffffu), z - widen_bits<KVC_F16>(r >> 16));
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// Operand of the product that sums weights: rows 4 i of what takes the codes' offset off, 4 i + 1 of z, 4 i + 2 of its rest; nobody looks at the others.
-__device__ __forceinline__ u32x4 sums_operand(const PairSpace& pairs, int h, uint32_t turned) {
-  const uint32_t lane = threadIdx.x & 63u, row = (lane & 3u) == 0 && turned ? 3u : lane & 3u;
-  return *(const u32x4*)&pairs.z[row][16 * (lane >> 4) + 8 * h];
+// Operand of the product that sums weights: even rows of z, odd ones of its rest.
+__device__ __forceinline__ u32x4 sums_operand(const PairSpace& pairs, int h) {
+  const uint32_t lane = threadIdx.x & 63u;
+  return *(const u32x4*)&pairs.z[lane & 1u][16 * (lane >> 4) + 8 * h];
 }
 
 // One tile of a wave's own.  The next tile's loads follow as soon as this one's have been used.
 template <int DT, int DP, int RB, bool BIG>
-__device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>& u, bool masked, uint32_t turned, uint32_t at, uint32_t missing, const Source<BIG>& next, Tile<DP>& t,
+__device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>& u, bool masked, uint32_t at, uint32_t missing, const Source<BIG>& next, Tile<DP>& t,
                                           const Rows<RB>& rows, const u32x4 (&query)[RB][Sizes<DP>::KS], State<DP, RB>& x, PairSpace& pairs) {
   using S = Sizes<DP>;
   const uint32_t lane = threadIdx.x & 63u, g = lane >> 4;
   put_key_pair<DT>(pairs, lane, t.kp, rows.unit);
-  const uint64_t flat = __ballot(put_value_pair<DT>(pairs, lane, t.vp));
+  put_value_pair<DT>(pairs, lane, t.vp);
+  const uint64_t flat = flat_tokens<DT>(t.vp);
   // (The order is the source's: left to itself the compiler makes all operands first, and has no registers for them.)
   f32x4 s[RB][4];
 #pragma unroll
@@ -309,7 +316,7 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>
     for (int e = 0; e < S::KS; ++e) {
       const u32x4 a = key_operand(t.k[e][k]);
 #pragma unroll
-      for (int b = 0; b < RB; ++b) s[b][k] = mfma_f16(a, query[b][e], e ? s[b][k] : f32x4{0, 0, 0, 0});
+      for (int b = 0; b < RB; ++b) s[b][k] = product(a, query[b][e], e ? s[b][k] : f32x4{0, 0, 0, 0});
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -321,7 +328,7 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>
     weights<DT, DP, RB>(masked, at, u.t1, missing, pairs, rows, b, s[b], x, w[b], fine[b]);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (flat) {  // (codes that a scale of 0 makes nothing of)
+  if (flat) {  // (codes that their scale makes nothing of)
     const uint32_t mine = (uint32_t)(flat >> (16 * g)) & 0xffffu;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -332,11 +339,11 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const u32x4 rows_of_sums = sums_operand(pairs, h, turned);
+    const u32x4 rows_of_sums = sums_operand(pairs, h);
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      add_product(rows_of_sums, w[b][h], x.total[b]);
-      if constexpr (DT == KVC_F16) add_product(rows_of_sums, fine[b][h], x.total[b]);
+      x.total[b] = product(rows_of_sums, w[b][h], x.total[b]);
+      if constexpr (DT == KVC_F16) x.total[b] = product(rows_of_sums, fine[b][h], x.total[b]);
     }
 #pragma unroll
     for (int v = 0; v < S::VS; ++v)
@@ -346,12 +353,12 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>
         const u32x4 both = halves(t.v[v][2 * h], t.v[v][2 * h + 1], DP == 64 ? ((lane & 8u) ? kHigh : kLow) : half ? kHigh : kLow);
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const u32x4 a = value_operand(both, n, turned);
+          const u32x4 a = value_operand(both, n);
           const int j = DP == 64 ? n : 2 * n + half;
 #pragma unroll
           for (int b = 0; b < RB; ++b) {
-            add_product(a, w[b][h], x.sum[b][v][j]);
-            if constexpr (DT == KVC_F16) add_product(a, fine[b][h], x.sum[b][v][j]);
+            x.sum[b][v][j] = product(a, w[b][h], x.sum[b][v][j]);
+            if constexpr (DT == KVC_F16) x.sum[b][v][j] = product(a, fine[b][h], x.sum[b][v][j]);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -401,9 +408,9 @@ __device__ __forceinline__ void make_queries(const AttendParams& p, uint32_t mos
         whole += x + y;
         query[b][e][i] = i % 2 ? narrow_pair<KVC_F16>(x * 0.0625f, y * 0.0625f) : narrow_pair<KVC_F16>(x, y);
       }
-    rows.whole[b] = row_sum(whole) * 5.9604644775390625e-8f;  // (2^-24, as the codes)
+    rows.whole[b] = row_sum(whole);
   }
-  rows.unit = __builtin_amdgcn_ldexpf(p.scale_log2, 24 - up);
+  rows.unit = __builtin_amdgcn_ldexpf(p.scale_log2, -up);
 }
 
 // ---- up to 16 rows --------------------------------------------------------------------------------------------------------
@@ -434,7 +441,7 @@ __device__ __forceinline__ void put_sums(const State<DP, RB>& x, float (*sums)[D
   const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, g = lane >> 4;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    const float total = row_sum(x.l[b]), off = x.total[b][0] + x.total[b][1] + x.total[b][2];
+    const float total = row_sum(x.l[b]), off = x.total[b][0] + x.total[b][1];
     float* const to = sums[b * 16 + col];
 #pragma unroll
     for (int v = 0; v < Sizes<DP>::VS; ++v)
@@ -443,7 +450,7 @@ __device__ __forceinline__ void put_sums(const State<DP, RB>& x, float (*sums)[D
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t at = element_of<DP>(g, v, j, i);
-          to[((at / 4) ^ col) * 4 + at % 4] = x.sum[b][v][j][i] + off;
+          to[((at / 4) ^ col) * 4 + at % 4] = fmaf(x.sum[b][v][j][i], size_of<DP>(j), off);
         }
     if (g == 0) {
       m[b * 16 + col] = x.m[b] != kNone ? x.m[b] : total == 0.0f ? kNone : 0.0f;  // (a row that saw NaN alone is not empty)
@@ -594,15 +601,14 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
       for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
   }
   PairSpace& pairs = lds.of[wave].pairs;
-  begin_pairs(pairs, lane);
-  uint32_t missing = 0, turned = 0;
+  uint32_t missing = 0;
 #pragma unroll 1
-  for (uint32_t pos = start; pos < end; pos += NEXT, turned ^= 1u) {
+  for (uint32_t pos = start; pos < end; pos += NEXT) {
     const uint32_t holes = at_tile.missing;
     missing |= holes;
     at_tile = source_of<BIG>(p, u, pos + NEXT, page[1]);  // (one that is not there reads page 0)
     page[1] = page_of_lane<BIG>(p, u, pos + 2 * NEXT);
-    take_tile<DT, DP, RB, BIG>(p, u, pos + kTile > plain || holes, turned, pos, holes, at_tile, tile, rows, query, x, pairs);
+    take_tile<DT, DP, RB, BIG>(p, u, pos + kTile > plain || holes, pos, holes, at_tile, tile, rows, query, x, pairs);
   }
   if (missing && lane == 0) fault(p, KVC_FAULT_PAGE);
   if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
@@ -672,11 +678,11 @@ __device__ __forceinline__ void load_share(const AttendParams& p, const Unit<BIG
 
 // Makes a wave's share of a tile's operands.
 template <int DT, int DP>
-__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, float unit, uint32_t turned, Made<DP>& to) {
+__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, float unit, Made<DP>& to) {
   const uint32_t lane = threadIdx.x & 63u, h = wave >> 1;
   if (wave == 0) put_key_pair<DT>(to.pairs, lane, t.kp, unit);
   if (wave == 1) put_value_pair<DT>(to.pairs, lane, t.vp);
-  const uint64_t flat = __ballot((t.vp & 0x7fffu) == 0);
+  const uint64_t flat = flat_tokens<DT>(t.vp);
 #pragma unroll
   for (int i = 0; i < Share<DP>::KE; ++i) {
 #pragma unroll
@@ -691,7 +697,7 @@ __device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, fl
 #pragma unroll
   for (int s = 0; s < Sizes<DP>::VS; ++s) {
     u32x4 y = t.v[s][0], z = t.v[s][1];
-    if (flat) {  // (codes that a scale of 0 makes nothing of)
+    if (flat) {  // (codes that their scale makes nothing of)
       const uint32_t mine = (uint32_t)(flat >> (16 * (lane >> 4) + 8 * h));
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -703,11 +709,11 @@ __device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, fl
       const u32x4 both = halves(y, z, (lane & 8u) ? kHigh : kLow);
 #pragma unroll
       for (int n = 0; n < 4; ++n)
-        if ((uint32_t)n >> 1 == (wave & 1u)) to.v[h][s][n][lane] = value_operand(both, n, turned);
+        if ((uint32_t)n >> 1 == (wave & 1u)) to.v[h][s][n][lane] = value_operand(both, n);
     } else {
       const u32x4 both = halves(y, z, (wave & 1u) ? kHigh : kLow);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) to.v[h][s][2 * n + (wave & 1u)][lane] = value_operand(both, n, turned);
+      for (int n = 0; n < 4; ++n) to.v[h][s][2 * n + (wave & 1u)][lane] = value_operand(both, n);
     }
   }
 }
@@ -725,7 +731,7 @@ __device__ __forceinline__ void read_first(const Made<DP>& made, u32x4 (&a)[kAhe
 
 // A tile that has been made.  Operands are read from LDS some products ahead of those that take them; the order is the source's.  ask(): a call in between.
 template <int DT, int DP, typename Ask>
-__device__ __forceinline__ void take_made(bool masked, uint32_t turned, uint32_t at, uint32_t t1, uint32_t missing, const Made<DP>& made, const Rows<kRB>& rows,
+__device__ __forceinline__ void take_made(bool masked, uint32_t at, uint32_t t1, uint32_t missing, const Made<DP>& made, const Rows<kRB>& rows,
                                           const u32x4 (&query)[kRB][Sizes<DP>::KS], State<DP, kRB>& x, u32x4 (&a)[kAhead + 1][2], Ask ask) {
   using S = Sizes<DP>;
   constexpr int KS = S::KS, NV = S::VS * S::NJ, RING = kAhead + 1;
@@ -742,7 +748,7 @@ __device__ __forceinline__ void take_made(bool masked, uint32_t turned, uint32_t
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int b = 0; b < kRB; ++b) s[b][k] = mfma_f16(a[n % RING][i], query[b][first + i], first + i ? s[b][k] : f32x4{0, 0, 0, 0});
+      for (int b = 0; b < kRB; ++b) s[b][k] = product(a[n % RING][i], query[b][first + i], first + i ? s[b][k] : f32x4{0, 0, 0, 0});
     __builtin_amdgcn_sched_barrier(0);
   }
   __builtin_amdgcn_s_setprio(0);
@@ -769,11 +775,11 @@ __device__ __forceinline__ void take_made(bool masked, uint32_t turned, uint32_t
       for (int i = 0; i < 2; ++i) a[m % RING][i] = values[2 * m + i][lane];
     }
     if (first == 0) {
-      const u32x4 rows_of_sums = sums_operand(made.pairs, h, turned);
+      const u32x4 rows_of_sums = sums_operand(made.pairs, h);
 #pragma unroll
       for (int b = 0; b < kRB; ++b) {
-        add_product(rows_of_sums, w[b][h], x.total[b]);
-        if constexpr (DT == KVC_F16) add_product(rows_of_sums, fine[b][h], x.total[b]);
+        x.total[b] = product(rows_of_sums, w[b][h], x.total[b]);
+        if constexpr (DT == KVC_F16) x.total[b] = product(rows_of_sums, fine[b][h], x.total[b]);
       }
     }
 #pragma unroll
@@ -781,8 +787,8 @@ __device__ __forceinline__ void take_made(bool masked, uint32_t turned, uint32_t
 #pragma unroll
       for (int b = 0; b < kRB; ++b) {
         f32x4& sum = x.sum[b][(first + i) / S::NJ][(first + i) % S::NJ];
-        add_product(a[n % RING][i], w[b][h], sum);
-        if constexpr (DT == KVC_F16) add_product(a[n % RING][i], fine[b][h], sum);
+        sum = product(a[n % RING][i], w[b][h], sum);
+        if constexpr (DT == KVC_F16) sum = product(a[n % RING][i], fine[b][h], sum);
       }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -870,9 +876,8 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
   }
-  if (wave == 0) begin_pairs(lds.made[0].pairs, lane), begin_pairs(lds.made[1].pairs, lane);
   uint32_t missing = 0;
-  if (u.t0 < end) make_share<DT, DP>(share, wave, rows.unit, 0, lds.made[0]);
+  if (u.t0 < end) make_share<DT, DP>(share, wave, rows.unit, lds.made[0]);
   source = source_of<BIG>(p, u, u.t0 + kTile, page[1]);
   next_holes = source.missing;
   load_share<DP, BIG>(p, u, source, wave, share);
@@ -883,7 +888,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
     meet();  // what is in `now` is there, and the other one has been read
     u32x4 first[kAhead + 1][2];
     read_first<DP>(now, first);
-    if (pos + kTile < end) make_share<DT, DP>(share, wave, rows.unit, turn ^ 1u, lds.made[turn ^ 1u]);
+    if (pos + kTile < end) make_share<DT, DP>(share, wave, rows.unit, lds.made[turn ^ 1u]);
     __builtin_amdgcn_sched_barrier(0);
     missing |= holes;
     auto ask = [&]() {
@@ -892,7 +897,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
       page[2] = page_of_lane<BIG>(p, u, pos + 3 * kTile);
     };
     if (pos >= mine) ask();
-    else take_made<DT, DP>(pos + kTile > plain || holes, turn, pos, u.t1, holes, now, rows, query, x, first, ask);
+    else take_made<DT, DP>(pos + kTile > plain || holes, pos, u.t1, holes, now, rows, query, x, first, ask);
     holes = next_holes;
     next_holes = source.missing;
   }

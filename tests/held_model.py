@@ -82,15 +82,18 @@ class Words:
         return code, value(pair & 0xffff), value(pair >> 16)
 
 
-def attention(q, keys, values, seen, scale):
+def attention(q, keys, values, seen, scale, most=None):
     """One row of a table and one KV head, in 64 bits.  q [n][G][D]; keys and values (codes [tokens][D], scale, mn [tokens]); seen [n][tokens].
     -> out [n][G][D], lse [n][G] and the bounds of their rounding.
 
-    u is half a step of the type, e = 2^-24 of 32-bit sums.  A score is s (q . c) + m sum(q): exact products, sums of D terms in 32 bits, and six
-    roundings more (sum, scale, fma, factor, shift, exp2's two steps): e (D + 8) (s |q| . c + |m| sum |q|) + 4 e.  Elements of the query below 2^-34 of its largest
-    lose what lies below 2^-38 of that, times codes of up to 15.
+    u is half a step of the type, e = 2^-24 of 32-bit sums.  A score is s (q . (c - 8)) + (m + 8 s) sum(q): exact products, sums of D terms in 32 bits,
+    and eight roundings more (sum, scale, two of the pair, factor, logarithm of the value's scale, shift, exp2's two steps): e (D + 8) (s |q| . |c - 8| +
+    |m + 8 s| sum |q|) + 4 e, and the logarithm lv of the value's scale, which goes into the exponent with the weight, and the shift, that is near the largest of
+    both, are rounded at their size: 4 e (|lv| + 10).  Elements of the query below 2^-34 of the largest one of all of the call's (of which `most` is told) lose
+    what lies below 2^-38 of that, times codes of up to 8.
     Weights, numerator and denominator: twice that, and e for each of `tokens` terms summed and 24 for joining.
-    w s is rounded to bf16 (2^-8), or twice (2^-16), times |c - 8|; what it is multiplied with, 128 + c and 136, and m + 8 s are summed in 32 bits."""
+    w s is rounded to fp16 (2^-11), or twice (2^-21), which tells in the value itself; below 2^-14 of the largest w s, or 2^-22 where it is held 2^8 larger, by
+    2^-25, or 2^-33, of that, times the value in steps of its scale.  What w s is multiplied with, codes of up to 15 + 8, and z s = m + 8 s, are summed in 32 bits."""
     dtype = q.dtype
     q = q.double()
     (kc, ks, km), (vc, vs, vm) = keys, values
@@ -98,7 +101,8 @@ def attention(q, keys, values, seen, scale):
     out, lse = torch.zeros_like(q), torch.full((n, G), -math.inf, dtype=torch.float64)
     off, lse_off = torch.zeros_like(q), torch.zeros_like(lse)
     u, e = torch.finfo(dtype).eps / 2, 2.0 ** -24
-    fine = 2.0 ** -16 if dtype == torch.float16 else 2.0 ** -8
+    fine, tiny = (2.0 ** -21, 2.0 ** -33) if dtype == torch.float16 else (2.0 ** -11, 2.0 ** -25)
+    most = q.abs().amax() if most is None else most
     smallest = 2.0 ** -25 if dtype == torch.float16 else 2.0 ** -134
     for i in range(n):
         at = seen[i]
@@ -114,12 +118,13 @@ def attention(q, keys, values, seen, scale):
         w = w / total
         out[i], lse[i] = w @ v, (top + torch.log(total))[:, 0]
         a = q[i].abs()
-        size = (a @ (kc[at].double() * ks[at][:, None]).T + a.sum(dim=-1, keepdim=True) * km[at].abs()).amax(dim=-1) * scale
-        lost = D * 2.0 ** -38 * a.amax(dim=-1) * 15 * ks[at].amax() * scale
-        score = e * ((D + 8) * size + 4) + lost
+        size = (a @ ((kc[at].double() - 8).abs() * ks[at][:, None]).T + a.sum(dim=-1, keepdim=True) * (km[at] + 8 * ks[at]).abs()).amax(dim=-1) * scale
+        lost = D * 2.0 ** -38 * most * 8 * ks[at].amax() * scale
+        steps = torch.where(vs[at] > 0, vs[at], vm[at].abs().clamp(min=2.0 ** -60))  # (a head of one value has a scale of its size)
+        score = e * ((D + 8) * size + 4 * (11 + torch.log2(steps).abs().amax())) + lost
         share = (2 * score + (tokens + 24) * e)[:, None]
-        sv = w * vs[at]
-        off[i] = (u * out[i].abs() + share * (1 + u) * (w @ v.abs()) + fine * (sv @ (vc[at].double() - 8).abs())
-                  + e * (tokens + 24) * (280 * sv.sum(dim=-1, keepdim=True) + (w @ (vm[at] + 8 * vs[at]).abs())[:, None]) + smallest)
+        sv = w * steps
+        off[i] = (u * out[i].abs() + (share * (1 + u) + fine) * (w @ v.abs()) + tiny * sv.amax(dim=-1, keepdim=True) * (v.abs() / steps[:, None]).sum(dim=0)
+                  + e * (tokens + 24) * (23 * sv.sum(dim=-1, keepdim=True) + (w @ (vm[at] + 8 * vs[at]).abs())[:, None]) + smallest)
         lse_off[i] = score + (tokens + 24) * e + 4 * e * lse[i].abs()
     return out, lse, off, lse_off

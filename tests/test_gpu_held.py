@@ -405,7 +405,7 @@ class Attend:
                     if hidden(row, pos):
                         seen[:, pos] = False
             for h in range(H):
-                part = held.attention(self.q[first:end, h * G:h * G + G], [x[:, h] for x in k], [x[:, h] for x in v], seen, self.scale)
+                part = held.attention(self.q[first:end, h * G:h * G + G], [x[:, h] for x in k], [x[:, h] for x in v], seen, self.scale, float(self.q.float().abs().max()))
                 for whole, y in zip((out, lse, off, lse_off), part):
                     whole[first:end, h * G:h * G + G] = y
         return out, lse, off, lse_off
