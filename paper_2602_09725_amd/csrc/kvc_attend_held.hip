@@ -967,8 +967,8 @@ Shape shape_of(const AttendParams& p, uint32_t waves, uint64_t tokens, uint64_t 
   Shape best{};
   if (tokens == 0) return best;
   const bool many = waves == 4;
-  const double size = p.D <= 64 ? 0.7 : p.D <= 128 ? 1.0 : 2.0, start = many ? 3.0 : 4.0;
-  const double alone = size * (many ? 0.0048 : 0.0018), shared = size * (many ? (p.dtype == KVC_F16 ? 0.0218 : 0.019) : 0.0025);
+  const double size = (p.D <= 64 ? 0.7 : p.D <= 128 ? 1.0 : 2.0) * (p.dtype == KVC_F16 ? 1.0 : many ? 0.73 : 0.82), start = many ? 3.0 : 4.0;
+  const double alone = size * (many ? 0.0195 : 0.0028), shared = size * (many ? 0.0195 : 0.0034);
   const uint64_t most = p.D > 128 ? 1 : many ? 2 : 3;  // workgroups to a CU
   const uint64_t step = many ? kTile : 4 * kTile, block = many ? 64 * kRB : 16;
   best.waves = waves;
