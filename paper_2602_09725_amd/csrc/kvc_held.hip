@@ -63,52 +63,73 @@ struct Quad {
 // Request r has the quads from this one on: as many as n tokens can touch, n / 4 + 2, fit below the next one's.
 __device__ __forceinline__ uint32_t first_quad(const BatchView& b, uint32_t r) { return (b.starts ? min((uint32_t)b.starts[r], b.n_new) / 4 + 2 * r : r); }
 
-// What quad j of a batch is; `first`: position of each request's first token, or null for the row's last ones.  Of a quad that has nothing, taken is 0.
-// PAGED: a quad lies in one page.
-template <bool PAGED>
-__device__ __forceinline__ Quad quad_of(const PoolView& p, const BatchView& b, const int32_t* first, uint32_t j, uint32_t r, bool tells) {
-  Quad q{};
-  uint32_t from = r, n = 1, bad = 0;
-  if (b.starts) {
-    const uint32_t a = (uint32_t)b.starts[r], e = (uint32_t)b.starts[r + 1];
-    from = min(a, b.n_new);
-    const uint32_t end = min(e, b.n_new);
-    n = end > from ? end - from : 0;
-    if (a > e || e > b.n_new || n > b.most_new) bad |= KVC_FAULT_LIST;
-    if ((r == 0 && a != 0) || (r + 1 == b.n_requests && e != b.n_new)) bad |= KVC_FAULT_LIST;
-  }
-  q.row = b.rows ? (uint32_t)b.rows[r] : r;
-  const bool known = q.row < p.n_rows;
-  if (!known) q.row = 0;
-  const uint32_t len = (uint32_t)p.lens[q.row];
-  if (!known || len > p.capacity) {
-    bad |= KVC_FAULT_LIST;
-    n = 0;
-  }
-  // positions [begin, begin + covered) are asked for, those within the row are there
-  const int64_t begin = first ? (int64_t)first[r] : (int64_t)len - n;
-  const uint32_t covered = min(n, b.most_new);
-  const int64_t low = begin < 0 ? 0 : begin, high = begin + covered < (int64_t)len ? begin + covered : (int64_t)len;
-  if (n && (begin < 0 || begin + covered > (int64_t)len)) bad |= KVC_FAULT_LIST;
-  const int64_t here = (low / 4 + (j - first_quad(b, r))) * 4;
-  if (n && here < high) {
-    q.position = (uint32_t)here;
-    q.token = (uint32_t)((int64_t)from + here - begin);
+// What quads of a batch are; `first`: position of each request's first token, or null for the row's last ones.  Of a quad that has nothing, taken is 0.
+// PAGED: a quad lies in one page.  Each question waits for the answer to the one before: those of all U quads are asked side by side, with indexes that
+// are in range whatever the answers were.
+template <bool PAGED, int U>
+__device__ __forceinline__ void quads_of(const PoolView& p, const BatchView& b, const int32_t* first, const uint32_t (&j)[U], const uint32_t (&r)[U], const bool (&there)[U],
+                                         bool tells, Quad (&q)[U]) {
+  uint32_t from[U], n[U], bad = 0, len[U];
+  int64_t begin[U], here[U], low[U], high[U];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (here + k >= low && here + k < high) q.taken |= 1u << k;
-    if constexpr (PAGED) {
-      uint32_t block;
-      fd_divmod(p.dbs, q.position, block, q.slot);
-      q.page = (uint32_t)p.tables[(uint64_t)q.row * p.table_len + block];
-      if (q.page >= p.num_blocks) {
-        bad |= KVC_FAULT_PAGE;
-        q.taken = 0;
-      }
+  for (int u = 0; u < U; ++u) {
+    from[u] = r[u];
+    n[u] = 1;
+    if (b.starts) {
+      const uint32_t a = (uint32_t)b.starts[r[u]], e = (uint32_t)b.starts[r[u] + 1];
+      from[u] = min(a, b.n_new);
+      const uint32_t end = min(e, b.n_new);
+      n[u] = end > from[u] ? end - from[u] : 0;
+      if (a > e || e > b.n_new || n[u] > b.most_new) bad |= KVC_FAULT_LIST;
+      if ((r[u] == 0 && a != 0) || (r[u] + 1 == b.n_requests && e != b.n_new)) bad |= KVC_FAULT_LIST;
+    }
+    q[u].row = b.rows ? (uint32_t)b.rows[r[u]] : r[u];
+    begin[u] = first ? (int64_t)first[r[u]] : 0;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool known = q[u].row < p.n_rows;
+    if (!known) q[u].row = 0;
+    len[u] = (uint32_t)p.lens[q[u].row];
+    if (!known || len[u] > p.capacity) {
+      if (there[u]) bad |= KVC_FAULT_LIST;
+      n[u] = 0;
     }
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    // positions [begin, begin + covered) are asked for, those within the row are there
+    if (!first) begin[u] = (int64_t)len[u] - n[u];
+    const uint32_t covered = min(n[u], b.most_new);
+    low[u] = begin[u] < 0 ? 0 : begin[u];
+    high[u] = begin[u] + covered < (int64_t)len[u] ? begin[u] + covered : (int64_t)len[u];
+    if (there[u] && n[u] && (begin[u] < 0 || begin[u] + covered > (int64_t)len[u])) bad |= KVC_FAULT_LIST;
+    here[u] = (low[u] / 4 + (j[u] - first_quad(b, r[u]))) * 4;
+    q[u].taken = 0;
+    q[u].page = q[u].slot = 0;
+    const bool some = there[u] && n[u] && here[u] < high[u];
+    q[u].position = some ? (uint32_t)here[u] : 0;
+    q[u].token = (uint32_t)((int64_t)from[u] + here[u] - begin[u]);
+    if (some) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (here[u] + k >= low[u] && here[u] + k < high[u]) q[u].taken |= 1u << k;
+    }
+    if constexpr (PAGED) {
+      uint32_t block;
+      fd_divmod(p.dbs, q[u].position, block, q[u].slot);
+      q[u].page = (uint32_t)p.tables[(uint64_t)q[u].row * p.table_len + block];
+    }
+  }
+  if constexpr (PAGED) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (q[u].taken && q[u].page >= p.num_blocks) {
+        bad |= KVC_FAULT_PAGE;
+        q[u].taken = 0;
+      }
+  }
   if (tells) fault(p, bad);
-  return q;
 }
 
 // Request of quad j, the workgroup's first one; all threads of a wave call it.
@@ -119,118 +140,153 @@ __device__ __forceinline__ uint32_t request_of_quad(const BatchView& b, uint32_t
   return c ? c - 1 : 0;
 }
 
-// Threads of a workgroup that have a quad's column (a kind and a head) each, and which one a thread's is.
+// A column is a kind and a head.  A thread's units are the same column of U quads that follow one another.
+template <int U>
 struct Column {
-  uint32_t quad, kind, head, request;
-  bool there;
+  uint32_t quad[U], request[U], kind, head;
+  bool there[U];
 };
-__device__ __forceinline__ Column column_of(const HeldParams& p, uint64_t unit, uint64_t first_unit) {
-  Column c;
-  const uint32_t H2 = 2 * p.H, first = (uint32_t)(first_unit / H2);
-  c.there = unit < (uint64_t)p.quads * H2;
-  const uint64_t at = c.there ? unit : first_unit;
-  uint32_t column;
-  if ((uint64_t)p.quads * H2 >> 31) c.quad = (uint32_t)(at / H2), column = (uint32_t)(at - (uint64_t)c.quad * H2);
-  else fd_divmod(p.dcolumns, (uint32_t)at, c.quad, column);
+template <int U>
+__device__ __forceinline__ Column<U> column_of(const HeldParams& p, uint64_t unit, uint64_t first_unit) {
+  Column<U> c;
+  const uint32_t H2 = 2 * p.H;
+  const uint64_t all = (uint64_t)((p.quads + U - 1) / U) * H2;
+  const bool mine = unit < all;
+  auto group_of = [&](uint64_t at, uint32_t& column) {
+    if (all >> 31) {
+      const uint32_t g = (uint32_t)(at / H2);
+      column = (uint32_t)(at - (uint64_t)g * H2);
+      return g;
+    }
+    uint32_t g;
+    fd_divmod(p.dcolumns, (uint32_t)at, g, column);
+    return g;
+  };
+  uint32_t column, unused;
+  const uint32_t group = group_of(mine ? unit : first_unit, column);
   c.kind = column >= p.H;
   c.head = column - c.kind * p.H;
-  c.request = request_of_quad(p.batch, first);
-  if (p.batch.starts)
-    while (c.request + 1 < p.batch.n_requests && first_quad(p.batch, c.request + 1) <= c.quad) ++c.request;
-  else
-    c.request = c.quad;
+  uint32_t r = request_of_quad(p.batch, group_of(first_unit, unused) * U);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    c.quad[u] = group * U + u;
+    c.there[u] = mine && c.quad[u] < p.quads;
+    if (p.batch.starts)
+      while (r + 1 < p.batch.n_requests && first_quad(p.batch, r + 1) <= c.quad[u]) ++r;
+    else
+      r = min(c.quad[u], p.batch.n_requests - 1);
+    c.request[u] = r;
+  }
   return c;
 }
 
-// Tokens of a batch to their slots: P threads have a head of a quad.
-template <int DT, int P>
+// Tokens of a batch to their slots: P threads have a head of U quads.
+template <int DT, int P, int U>
 __global__ void __launch_bounds__(256) write_kernel(HeldParams p) {
+  fetch_params<HeldParams>();
   const uint64_t first = (uint64_t)blockIdx.x * (256 / P);
   const uint32_t w = threadIdx.x % P;
-  const Column c = column_of(p, first + threadIdx.x / P, first);
-  const Quad q = quad_of<true>(p.pool, p.batch, nullptr, c.quad, c.request, c.there && w == 0 && c.kind == 0 && c.head == 0);
-  const bool mine = c.there && w < p.W;
-  const uint16_t* const from = (c.kind ? p.v : p.k) + (uint64_t)(c.head * p.W + w) * 8;
-  u32x4 v[4];
+  const Column<U> c = column_of<U>(p, first + threadIdx.x / P, first);
+  Quad q[U];
+  quads_of<true, U>(p.pool, p.batch, nullptr, c.quad, c.request, c.there, w == 0 && c.kind == 0 && c.head == 0, q);
+  // (lanes beyond a head's words have what its first one has)
+  const uint16_t* const from = (c.kind ? p.v : p.k) + (uint64_t)(c.head * p.W + (w < p.W ? w : 0)) * 8;
+  u32x4 v[U][4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const bool live = mine && (q.taken >> k & 1u);
-    v[k] = u32x4{0, 0, 0, 0};
-    if (live) v[k] = *(const KVC_GLOBAL u32x4*)(from + (int64_t)(uint32_t)(q.token + k) * p.token_stride);
-  }
-  if (w >= p.W) {  // lanes beyond a head's words have what its first one has
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (c.there && (q.taken >> k & 1u)) v[k] = *(const KVC_GLOBAL u32x4*)((c.kind ? p.v : p.k) + (uint64_t)c.head * p.W * 8 + (int64_t)(uint32_t)(q.token + k) * p.token_stride);
-  }
-  u32x4 codes, pairs;
-  quantize<DT, P>(v, codes, pairs);
-  if (!mine || !q.taken) return;
-  uint8_t* const page = page_at(p.pool, p.layer, c.kind, q.page);
-  uint8_t* const to = page + codes_at(p.pool, p.W, c.head, q.slot) + w * 16;
-  uint8_t* const pair_to = page + pairs_at(p.pool, p.W, p.H, c.head, q.slot);
-  if (q.taken == 15) {
-    *(KVC_GLOBAL u32x4*)to = codes;
-    if (w == 0) *(KVC_GLOBAL u32x4*)pair_to = pairs;
-    return;
-  }
+    for (int k = 0; k < 4; ++k) {
+      v[u][k] = u32x4{0, 0, 0, 0};
+      if (q[u].taken >> k & 1u) v[u][k] = stream_load<u32x4>(from + (int64_t)(uint32_t)(q[u].token + k) * p.token_stride);
+    }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (!(q.taken >> k & 1u)) continue;
-    ((KVC_GLOBAL uint32_t*)to)[k] = codes[k];
-    if (w == 0) ((KVC_GLOBAL uint32_t*)pair_to)[k] = pairs[k];
+  for (int u = 0; u < U; ++u) {
+    u32x4 codes, pairs;
+    quantize<DT, P>(v[u], codes, pairs);
+    if (w >= p.W || !q[u].taken) continue;
+    uint8_t* const page = page_at(p.pool, p.layer, c.kind, q[u].page);
+    uint8_t* const to = page + codes_at(p.pool, p.W, c.head, q[u].slot) + w * 16;
+    uint8_t* const pair_to = page + pairs_at(p.pool, p.W, p.H, c.head, q[u].slot);
+    if (q[u].taken == 15) {
+      *(KVC_GLOBAL u32x4*)to = codes;
+      if (w == 0) *(KVC_GLOBAL u32x4*)pair_to = pairs;
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!(q[u].taken >> k & 1u)) continue;
+      ((KVC_GLOBAL uint32_t*)to)[k] = codes[k];
+      if (w == 0) ((KVC_GLOBAL uint32_t*)pair_to)[k] = pairs[k];
+    }
   }
 }
 
-// Tokens of rows back: a thread has a word of a quad.
-template <int DT>
-__global__ void __launch_bounds__(256) read_kernel(HeldParams p) {
-  const uint64_t all = (uint64_t)p.quads * 2 * p.H * p.W, begin = (uint64_t)blockIdx.x * 256;
-  const uint64_t here = begin + threadIdx.x, at = here < all ? here : all - 1;
-  uint64_t unit;
-  uint32_t w;
+// A thread's unit and word of so many threads.
+__device__ __forceinline__ uint64_t unit_of_thread(const HeldParams& p, uint64_t all, uint64_t at, uint32_t& w) {
   if (all >> 31) {
-    unit = at / p.W, w = (uint32_t)(at - unit * p.W);
-  } else {
-    uint32_t u;
-    fd_divmod(p.dwords, (uint32_t)at, u, w);
-    unit = u;
+    const uint64_t unit = at / p.W;
+    w = (uint32_t)(at - unit * p.W);
+    return unit;
   }
-  const Column c = column_of(p, unit, begin / p.W);
-  const Quad q = quad_of<true>(p.pool, p.batch, p.first, c.quad, c.request, here < all && w == 0 && c.kind == 0 && c.head == 0);
-  if (here >= all || !q.taken) return;
-  const uint8_t* const page = page_at(p.pool, p.layer, c.kind, q.page);
-  const u32x4 codes = *(const KVC_GLOBAL u32x4*)(page + codes_at(p.pool, p.W, c.head, q.slot) + w * 16);
-  const u32x4 pairs = *(const KVC_GLOBAL u32x4*)(page + pairs_at(p.pool, p.W, p.H, c.head, q.slot));
+  uint32_t unit;
+  fd_divmod(p.dwords, (uint32_t)at, unit, w);
+  return unit;
+}
+
+// Tokens of rows back: a thread has a word of U quads.
+template <int DT, int U>
+__global__ void __launch_bounds__(256) read_kernel(HeldParams p) {
+  fetch_params<HeldParams>();
+  const uint64_t all = (uint64_t)((p.quads + U - 1) / U) * 2 * p.H * p.W, begin = (uint64_t)blockIdx.x * 256, here = begin + threadIdx.x;
+  uint32_t w, unused;
+  const uint64_t unit = unit_of_thread(p, all, here < all ? here : all - 1, w);
+  const Column<U> c = column_of<U>(p, unit, unit_of_thread(p, all, begin, unused));
+  Quad q[U];
+  quads_of<true, U>(p.pool, p.batch, p.first, c.quad, c.request, c.there, here < all && w == 0 && c.kind == 0 && c.head == 0, q);
+  if (here >= all) return;
+  u32x4 codes[U], pairs[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint8_t* const page = page_at(p.pool, p.layer, c.kind, q[u].taken ? q[u].page : 0);
+    codes[u] = stream_load<u32x4>(page + codes_at(p.pool, p.W, c.head, q[u].slot) + w * 16);
+    pairs[u] = *(const KVC_GLOBAL u32x4*)(page + pairs_at(p.pool, p.W, p.H, c.head, q[u].slot));
+  }
   uint16_t* const to = (c.kind ? p.v_out : p.k_out) + (uint64_t)(c.head * p.W + w) * 8;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (q.taken >> k & 1u) stream_store<u32x4>(to + (int64_t)(uint32_t)(q.token + k) * p.token_stride, values_of<DT>(codes[k], pairs[k]));
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (q[u].taken >> k & 1u)
+        stream_store<u32x4>(to + (int64_t)(uint32_t)(q[u].token + k) * p.token_stride, values_of<DT>(codes[u][k], pairs[u][k]));
 }
 
 // The same from a pool of 16 bits: a thread has eight elements of a quad's tokens.
 __global__ void __launch_bounds__(256) read_wide_kernel(HeldParams p) {
-  const uint64_t all = (uint64_t)p.quads * 2 * p.H * p.W, begin = (uint64_t)blockIdx.x * 256;
-  const uint64_t here = begin + threadIdx.x, at = here < all ? here : all - 1;
-  const uint64_t unit = at / p.W;
-  const uint32_t w = (uint32_t)(at - unit * p.W);
-  const Column c = column_of(p, unit, begin / p.W);
-  const Quad q = quad_of<false>(p.pool, p.batch, p.first, c.quad, c.request, here < all && w == 0 && c.kind == 0 && c.head == 0);
+  const uint64_t all = (uint64_t)p.quads * 2 * p.H * p.W, begin = (uint64_t)blockIdx.x * 256, here = begin + threadIdx.x;
+  uint32_t w, unused;
+  const uint64_t unit = unit_of_thread(p, all, here < all ? here : all - 1, w);
+  const Column<1> c = column_of<1>(p, unit, unit_of_thread(p, all, begin, unused));
+  Quad qs[1];
+  quads_of<false, 1>(p.pool, p.batch, p.first, c.quad, c.request, c.there, here < all && w == 0 && c.kind == 0 && c.head == 0, qs);
   if (here >= all) return;
+  const Quad& q = qs[0];
   uint16_t* const to = (c.kind ? p.v_out : p.k_out) + (uint64_t)(c.head * p.W + w) * 8;
-  uint32_t bad = 0;
+  uint32_t bad = 0, page[4], slot[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t block;  // (a page of any number of tokens may end inside a quad)
+    fd_divmod(p.pool.dbs, q.taken >> k & 1u ? q.position + k : 0u, block, slot[k]);
+    page[k] = (uint32_t)p.pool.tables[(uint64_t)q.row * p.pool.table_len + block];
+  }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (!(q.taken >> k & 1u)) continue;
-    uint32_t block, slot;  // (a page of any number of tokens may end inside a quad)
-    fd_divmod(p.pool.dbs, q.position + k, block, slot);
-    const uint32_t page = (uint32_t)p.pool.tables[(uint64_t)q.row * p.pool.table_len + block];
-    if (page >= p.pool.num_blocks) {
+    if (page[k] >= p.pool.num_blocks) {
       bad |= KVC_FAULT_PAGE;
       continue;
     }
-    const uint8_t* const from = page_at(p.pool, p.layer, c.kind, page) + (uint64_t)slot * p.pool.token_bytes + (uint64_t)(c.head * p.W + w) * 16;
-    stream_store<u32x4>(to + (int64_t)(uint32_t)(q.token + k) * p.token_stride, *(const KVC_GLOBAL u32x4*)from);
+    const uint8_t* const from = page_at(p.pool, p.layer, c.kind, page[k]) + (uint64_t)slot[k] * p.pool.token_bytes + (uint64_t)(c.head * p.W + w) * 16;
+    stream_store<u32x4>(to + (int64_t)(uint32_t)(q.token + k) * p.token_stride, stream_load<u32x4>(from));
   }
   if (w == 0 && c.head == 0 && c.kind == 0) fault(p.pool, bad);
 }
@@ -297,10 +353,10 @@ __global__ void __launch_bounds__(256) convert_kernel(ConvertParams p) {
 
 template <int DT>
 __global__ void __launch_bounds__(256) convert_back_kernel(ConvertParams p) {
-  const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  const uint64_t unit = at / p.W;
-  const uint32_t w = (uint32_t)(at - unit * p.W);
-  const PageQuad q = page_quad_of(p, unit);
+  const uint64_t first = (uint64_t)blockIdx.x * 256, unit0 = first / p.W;  // (uniform)
+  uint32_t more, w;
+  fd_divmod(p.dwords, (uint32_t)(first - unit0 * p.W) + threadIdx.x, more, w);
+  const PageQuad q = page_quad_of(p, unit0 + more);
   if (!q.there) return;
   const uint8_t* const page = page_at(p.held, q.layer, q.kind, q.held_page);
   const u32x4 codes = stream_load<u32x4>(page + codes_at(p.held, p.W, q.head, q.slot) + w * 16);
@@ -319,17 +375,22 @@ uint32_t threads_of(uint32_t W) {
   return P;
 }
 
-template <int DT>
+template <int DT, int U>
 void launch_write_of(const HeldParams& p, uint32_t P, uint32_t groups, hipStream_t stream) {
   switch (P) {
-    case 1: hipLaunchKernelGGL((write_kernel<DT, 1>), dim3(groups), dim3(256), 0, stream, p); break;
-    case 2: hipLaunchKernelGGL((write_kernel<DT, 2>), dim3(groups), dim3(256), 0, stream, p); break;
-    case 4: hipLaunchKernelGGL((write_kernel<DT, 4>), dim3(groups), dim3(256), 0, stream, p); break;
-    case 8: hipLaunchKernelGGL((write_kernel<DT, 8>), dim3(groups), dim3(256), 0, stream, p); break;
-    case 16: hipLaunchKernelGGL((write_kernel<DT, 16>), dim3(groups), dim3(256), 0, stream, p); break;
-    default: hipLaunchKernelGGL((write_kernel<DT, 32>), dim3(groups), dim3(256), 0, stream, p); break;
+    case 1: hipLaunchKernelGGL((write_kernel<DT, 1, U>), dim3(groups), dim3(256), 0, stream, p); break;
+    case 2: hipLaunchKernelGGL((write_kernel<DT, 2, U>), dim3(groups), dim3(256), 0, stream, p); break;
+    case 4: hipLaunchKernelGGL((write_kernel<DT, 4, U>), dim3(groups), dim3(256), 0, stream, p); break;
+    case 8: hipLaunchKernelGGL((write_kernel<DT, 8, U>), dim3(groups), dim3(256), 0, stream, p); break;
+    case 16: hipLaunchKernelGGL((write_kernel<DT, 16, U>), dim3(groups), dim3(256), 0, stream, p); break;
+    default: hipLaunchKernelGGL((write_kernel<DT, 32, U>), dim3(groups), dim3(256), 0, stream, p); break;
   }
 }
+
+// Quads of a thread: one each until the chip has eight workgroups a CU of them.
+constexpr uint32_t kQuads = 4;
+uint32_t quads_each(const HeldParams& p, uint32_t P) { return (uint64_t)p.quads * 2 * p.H * P < (uint64_t)kQuads * 256 * 8 * 256 ? 1 : kQuads; }
+uint64_t groups_of(const HeldParams& p, uint32_t P, uint32_t each) { return ((uint64_t)((p.quads + each - 1) / each) * 2 * p.H * P + 255) / 256; }
 
 template <int DT>
 void launch_convert_of(const ConvertParams& p, uint32_t P, uint32_t groups, hipStream_t stream) {
@@ -346,20 +407,24 @@ void launch_convert_of(const ConvertParams& p, uint32_t P, uint32_t groups, hipS
 }  // namespace
 
 kvc_status launch_write_held(const HeldParams& p, hipStream_t stream) {
-  const uint32_t P = threads_of(p.W);
-  const uint64_t groups = ((uint64_t)p.quads * 2 * p.H * P + 255) / 256;
+  const uint32_t P = threads_of(p.W), each = quads_each(p, P) == 1 ? 1 : 2;
+  const uint64_t groups = groups_of(p, P, each);
   if (groups > kMostGroups) return KVC_ERR_UNSUPPORTED;
-  if (p.dtype == KVC_F16) launch_write_of<KVC_F16>(p, P, (uint32_t)groups, stream);
-  else launch_write_of<KVC_BF16>(p, P, (uint32_t)groups, stream);
+  if (p.dtype == KVC_F16) each == 1 ? launch_write_of<KVC_F16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_F16, 2>(p, P, (uint32_t)groups, stream);
+  else each == 1 ? launch_write_of<KVC_BF16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_BF16, 2>(p, P, (uint32_t)groups, stream);
   return launched();
 }
 
 kvc_status launch_read(const HeldParams& p, hipStream_t stream) {
-  const uint64_t groups = ((uint64_t)p.quads * 2 * p.H * p.W + 255) / 256;
+  const uint32_t each = p.pool.held ? quads_each(p, p.W) : 1;
+  const uint64_t groups = groups_of(p, p.W, each);
   if (groups > kMostGroups) return KVC_ERR_UNSUPPORTED;
-  if (!p.pool.held) hipLaunchKernelGGL(read_wide_kernel, dim3((uint32_t)groups), dim3(256), 0, stream, p);
-  else if (p.dtype == KVC_F16) hipLaunchKernelGGL(read_kernel<KVC_F16>, dim3((uint32_t)groups), dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL(read_kernel<KVC_BF16>, dim3((uint32_t)groups), dim3(256), 0, stream, p);
+  const dim3 grid((uint32_t)groups);
+  if (!p.pool.held) hipLaunchKernelGGL(read_wide_kernel, grid, dim3(256), 0, stream, p);
+  else if (p.dtype == KVC_F16 && each == 1) hipLaunchKernelGGL((read_kernel<KVC_F16, 1>), grid, dim3(256), 0, stream, p);
+  else if (p.dtype == KVC_F16) hipLaunchKernelGGL((read_kernel<KVC_F16, kQuads>), grid, dim3(256), 0, stream, p);
+  else if (each == 1) hipLaunchKernelGGL((read_kernel<KVC_BF16, 1>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((read_kernel<KVC_BF16, kQuads>), grid, dim3(256), 0, stream, p);
   return launched();
 }
 

@@ -90,7 +90,7 @@ struct ConvertParams {
   PoolView wide, held;
   const int32_t *src, *dst;
   uint32_t n, back, H, W, dtype;
-  FastDiv deach, dkinds, dheads;  // quads of all heads of a page, 2 L, H
+  FastDiv deach, dkinds, dheads, dwords;  // quads of all heads of a page, 2 L, H, W
 };
 kvc_status launch_convert(const ConvertParams& p, hipStream_t stream);
 

@@ -294,6 +294,7 @@ kvc_status kvc_pages_convert(const kvc_pool* from, const kvc_pool* to, const int
   p.deach = make_fastdiv(p.H * (p.held.block_size / 4));
   p.dkinds = make_fastdiv(2 * p.held.L);
   p.dheads = make_fastdiv(p.H);
+  p.dwords = make_fastdiv(p.W);
   return launch_convert(p, as_stream(stream));
 }
 
