@@ -1,7 +1,7 @@
 """Serving from a restored cache: a prompt's KV cache comes out of packed frames into pages, many requests take it up, and each
 goes on with tokens of its own.
 
-  restore   kvc_pages_grow, kvc_restore_paged: the prompt's pages are row 0's
+  restore   kvc_pages_grow, kvc_restore_paged: the prompt's pages are row 0's (of a pool in 4 bits: restored beside it, and moved by kvc_pages_convert)
   admit     kvc_pages_fork: the requests' rows share whole pages of the prompt, and have a copy of its last one
   step      kvc_pages_grow, then in every layer kvc_append_paged and kvc_attend_paged
   finish    kvc_pages_free: pages that no row holds any more are free again
@@ -9,7 +9,7 @@ goes on with tokens of its own.
 
 The model is a stand-in (random projections around the attention, no feed-forward part): what is shown is the cache's life.
 
-  python examples/serve_shared_prefix.py [--layers 32] [--prompt 32768] [--requests 64] [--steps 16] [--dtype f16]
+  python examples/serve_shared_prefix.py [--layers 32] [--prompt 32768] [--requests 64] [--steps 16] [--dtype f16] [--held]
 """
 import argparse
 import math
@@ -50,19 +50,21 @@ class Model:
 
 
 class Server:
-    """A pool of pages with rows 1 .. max_rows for requests; row 0 is the prompt's."""
+    """A pool of pages with rows 1 .. max_rows for requests; row 0 is the prompt's.  held: its pages hold tokens in 4 bits."""
 
-    def __init__(self, model, max_rows, max_tokens, num_blocks, block_size):
+    def __init__(self, model, max_rows, max_tokens, num_blocks, block_size, held=False):
         m, (dtype, code) = model, DTYPES[model.dtype]
         self.model, self.block, self.max_tokens = model, block_size, max_tokens
-        self.cache = [torch.zeros((2, num_blocks, block_size, m.heads, m.head_dim), dtype=dtype, device="cuda") for _ in range(m.layers)]
+        self.held = held
+        shape = (m.heads * (m.head_dim // 8 + 1) * block_size,) if held else (block_size, m.heads, m.head_dim)
+        self.cache = [torch.zeros((2, num_blocks, *shape), dtype=torch.int32 if held else dtype, device="cuda") for _ in range(m.layers)]
         self.pointers = torch.tensor([c.data_ptr() for c in self.cache], dtype=torch.int64, device="cuda")
         self.table_len = -(-max_tokens // block_size)
         self.tables = torch.full((max_rows + 1, self.table_len), -1, dtype=torch.int32, device="cuda")
         self.lens = torch.zeros(max_rows + 1, dtype=torch.int32, device="cuda")
         self.refs = torch.zeros(num_blocks, dtype=torch.int32, device="cuda")
         self.err = torch.zeros(1, dtype=torch.int32, device="cuda")
-        self.pool = kvc.Pool(m.layers, m.heads, m.head_dim, code, num_blocks, block_size, max_rows + 1, self.table_len, self.pointers.data_ptr(),
+        self.pool = kvc.Pool(m.layers, m.heads, m.head_dim, code | (kvc.KVC_HELD_Q4 if held else 0), num_blocks, block_size, max_rows + 1, self.table_len, self.pointers.data_ptr(),
                              self.tables.data_ptr(), self.lens.data_ptr(), self.refs.data_ptr(), self.err.data_ptr())
         self.books = torch.empty(kvc.pages_workspace(self.pool), dtype=torch.uint8, device="cuda")
         self.where = torch.empty(num_blocks, dtype=torch.int32, device="cuda")
@@ -76,9 +78,34 @@ class Server:
         """The prompt's cache, from packed frames to pages that row 0 takes."""
         row, count = i32([0]), i32([n_tokens])
         kvc.kvc_pages_grow(self.pool, row.data_ptr(), count.data_ptr(), 1, *self._room())
-        kvc.kvc_restore_paged(layout, frames.data_ptr(), meta.data_ptr(), 0, n_tokens, self.pointers.data_ptr(), self.pool.num_blocks, self.block,
-                              self.tables.data_ptr(), self.table_len, self.err.data_ptr(), stream())
+        if self.held:
+            self._restore_held(layout, frames, meta, n_tokens)
+        else:
+            kvc.kvc_restore_paged(layout, frames.data_ptr(), meta.data_ptr(), 0, n_tokens, self.pointers.data_ptr(), self.pool.num_blocks, self.block,
+                                  self.tables.data_ptr(), self.table_len, self.err.data_ptr(), stream())
         self.prompt = n_tokens
+
+    def _restore_held(self, layout, frames, meta, n_tokens):
+        """Restores to pages of 16 bits that are the prompt's alone, and moves them to row 0's.  (They are kept until the next prompt: the calls are on their way.)"""
+        m, (dtype, code), pages = self.model, DTYPES[self.model.dtype], -(-n_tokens // self.block)
+        wide = torch.zeros((m.layers, 2, pages, self.block, m.heads, m.head_dim), dtype=dtype, device="cuda")
+        pointers = torch.tensor([c.data_ptr() for c in wide], dtype=torch.int64, device="cuda")
+        order = torch.arange(pages, dtype=torch.int32, device="cuda")
+        kvc.kvc_restore_paged(layout, frames.data_ptr(), meta.data_ptr(), 0, n_tokens, pointers.data_ptr(), pages, self.block, order.data_ptr(), pages,
+                              self.err.data_ptr(), stream())
+        pool = kvc.Pool(m.layers, m.heads, m.head_dim, code, pages, self.block, 1, 1, pointers.data_ptr(), self.tables.data_ptr(), self.lens.data_ptr(), None,
+                        self.err.data_ptr())
+        kvc.kvc_pages_convert(pool, self.pool, order.data_ptr(), self.tables.data_ptr(), pages, stream())
+        self.restored = (wide, pointers, order)
+
+    def read_back(self, row, layer):
+        """Keys and values of a row, as what its pages hold stands for."""
+        m, n = self.model, self.length.get(row, self.prompt)
+        rows, starts = i32([row]), i32([0, n])
+        k, v = (torch.empty((n, m.heads, m.head_dim), dtype=DTYPES[m.dtype][0], device="cuda") for _ in range(2))
+        batch = kvc.Batch(1, n, n, rows.data_ptr(), starts.data_ptr())
+        kvc.kvc_read_paged(self.pool, batch, None, layer, k.data_ptr(), v.data_ptr(), m.heads * m.head_dim, stream())
+        return k, v
 
     def admit(self, rows):
         parents, children = i32([0] * len(rows)), i32(rows)
@@ -148,11 +175,12 @@ def main():
                         ("steps", 16), ("block", 16)):
         a.add_argument("--" + name, type=int, default=value)
     a.add_argument("--dtype", choices=sorted(DTYPES), default="f16")
+    a.add_argument("--held", action="store_true", help="hold the cache in 4 bits")
     o = a.parse_args()
     model = Model(o.layers, o.q_heads, o.heads, o.head_dim, o.dtype)
     own = o.question + 2 * o.steps
     blocks = -(-o.prompt // o.block) + o.requests * (-(-own // o.block) + 2)
-    server = Server(model, o.requests, o.prompt + own, blocks, o.block)
+    server = Server(model, o.requests, o.prompt + own, blocks, o.block, o.held)
     server.restore(*packed_prompt(model, o.prompt), o.prompt)
     rows = list(range(1, o.requests + 1))
     server.admit(rows)
