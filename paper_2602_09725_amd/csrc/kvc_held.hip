@@ -432,9 +432,12 @@ void launch_write_of(const HeldParams& p, uint32_t P, uint32_t groups, hipStream
   }
 }
 
-// Quads of a thread: one each until the chip has eight workgroups a CU of them.
-constexpr uint32_t kQuads = 4;
-uint32_t quads_each(const HeldParams& p, uint32_t P) { return (uint64_t)p.quads * 2 * p.H * P < (uint64_t)kQuads * 256 * 8 * 256 ? 1 : kQuads; }
+// Quads of a thread: one while that is fewer than twelve workgroups a CU; of more, whose loads the chip cannot have in flight at once, several that ask side by
+// side.  8 heads of 128, one quad / several: 8500 tokens (8 workgroups a CU) written 15.7 / 15.7 us, read 14.3 / 14.3; 16 000 tokens (16 a CU) written
+// 25.1 / 20.8, read 23.5 / 19.5; 160 000 tokens written 200 / 166; 32 rows of up to 8000 tokens read 177 / 132.  Two to write (with four: 16 000 tokens 24.3 us,
+// 160 000 173), four to read (with two: 20.7 and 179 against 19.5 and 160).
+constexpr uint32_t kQuadsRead = 4, kQuadsWritten = 2;
+uint32_t quads_each(const HeldParams& p, uint32_t P, uint32_t most) { return (uint64_t)p.quads * 2 * p.H * P < 12ull * 256 * 256 ? 1 : most; }
 uint64_t groups_of(const HeldParams& p, uint32_t P, uint32_t each) { return ((uint64_t)((p.quads + each - 1) / each) * 2 * p.H * P + 255) / 256; }
 
 template <int DT>
@@ -452,24 +455,24 @@ void launch_convert_of(const ConvertParams& p, uint32_t P, uint32_t groups, hipS
 }  // namespace
 
 kvc_status launch_write_held(const HeldParams& p, hipStream_t stream) {
-  const uint32_t P = threads_of(p.W), each = quads_each(p, P) == 1 ? 1 : 2;
+  const uint32_t P = threads_of(p.W), each = quads_each(p, P, kQuadsWritten);
   const uint64_t groups = groups_of(p, P, each);
   if (groups > kMostGroups) return KVC_ERR_UNSUPPORTED;
-  if (p.dtype == KVC_F16) each == 1 ? launch_write_of<KVC_F16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_F16, 2>(p, P, (uint32_t)groups, stream);
-  else each == 1 ? launch_write_of<KVC_BF16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_BF16, 2>(p, P, (uint32_t)groups, stream);
+  if (p.dtype == KVC_F16) each == 1 ? launch_write_of<KVC_F16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_F16, kQuadsWritten>(p, P, (uint32_t)groups, stream);
+  else each == 1 ? launch_write_of<KVC_BF16, 1>(p, P, (uint32_t)groups, stream) : launch_write_of<KVC_BF16, kQuadsWritten>(p, P, (uint32_t)groups, stream);
   return launched();
 }
 
 kvc_status launch_read(const HeldParams& p, hipStream_t stream) {
-  const uint32_t each = p.pool.held ? quads_each(p, p.W) : 1;
+  const uint32_t each = p.pool.held ? quads_each(p, p.W, kQuadsRead) : 1;
   const uint64_t groups = groups_of(p, p.W, each);
   if (groups > kMostGroups) return KVC_ERR_UNSUPPORTED;
   const dim3 grid((uint32_t)groups);
   if (!p.pool.held) hipLaunchKernelGGL(read_wide_kernel, grid, dim3(256), 0, stream, p);
   else if (p.dtype == KVC_F16 && each == 1) hipLaunchKernelGGL((read_kernel<KVC_F16, 1>), grid, dim3(256), 0, stream, p);
-  else if (p.dtype == KVC_F16) hipLaunchKernelGGL((read_kernel<KVC_F16, kQuads>), grid, dim3(256), 0, stream, p);
+  else if (p.dtype == KVC_F16) hipLaunchKernelGGL((read_kernel<KVC_F16, kQuadsRead>), grid, dim3(256), 0, stream, p);
   else if (each == 1) hipLaunchKernelGGL((read_kernel<KVC_BF16, 1>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((read_kernel<KVC_BF16, kQuads>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((read_kernel<KVC_BF16, kQuadsRead>), grid, dim3(256), 0, stream, p);
   return launched();
 }
 
