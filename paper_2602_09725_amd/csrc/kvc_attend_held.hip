@@ -227,6 +227,14 @@ __device__ __forceinline__ u32x4 value_operand(u32x4 both, int n) {
 template <int DP>
 constexpr float size_of(int j) { return (DP == 64 ? j : j / 2) % 2 ? 0.0625f : 1.0f; }
 
+// Sums of more than 128 elements have no room among the registers that other arithmetic takes: they stay in the matrix unit's own also where they are multiplied, once in
+// many tiles.  (Left to itself the compiler moves all of them there and back for every tile; and 16 rows' fit two
+// waves a SIMD so: a prompt of 8000 tokens, 16 query heads of 256, 974 -> 860 us, 64 requests of up to 2000 tokens 76 -> 45.)
+template <int DP>
+__device__ __forceinline__ void stay(f32x4& v) {
+  if constexpr (DP > 128) asm volatile("" : "+a"(v));
+}
+
 // Weights of a tile from its products s[k][i], those of token 16 g + 4 i + k (they are overwritten): operands w[h] of tokens 16 g + 8 h .. + 7, and for fp16
 // what their rounding left.  masked: not all of it is there and seen by all rows (wave-uniform); missing: quads on no page.  The number subtracted from an exponent need not be
 // the largest one, as long as no weight leaves fp16; so that small ones stay in it too it lies 2^8 below the product that moves it for a pool of fp16.  (The order is the source's: a few of LDS's numbers at a time.)
@@ -270,7 +278,11 @@ __device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, u
 #pragma unroll
     for (int v = 0; v < Sizes<DP>::VS; ++v)
 #pragma unroll
-      for (int j = 0; j < Sizes<DP>::NJ; ++j) x.sum[b][v][j] *= keep;
+      for (int j = 0; j < Sizes<DP>::NJ; ++j) {
+        stay<DP>(x.sum[b][v][j]);
+        x.sum[b][v][j] *= keep;
+        stay<DP>(x.sum[b][v][j]);
+      }
   }
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -896,7 +908,8 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
       load_share<DP, BIG>(p, u, source, wave, share);
       page[2] = page_of_lane<BIG>(p, u, pos + 3 * kTile);
     };
-    if (pos >= mine) ask();
+    // (with one wave a SIMD a wave that has seen all of its tokens would wait for the others; a branch around its sums has them all moved between registers)
+    if (DP <= 128 && pos >= mine) ask();
     else take_made<DT, DP>(pos + kTile > plain || holes, pos, u.t1, holes, now, rows, query, x, first, ask);
     holes = next_holes;
     next_holes = source.missing;
@@ -911,7 +924,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
 
 // BLOCKS: a part has four waves side by side.
 template <int DT, int DP, bool BIG, bool BLOCKS>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : BLOCKS ? 2 : 3) attend_held_kernel(AttendParams p) {
+__global__ void __launch_bounds__(256, DP > 128 ? (BLOCKS || BIG ? 1 : 2) : BLOCKS ? 2 : 3) attend_held_kernel(AttendParams p) {
   union Both {
     Lds<DP> few;
     typename std::conditional<BLOCKS, BlockLds<DP>, uint32_t>::type many;
@@ -936,10 +949,12 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : BLOCKS ? 2 : 3) attend_hel
   }
 }
 
+bool is_big(const AttendParams& p) { return (uint64_t)p.pool.num_blocks * p.pool.page_bytes >> 32; }
+
 template <int DT, int DP>
 kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
   const uint32_t groups = (uint32_t)attend_groups(p);
-  const bool big = (uint64_t)p.pool.num_blocks * p.pool.page_bytes >> 32;
+  const bool big = is_big(p);
   const bool blocks = p.part[0].waves == 4 || p.part[1].waves == 4;
   if (groups && big && blocks) hipLaunchKernelGGL((attend_held_kernel<DT, DP, true, true>), dim3(groups), dim3(256), 0, stream, p);
   else if (groups && big) hipLaunchKernelGGL((attend_held_kernel<DT, DP, true, false>), dim3(groups), dim3(256), 0, stream, p);
@@ -952,6 +967,7 @@ kvc_status launch_of(const AttendParams& p, hipStream_t stream) {
 }  // namespace
 
 namespace {
+
 
 // What a part of the work takes in units of 16 or 128 rows and of so many tokens each.
 struct Shape {
@@ -967,9 +983,9 @@ Shape shape_of(const AttendParams& p, uint32_t waves, uint64_t tokens, uint64_t 
   Shape best{};
   if (tokens == 0) return best;
   const bool many = waves == 4;
-  const double size = (p.D <= 64 ? 0.7 : p.D <= 128 ? 1.0 : 2.0) * (p.dtype == KVC_F16 ? 1.0 : many ? 0.73 : 0.82), start = many ? 3.0 : 4.0;
+  const double size = (p.D <= 64 ? 0.7 : p.D <= 128 ? 1.0 : many ? 1.3 : 1.5) * (p.dtype == KVC_F16 ? 1.0 : many ? 0.73 : 0.82), start = !many ? 4.0 : p.D <= 128 ? 3.0 : 4.5;
   const double alone = size * (many ? 0.0195 : 0.0028), shared = size * (many ? 0.0195 : 0.0034);
-  const uint64_t most = p.D > 128 ? 1 : many ? 2 : 3;  // workgroups to a CU
+  const uint64_t most = p.D > 128 ? (many || is_big(p) ? 1 : 2) : many ? 2 : 3;  // workgroups to a CU
   const uint64_t step = many ? kTile : 4 * kTile, block = many ? 64 * kRB : 16;
   best.waves = waves;
   best.time = 1e300;
