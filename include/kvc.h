@@ -683,7 +683,8 @@ kvc_status kvc_read_paged(const kvc_pool* pool, const kvc_batch* batch, const in
  * Arithmetic: products of 16-bit values summed in fp32, softmax and sums in fp32,
  * probabilities rounded to the cache's type before they meet V (those of fp16 down to 2^-32 of a
  * row's largest count), one rounding at the end.  Of a pool of KVC_HELD_Q4 the keys and values are x_hat before it is rounded to the
- * type; weights times a token's scale are rounded to bf16, or held in twice its bits for fp16. */
+ * type (an x_hat beyond the type's numbers counts as it is); the prefix is read once for each 16 or 128 rows; weights times a
+ * value's scale are rounded to fp16, for a pool of fp16 to two such numbers, and the sum of weights is of those before. */
 typedef struct {
   uint32_t struct_size; /* sizeof(kvc_attention)                                */
   uint32_t abi_version; /* KVC_ABI_VERSION                                      */
