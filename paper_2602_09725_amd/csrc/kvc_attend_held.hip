@@ -124,7 +124,7 @@ __device__ __forceinline__ Source<BIG> source_of(const AttendParams& p, const Un
   const bool gone = pos >= u.t1, bad = page >= p.pool.num_blocks, none = bad || gone;
   const uint32_t slot = pos - fd_div(p.pool.dbs, pos) * p.pool.block_size;
   const Offset begin = none ? (Offset)0 : (Offset)page * (Offset)p.pool.page_bytes;
-  return Source<BIG>{begin + (none ? 0u : slot / 4 * u.quad_bytes), begin + (none ? 0u : slot * 4), (uint32_t)__ballot(bad && !gone) & 0xffffu};
+  return Source<BIG>{begin + (none ? (Offset)0 : (Offset)(slot / 4) * u.quad_bytes), begin + (none ? (Offset)0 : (Offset)slot * 4), (uint32_t)__ballot(bad && !gone) & 0xffffu};
 }
 
 template <int DP, bool BIG>
