@@ -151,13 +151,17 @@ __device__ __forceinline__ void load_values(const AttendParams& p, const Unit<BI
   }
 }
 
-// A head whose values are all alike has scale 0.  It is given a scale of its value's size, and codes of 0 (as one whose least value is beyond 2^15 steps, which no
-// values of 16 bits have).
-__device__ __forceinline__ bool is_flat(float s, float m) { return fabsf(m) * 3.0517578125e-5f >= s; }
+// Scales of values lie in [2^-60, 2^40]: a sum of weights, each held times its value's scale, has what it needs of fp32's range then.  (fp16's all do.)  Larger ones count as not
+// finite.
+constexpr float kLeastScale = 8.67361738e-19f, kMostScale = 1.09951163e12f;
+
+// A head whose values are all alike has scale 0.  It is given a scale of its value's size, and codes of 0 (as one of smaller steps than that, or whose least value is beyond
+// 2^15 steps, which no values of 16 bits have).
+__device__ __forceinline__ bool is_flat(float s, float m) { return fabsf(m) * 3.0517578125e-5f >= s || s < kLeastScale; }
 
 // The least value in steps of the scale.
 __device__ __forceinline__ void steps_of(float& s, float m, float& z) {
-  if (is_flat(s, m)) s = fmaxf(fabsf(m), 8.67361738e-19f);  // (2^-60: its reciprocal, and sums of it, are numbers)
+  if (is_flat(s, m)) s = fmaxf(fabsf(m), kLeastScale);
   const float r = __builtin_amdgcn_rcpf(s);
   z = m * r;
   z = fmaf(fmaf(-z, s, m), r, z);
@@ -183,10 +187,11 @@ __device__ __forceinline__ uint64_t flat_tokens(uint32_t pair) {
 template <int DT>
 __device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, uint32_t pair) {
   constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
-  const bool wild = (pair & kExp) == kExp || (pair >> 16 & kExp) == kExp;
+  bool wild = (pair & kExp) == kExp || (pair >> 16 & kExp) == kExp;
   float s, m, z;
   widen_pair<DT>(pair, s, m);
   steps_of(s, m, z);
+  if (DT == KVC_BF16) wild |= s > kMostScale;
   z = wild ? 0.0f : z + 8.0f;
   to.lv[token] = wild ? __builtin_nanf("") : __builtin_amdgcn_logf(s);
   to.rv[token] = __builtin_amdgcn_rcpf(s);

@@ -268,3 +268,43 @@ def test_layers_beyond_4_gib(kvc_lib, D, H, G, new):
     kvc.kvc_pages_copy(d.pool, source.data_ptr(), place.data_ptr(), 2, hz.stream_handle())
     torch.cuda.synchronize()
     assert torch.equal(cache[0][:, [3, 4]], cache[0][:, [places[1], places[8]]])
+
+
+def check_all_sizes(a):
+    """Against the model, where values are of all sizes: rows that see a bf16 head with a scale above 2^40, or of one number above it, are NaN; a result may be
+    beyond the type, the largest number or infinity then (x_hat of 65504 and its like reaches 65536), if the bound reaches it."""
+    got, norm = a.run()
+    assert a.d.fault() == 0
+    out, lse, off, lse_off = a.model()
+    code, s, m = a.d.form.get(a.d.cache[1, 1].cpu(), TORCH[a.dtype])
+    wild = (s > 2.0 ** 40) | ((s * 2 ** 15 <= m.abs()) & (m.abs() > 2.0 ** 40))
+    bad = torch.zeros(norm.shape, dtype=torch.bool)
+    for r, row in enumerate(a.rows):
+        table, total, n = a.d.host_tables[row], a.d.host_lens[row], a.starts[r + 1] - a.starts[r]
+        for i in range(n):
+            last = total - n + i
+            for h in range(a.H):
+                bad[a.starts[r] + i, h * a.G:(h + 1) * a.G] = any(bool(wild[table[t // a.d.block], t % a.d.block, h]) for t in range(last + 1))
+    assert torch.isnan(got[bad]).all() and torch.isnan(norm[bad]).all()
+    most = torch.finfo(TORCH[a.dtype]).max
+    far, ok = off[~bad], got[~bad].double()
+    ok = torch.where(ok.isinf(), ok.sign() * most, ok)
+    assert bool(((ok - out[~bad].clamp(-most, most)).abs() <= far).all())
+    assert bool(((norm[~bad].double() - lse[~bad]).abs() <= lse_off[~bad]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("G,D,new", [(4, 64, [0, 3, 0, 1, 0]), (8, 128, [0, 60, 0, 45, 0]), (2, 256, [0, 70, 0, 90, 0])])
+@pytest.mark.parametrize("prefix", [0, 101])
+def test_requests_without_tokens(kvc_lib, dtype, G, D, new, prefix):
+    """First, last and between others; a row of nothing among them.  Written, attended to and read back."""
+    a = Attend(new, [0, 90, 10, 100, 5], prefix, 2, G, D, 8, dtype, seed=7)
+    k, v = tokens_like(a.n, 2, D, dtype, 8), tokens_like(a.n, 2, D, dtype, 9)
+    kd, vd = k.cuda(), v.cuda()
+    kvc.kvc_append_paged(a.d.pool, a.batch, 1, kd.data_ptr(), vd.data_ptr(), 2 * D, hz.stream_handle())
+    check_all_sizes(a)
+    out = torch.zeros((2, a.n, 2, D), dtype=TORCH[dtype], device="cuda")
+    kvc.kvc_read_paged(a.d.pool, a.batch, None, 1, out[0].data_ptr(), out[1].data_ptr(), 2 * D, hz.stream_handle())
+    assert a.d.fault() == 0
+    for got, x in zip(out.cpu(), (k, v)):
+        assert torch.equal(got, held.rounded(held.stands_for(*held.quantized(x)), TORCH[dtype]))
