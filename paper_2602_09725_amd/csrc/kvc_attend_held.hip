@@ -64,6 +64,7 @@ struct Unit {
   uint64_t values;                          // from keys to values
   const int32_t* table;
   uint32_t t0, t1, bound;  // tokens of the unit that are there; none that the host knows of lies at or beyond `bound`
+  uint32_t first;          // tokens below it are the other part's: up to three, where the prefix ends inside the quad that t0 is
   uint32_t quad_bytes;     // codes of a quad
 };
 
@@ -183,9 +184,10 @@ __device__ __forceinline__ uint64_t flat_tokens(uint32_t pair) {
   return __ballot(is_flat(s, m));
 }
 
-// A pair that is not finite makes NaN of the weights that see it, and nothing of the others.
+// A pair that is not finite makes NaN of the weights that see it, and nothing of the others.  there: the token is the part's own; one that is not has weight 0 for all rows.
+// (Decided here it costs a token a lane; among the masks of scores, 16 a lane, calls without a prefix took 7 % longer.)
 template <int DT>
-__device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, uint32_t pair) {
+__device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, uint32_t pair, bool there) {
   constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
   bool wild = (pair & kExp) == kExp || (pair >> 16 & kExp) == kExp;
   float s, m, z;
@@ -193,7 +195,7 @@ __device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, ui
   steps_of(s, m, z);
   if (DT == KVC_BF16) wild |= s > kMostScale;
   z = wild ? 0.0f : z + 8.0f;
-  to.lv[token] = wild ? __builtin_nanf("") : __builtin_amdgcn_logf(s);
+  to.lv[token] = !there ? kNone : wild ? __builtin_nanf("") : __builtin_amdgcn_logf(s);
   to.rv[token] = __builtin_amdgcn_rcpf(s);
   const uint32_t high = narrow_pair<KVC_F16>(z, 0.0f);
   to.z[0][token] = (uint16_t)high;
@@ -322,8 +324,9 @@ __device__ __forceinline__ void take_tile(const AttendParams& p, const Unit<BIG>
                                           const Rows<RB>& rows, const u32x4 (&query)[RB][Sizes<DP>::KS], State<DP, RB>& x, PairSpace& pairs) {
   using S = Sizes<DP>;
   const uint32_t lane = threadIdx.x & 63u, g = lane >> 4;
-  put_key_pair<DT>(pairs, lane, t.kp, rows.unit);
-  put_value_pair<DT>(pairs, lane, t.vp);
+  const bool there = at + lane >= u.first;
+  put_key_pair<DT>(pairs, lane, there ? t.kp : 0, rows.unit);
+  put_value_pair<DT>(pairs, lane, there ? t.vp : 0, there);
   const uint64_t flat = flat_tokens<DT>(t.vp);
   // (The order is the source's: left to itself the compiler makes all operands first, and has no registers for them.)
   f32x4 s[RB][4];
@@ -561,6 +564,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   Unit<BIG> u;
   u.bound = shared ? p.prefix : p.most_tokens;
   u.t0 = (shared ? 0 : p.own_from) + at_work.split * part.tokens;
+  u.first = shared ? 0 : p.prefix;
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
   constexpr uint32_t NEXT = LONE ? kTile : 4 * kTile;
   const uint32_t start = u.t0 + (LONE ? 0 : wave * kTile);
@@ -605,7 +609,8 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   }
   lanes_see(most, least);
   least = wave_uniform(least);
-  const uint32_t end = min(u.t1, wave_uniform(most)), plain = min(least, u.t1);
+  const uint32_t seen = min(u.t1, wave_uniform(most)), plain = min(least, u.t1);
+  const uint32_t end = seen > u.first ? seen : 0;  // (a quad that has none of the part's tokens is not looked at)
   u32x4 query[RB][S::KS];
   make_queries<DT, DP, RB>(p, load_queries<DT, DP, RB>(p, from, query, rows), query, rows);
 
@@ -631,7 +636,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
     take_tile<DT, DP, RB, BIG>(p, u, pos + kTile > plain || holes, pos, holes, at_tile, tile, rows, query, x, pairs);
   }
   if (missing && lane == 0) fault(p, KVC_FAULT_PAGE);
-  if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
+  if (u.t0 >= seen && p.pieces > 1) return;  // the join does not look for it
 
   // Results go through LDS, so that a row's are written side by side; waves along the tokens are joined there.
   put_sums<DP, 1>(x, lds.of[wave].sums, lds.m[wave], lds.l[wave]);
@@ -699,12 +704,13 @@ __device__ __forceinline__ void load_share(const AttendParams& p, const Unit<BIG
   }
 }
 
-// Makes a wave's share of a tile's operands.
+// Makes a wave's share of the operands of the tile at `at`.
 template <int DT, int DP>
-__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, float unit, Made<DP>& to) {
+__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, uint32_t at, uint32_t first_token, float unit, Made<DP>& to) {
   const uint32_t lane = threadIdx.x & 63u, h = wave >> 1;
-  if (wave == 0) put_key_pair<DT>(to.pairs, lane, t.kp, unit);
-  if (wave == 1) put_value_pair<DT>(to.pairs, lane, t.vp);
+  const bool there = at + lane >= first_token;
+  if (wave == 0) put_key_pair<DT>(to.pairs, lane, there ? t.kp : 0, unit);
+  if (wave == 1) put_value_pair<DT>(to.pairs, lane, there ? t.vp : 0, there);
   const uint64_t flat = flat_tokens<DT>(t.vp);
 #pragma unroll
   for (int i = 0; i < Share<DP>::KE; ++i) {
@@ -838,6 +844,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
   Unit<BIG> u;
   u.bound = shared ? p.prefix : p.most_tokens;
   u.t0 = (shared ? 0 : p.own_from) + at_work.split * part.tokens;
+  u.first = shared ? 0 : p.prefix;
   u.table = p.pool.tables + (uint64_t)(shared ? p.prefix_row : wave_uniform(q.row)) * p.pool.table_len;
   uint32_t page[3];
 #pragma unroll
@@ -884,7 +891,8 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
   if (lane == 0) lds.most[wave] = largest, lds.seen[wave] = most;
   meet();
   largest = wave_uniform(max(max(lds.most[0], lds.most[1]), max(lds.most[2], lds.most[3])));
-  const uint32_t end = min(u.t1, wave_uniform(max(max(lds.seen[0], lds.seen[1]), max(lds.seen[2], lds.seen[3]))));
+  const uint32_t seen = min(u.t1, wave_uniform(max(max(lds.seen[0], lds.seen[1]), max(lds.seen[2], lds.seen[3]))));
+  const uint32_t end = seen > u.first ? seen : 0;  // (a quad that has none of the part's tokens is not looked at)
   const uint32_t mine = min(u.t1, most), plain = min(least, u.t1);
   make_queries<DT, DP, kRB>(p, largest, query, rows);
 
@@ -900,7 +908,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
       for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
   }
   uint32_t missing = 0;
-  if (u.t0 < end) make_share<DT, DP>(share, wave, rows.unit, lds.made[0]);
+  if (u.t0 < end) make_share<DT, DP>(share, wave, u.t0, u.first, rows.unit, lds.made[0]);
   source = source_of<BIG>(p, u, u.t0 + kTile, page[1]);
   next_holes = source.missing;
   load_share<DP, BIG>(p, u, source, wave, share);
@@ -911,7 +919,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
     meet();  // what is in `now` is there, and the other one has been read
     u32x4 first[kAhead + 1][2];
     read_first<DP>(now, first);
-    if (pos + kTile < end) make_share<DT, DP>(share, wave, rows.unit, lds.made[turn ^ 1u]);
+    if (pos + kTile < end) make_share<DT, DP>(share, wave, pos + kTile, u.first, rows.unit, lds.made[turn ^ 1u]);
     __builtin_amdgcn_sched_barrier(0);
     missing |= holes;
     auto ask = [&]() {
@@ -926,7 +934,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
     next_holes = source.missing;
   }
   if (missing && threadIdx.x == 0) fault(p, KVC_FAULT_PAGE);
-  if (u.t0 >= end && p.pieces > 1) return;  // the join does not look for it
+  if (u.t0 >= seen && p.pieces > 1) return;  // the join does not look for it
   meet();  // the sums lie where the operands were
   put_sums<DP, kRB>(x, lds.sums[wave], lds.m[wave], lds.l[wave]);
   __builtin_amdgcn_wave_barrier();
@@ -1023,10 +1031,10 @@ kvc_status plan_attend_held(AttendParams& p) {
   p.pieces = 0;
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = p.lift = 0.0f;
-  // Tiles lie on quads of the pages: up to three last tokens of a prefix that ends inside one are read through each row's own table, which has them too.
-  p.prefix &= ~3u;
-  p.own_from = p.prefix;
-  const uint64_t tokens[2] = {p.own_from, p.most_tokens - p.own_from}, requests[2] = {1, p.batch.n_requests};
+  // Tiles lie on quads of the pages: a quad that the prefix ends in is a tile's in both parts, the prefix's through its row's table and the rows' own through theirs, each
+  // with its tokens alone.
+  p.own_from = p.prefix & ~3u;
+  const uint64_t tokens[2] = {p.prefix, p.most_tokens > p.prefix ? p.most_tokens - p.own_from : 0}, requests[2] = {1, p.batch.n_requests};
   const uint64_t rows[2] = {(uint64_t)p.batch.n_new * p.G, (uint64_t)p.batch.most_new * p.G};
   Shape few[2], many[2];
   for (int i = 0; i < 2; ++i) {
