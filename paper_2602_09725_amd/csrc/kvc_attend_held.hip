@@ -244,12 +244,13 @@ __device__ __forceinline__ void stay(f32x4& v) {
 
 // Weights of a tile from its products s[k][i], those of token 16 g + 4 i + k (they are overwritten): operands w[h] of tokens 16 g + 8 h .. + 7, and for fp16
 // what their rounding left.  masked: not all of it is there and seen by all rows (wave-uniform); missing: quads on no page.  The number subtracted from an exponent need not be
-// the largest one, as long as no weight leaves fp16; so that small ones stay in it too it lies 2^8 below the product that moves it for a pool of fp16.  (The order is the source's: a few of LDS's numbers at a time.)
+// the largest one, as long as no weight leaves fp16; so that small ones stay in it too it lies 2^8 below the product that moves it.  Weights times scales down to 2^-33 of a row's largest
+// count then; they are rounded to steps of 2^-24, and those below half of one are lost, while the sum of weights has them.  (The order is the source's: a few of LDS's numbers at a time.)
 template <int DT, int DP, int RB>
 __device__ __forceinline__ void weights(bool masked, uint32_t at, uint32_t t1, uint32_t missing, const PairSpace& pairs, const Rows<RB>& rows, int b, f32x4 (&s)[4],
                                         State<DP, RB>& x, u32x4 (&w)[2], u32x4 (&fine)[2]) {
   const uint32_t g = (threadIdx.x & 63u) >> 4;
-  constexpr float kLift = DT == KVC_F16 ? 8.0f : 0.0f, kMost = DT == KVC_F16 ? 15.0f : 6.0f;
+  constexpr float kLift = 8.0f, kMost = 15.0f;
   const float shift = x.m[b] == kNone ? 0.0f : x.m[b];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
