@@ -687,7 +687,7 @@ kvc_status kvc_read_paged(const kvc_pool* pool, const kvc_batch* batch, const in
  * value's scale are rounded to fp16, for a pool of fp16 to two such numbers (in steps of at most 2^-32 of a row's largest one: smaller ones than half of that
  * add nothing to the values' sum), and the sum of weights is of those before.  Queries are
  * taken as fp16 numbers times a power of two that up to 128 rows share: of an element less than 2^-24 of the largest finite one among them low bits are lost, and
- * one less than 2^-36 of it may count as 0.  Finite queries lie below 2^115.
+ * one of at most 2^-35 of it may count as 0.  Finite queries lie below 2^115.
  * Values in bf16: a head with a scale above 2^40, or of one number above it, counts as NaN; steps of a scale below 2^-60 count as 0. */
 typedef struct {
   uint32_t struct_size; /* sizeof(kvc_attention)                                */

@@ -97,7 +97,7 @@ kvc_status launch_convert(const ConvertParams& p, hipStream_t stream);
 // One of the two parts of an attention call: the shared prefix, or the rows' own tokens.
 struct AttendPart {
   uint32_t waves;       // waves of a workgroup that stand side by side along the rows: 1 or 4
-  uint32_t row_blocks;  // blocks of 32 * waves rows
+  uint32_t row_blocks;  // blocks of 32 rows, or of 128 where four waves stand side by side (over 4 bits of 16 or 128)
   uint32_t splits;      // pieces of the tokens, 0: the part is empty
   uint32_t tokens;      // of a piece
   uint32_t units;       // workgroups

@@ -64,3 +64,34 @@ def test_small_weights_behind_a_large_one(kvc_lib, dtype, gap, shape):
             off[a.starts[r]:a.starts[r + 1]] -= (2.0 ** -25 - 2.0 ** -33) * steps[:, None, None]
         assert (off > 0).all()
     compare(got, norm, (out, lse, off, lse_off))
+
+
+@pytest.mark.parametrize("element", range(1, 9))
+@pytest.mark.parametrize("new", [1, 150])
+def test_small_elements_of_a_query_beside_a_large_one(kvc_lib, element, new):
+    """Of 2^-34 of the largest: it still counts, at each place of a word.  Keys of steps of 2^33 that only it meets make a product of 7/2 of it."""
+    a = Call([new], [new + 1], 0, 1, 2, 64, 8, "bf16")
+    a.q = torch.zeros_like(a.q)
+    a.q[..., 0], a.q[..., element] = 1.0, 2.0 ** -34
+    d = a.d
+    words = d.cache.cpu()
+    form, table = d.form, d.host_tables[1]
+    value = lambda v: torch.tensor(v, dtype=torch.bfloat16).view(torch.int16).item() & 0xffff  # noqa: E731
+    s, m = value(2.0 ** 33), value(-2.0 ** 36)
+    for t in range(new + 1):
+        page, slot = table[t // d.block], t % d.block
+        words[1, 0, page, form.pair(0, slot)] = 0
+        if t == 0:
+            w = s | m << 16
+            words[1, 0, page, form.pair(0, slot)] = w - (w >= 2 ** 31) * 2 ** 32
+            for i in range(8):  # codes of 8, which with the least value stand for 0, and one of 15
+                codes = [15 if 8 * i + k == element else 8 for k in range(8)]
+                w = sum(c << held.shift_of(k) for k, c in enumerate(codes))
+                words[1, 0, page, form.word(0, slot, i)] = w - (w >= 2 ** 31) * 2 ** 32
+    d.cache.copy_(words)
+    _, norm = a.run()
+    assert a.d.fault() == 0
+    # the first token's score is 7 / 2 * scale, exact but for a few roundings of 32 bits; of n others it is 0
+    others = torch.arange(1, new + 1, dtype=torch.float64)[:, None]
+    want = torch.log(math.exp(3.5 * a.scale) + others)
+    assert bool(((norm.double() - want).abs() <= 2.0 ** -24 * (40 + new) * (1 + want.abs())).all())
