@@ -1,7 +1,7 @@
 """Serving from a restored cache: a prompt's KV cache comes out of packed frames into pages, many requests take it up, and each
 goes on with tokens of its own.
 
-  restore   kvc_pages_grow, kvc_restore_paged: the prompt's pages are row 0's (of a pool in 4 bits: restored beside it, and moved by kvc_pages_convert)
+  restore   kvc_pages_grow, kvc_restore_paged: the prompt's pages are row 0's (of a pool in 4 bits: restored beside it, a chunk at a time, and moved by kvc_pages_convert)
   admit     kvc_pages_fork: the requests' rows share whole pages of the prompt, and have a copy of its last one
   step      kvc_pages_grow, then in every layer kvc_append_paged and kvc_attend_paged
   finish    kvc_pages_free: pages that no row holds any more are free again
@@ -86,17 +86,23 @@ class Server:
         self.prompt = n_tokens
 
     def _restore_held(self, layout, frames, meta, n_tokens):
-        """Restores to pages of 16 bits that are the prompt's alone, and moves them to row 0's.  (They are kept until the next prompt: the calls are on their way.)"""
+        """Restores chunk by chunk to a few pages of 16 bits, taken in turn, and moves those that are complete to row 0's."""
         m, (dtype, code), pages = self.model, DTYPES[self.model.dtype], -(-n_tokens // self.block)
-        wide = torch.zeros((m.layers, 2, pages, self.block, m.heads, m.head_dim), dtype=dtype, device="cuda")
+        chunk, (frame_bytes, meta_bytes, _) = layout.chunk_tokens, kvc.chunk_sizes(layout)
+        ring = min(pages, chunk // self.block + 2)
+        wide = torch.zeros((m.layers, 2, ring, self.block, m.heads, m.head_dim), dtype=dtype, device="cuda")
         pointers = torch.tensor([c.data_ptr() for c in wide], dtype=torch.int64, device="cuda")
-        order = torch.arange(pages, dtype=torch.int32, device="cuda")
-        kvc.kvc_restore_paged(layout, frames.data_ptr(), meta.data_ptr(), 0, n_tokens, pointers.data_ptr(), pages, self.block, order.data_ptr(), pages,
-                              self.err.data_ptr(), stream())
-        pool = kvc.Pool(m.layers, m.heads, m.head_dim, code, pages, self.block, 1, 1, pointers.data_ptr(), self.tables.data_ptr(), self.lens.data_ptr(), None,
+        turn = torch.arange(pages, dtype=torch.int32, device="cuda") % ring
+        pool = kvc.Pool(m.layers, m.heads, m.head_dim, code, ring, self.block, 1, 1, pointers.data_ptr(), self.tables.data_ptr(), self.lens.data_ptr(), None,
                         self.err.data_ptr())
-        kvc.kvc_pages_convert(pool, self.pool, order.data_ptr(), self.tables.data_ptr(), pages, stream())
-        self.restored = (wide, pointers, order)
+        moved = 0
+        for i, begin in enumerate(range(0, n_tokens, chunk)):
+            end = min(n_tokens, begin + chunk)
+            kvc.kvc_restore_paged(layout, frames.data_ptr() + i * frame_bytes, meta.data_ptr() + i * meta_bytes, begin, end - begin, pointers.data_ptr(), ring, self.block,
+                                  turn.data_ptr(), pages, self.err.data_ptr(), stream())
+            whole = pages if end == n_tokens else end // self.block  # (a page that the chunk ends in waits for the next one)
+            kvc.kvc_pages_convert(pool, self.pool, turn[moved:].data_ptr(), self.tables[0, moved:].data_ptr(), whole - moved, stream())
+            moved = whole
 
     def read_back(self, row, layer):
         """Keys and values of a row, as what its pages hold stands for."""
