@@ -658,7 +658,8 @@ typedef struct {
  *   k, v          DEVICE in: [n_new][H][D], 16-byte aligned, the [H][D] of a token contiguous
  *   token_stride  elements from a token to the next, of k and of v; a multiple of 8
  * A token whose page is outside the pool (KVC_FAULT_PAGE), or whose position is not in its
- * row (KVC_FAULT_LIST), is left out. */
+ * row (KVC_FAULT_LIST), is left out.  A row that is in the batch twice is written to by both requests in no order (in
+ * 4 bits a token may then have the codes of one and the scale of the other). */
 kvc_status kvc_append_paged(const kvc_pool* pool, const kvc_batch* batch, int32_t layer, const void* k, const void* v,
                             int64_t token_stride, void* stream);
 
