@@ -833,7 +833,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendParams p) {
   if (p.pieces == 0 && there && head == 0 && self == 0) fault(p, q.faults);  // (no other kernel has looked at it)
   const uint32_t limit = limit_of(p, q, token), prefix = min(limit, prefix_there(p));
   // pieces that hold something: those that begin below what the row sees
-  uint32_t a = p.part[0].splits ? fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1) : 0;
+  // (over 4 bits the prefix's last piece may have up to three tokens more than the others)
+  uint32_t a = p.part[0].splits ? min(p.part[0].splits, fd_div(p.part[0].dtokens, prefix + p.part[0].tokens - 1)) : 0;
   uint32_t n = p.part[1].splits && limit > p.own_from ? fd_div(p.part[1].dtokens, limit - p.own_from + p.part[1].tokens - 1) : 0;
   if (!there) a = n = 0;
   const uint32_t split = p.part[0].splits, end = split + n;

@@ -185,7 +185,7 @@ __device__ __forceinline__ uint64_t flat_tokens(uint32_t pair) {
 }
 
 // A pair that is not finite makes NaN of the weights that see it, and nothing of the others.  there: the token is the part's own; one that is not has weight 0 for all rows.
-// (Decided here it costs a token a lane; among the masks of scores, 16 a lane, calls without a prefix took 7 % longer.)
+// (Only a part's first tile has such tokens.  Decided here it costs a token a lane; among the masks of scores, 16 a lane, calls without a prefix took 7 % longer.)
 template <int DT>
 __device__ __forceinline__ void put_value_pair(PairSpace& to, uint32_t token, uint32_t pair, bool there) {
   constexpr uint32_t kExp = DT == KVC_F16 ? 0x7c00u : 0x7f80u;
@@ -236,7 +236,8 @@ constexpr float size_of(int j) { return (DP == 64 ? j : j / 2) % 2 ? 0.0625f : 1
 
 // Sums of more than 128 elements have no room among the registers that other arithmetic takes: they stay in the matrix unit's own also where they are multiplied, once in
 // many tiles.  (Left to itself the compiler moves all of them there and back for every tile; and 16 rows' fit two
-// waves a SIMD so: a prompt of 8000 tokens, 16 query heads of 256, 974 -> 860 us, 64 requests of up to 2000 tokens 76 -> 45.)
+// waves a SIMD so: a prompt of 8000 tokens, 16 query heads of 256, 974 -> 860 us, 64 requests of up to 2000 tokens 76 -> 45.  The 16-row body is short of registers
+// then: 7 of a lane, 10 with fp16's second weights, lie in memory; of 128 elements with offsets of 64 bits 2 with fp16.)
 template <int DP>
 __device__ __forceinline__ void stay(f32x4& v) {
   if constexpr (DP > 128) asm volatile("" : "+a"(v));
@@ -587,7 +588,7 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
   place_of_head(p, at_work.head, u);
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
   if (shared && u.t1 < p.prefix && speaker == 0) fault(p, KVC_FAULT_LIST);
-  u.t1 = min(u.t1, u.t0 + part.tokens);
+  u.t1 = min(u.t1, at_work.split + 1 < part.splits ? u.t0 + part.tokens : ~0u);  // (the prefix's last piece has its last tokens too)
   const bool has_tile = start < u.t1;
   Tile<DP> tile;
   Source<BIG> at_tile = source_of<BIG>(p, u, start, page[0]);
@@ -654,8 +655,9 @@ __device__ __forceinline__ void attend_unit(const AttendParams& p, const AttendP
 //
 // Four waves side by side along the rows, 32 each, take the same tiles.  What a tile's codes become as operands is made once: each wave makes a quarter of it,
 // for the tile after the present one, into LDS, where an operand's 16 bytes a lane lie side by side.  One barrier a tile.
-// Arithmetic on scores bounds it (scale, shift, exp2, rounding, a sum: the matrix unit is busy 34 % of the time): 10 000 rows of 128 over 32K tokens of 8 heads 1.72 ms, 786
-// TFLOP/s.  Two workgroups a CU (69 KB of LDS, 252 registers) let one's products run beside the other's scores; waves in products go first (1765 -> 1745 us).  Of heads of
+// Scores and products, which take turns in a wave, bound it (scale, shift, exp2, rounding, a sum: vector instructions are issued nearly half of the time, the matrix unit is busy 34 %), and
+// reads of LDS are not far behind (79 instructions a wave and tile, most of 16 bytes a lane, which take 8 cycles each: 80 %): 10 000 rows of 128 over 32K tokens of 8 heads 1.73 ms, 782
+// TFLOP/s; fp16, whose weights are two numbers, 2.2 ms.  Two workgroups a CU (69 KB of LDS, 252 registers) let one's products run beside the other's scores; waves in products go first (1765 -> 1745 us).  Of heads of
 // more than 128 one fits (135 KB, sums of 128 registers), whose phases take turns.
 
 template <int DP>
@@ -705,11 +707,10 @@ __device__ __forceinline__ void load_share(const AttendParams& p, const Unit<BIG
   }
 }
 
-// Makes a wave's share of the operands of the tile at `at`.
+// Makes a wave's share of a tile's operands.  there: token `lane` is the part's own.
 template <int DT, int DP>
-__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, uint32_t at, uint32_t first_token, float unit, Made<DP>& to) {
+__device__ __forceinline__ void make_share(const Share<DP>& t, uint32_t wave, bool there, float unit, Made<DP>& to) {
   const uint32_t lane = threadIdx.x & 63u, h = wave >> 1;
-  const bool there = at + lane >= first_token;
   if (wave == 0) put_key_pair<DT>(to.pairs, lane, there ? t.kp : 0, unit);
   if (wave == 1) put_value_pair<DT>(to.pairs, lane, there ? t.vp : 0, there);
   const uint64_t flat = flat_tokens<DT>(t.vp);
@@ -866,7 +867,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
   place_of_head(p, at_work.head, u);
   u.t1 = shared ? prefix_there(p) : min(wave_uniform(q.len), p.most_tokens);
   if (shared && u.t1 < p.prefix && threadIdx.x == 0) fault(p, KVC_FAULT_LIST);
-  u.t1 = min(u.t1, u.t0 + part.tokens);
+  u.t1 = min(u.t1, at_work.split + 1 < part.splits ? u.t0 + part.tokens : ~0u);  // (the prefix's last piece has its last tokens too)
   // (a tile that is not there is read from page 0)
   Share<DP> share;
   Source<BIG> source = source_of<BIG>(p, u, u.t0, page[0]);
@@ -909,7 +910,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
       for (int j = 0; j < S::NJ; ++j) x.sum[b][v][j] = f32x4{0, 0, 0, 0};
   }
   uint32_t missing = 0;
-  if (u.t0 < end) make_share<DT, DP>(share, wave, u.t0, u.first, rows.unit, lds.made[0]);
+  if (u.t0 < end) make_share<DT, DP>(share, wave, u.t0 + lane >= u.first, rows.unit, lds.made[0]);
   source = source_of<BIG>(p, u, u.t0 + kTile, page[1]);
   next_holes = source.missing;
   load_share<DP, BIG>(p, u, source, wave, share);
@@ -920,7 +921,7 @@ __device__ __forceinline__ void attend_block(const AttendParams& p, const Attend
     meet();  // what is in `now` is there, and the other one has been read
     u32x4 first[kAhead + 1][2];
     read_first<DP>(now, first);
-    if (pos + kTile < end) make_share<DT, DP>(share, wave, pos + kTile, u.first, rows.unit, lds.made[turn ^ 1u]);
+    if (pos + kTile < end) make_share<DT, DP>(share, wave, true, rows.unit, lds.made[turn ^ 1u]);
     __builtin_amdgcn_sched_barrier(0);
     missing |= holes;
     auto ask = [&]() {
@@ -1033,9 +1034,10 @@ kvc_status plan_attend_held(AttendParams& p) {
   p.dheads = make_fastdiv(p.H * p.G);
   p.slack = p.lift = 0.0f;
   // Tiles lie on quads of the pages: a quad that the prefix ends in is a tile's in both parts, the prefix's through its row's table and the rows' own through theirs, each
-  // with its tokens alone.
+  // with its tokens alone.  The prefix's pieces are cut as if it ended where that quad begins, and the last one has what follows (128 rows of 8 heads over 515 tokens: 25.1 us
+  // with a piece of 3 tokens, 22.0 so).
   p.own_from = p.prefix & ~3u;
-  const uint64_t tokens[2] = {p.prefix, p.most_tokens > p.prefix ? p.most_tokens - p.own_from : 0}, requests[2] = {1, p.batch.n_requests};
+  const uint64_t tokens[2] = {p.own_from ? p.own_from : p.prefix, p.most_tokens > p.prefix ? p.most_tokens - p.own_from : 0}, requests[2] = {1, p.batch.n_requests};
   const uint64_t rows[2] = {(uint64_t)p.batch.n_new * p.G, (uint64_t)p.batch.most_new * p.G};
   Shape few[2], many[2];
   for (int i = 0; i < 2; ++i) {

@@ -99,7 +99,7 @@ struct AttendPart {
   uint32_t waves;       // waves of a workgroup that stand side by side along the rows: 1 or 4
   uint32_t row_blocks;  // blocks of 32 rows, or of 128 where four waves stand side by side (over 4 bits of 16 or 128)
   uint32_t splits;      // pieces of the tokens, 0: the part is empty
-  uint32_t tokens;      // of a piece
+  uint32_t tokens;      // of a piece (over 4 bits the prefix's last one has up to three more)
   uint32_t units;       // workgroups
   uint32_t lone;        // units in all, a wave each; 0: a workgroup each
   FastDiv drows, dsplits, drequests, dtokens;

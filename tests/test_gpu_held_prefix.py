@@ -45,7 +45,7 @@ def others(a):
 
 @ALL
 @BOTH
-@pytest.mark.parametrize("prefix", [301, 302, 303, 130, 3, 1])
+@pytest.mark.parametrize("prefix", [301, 302, 303, 257, 514, 130, 67, 3, 1])
 def test_the_prefix_is_read_through_its_row(kvc_lib, shape, dtype, prefix):
     """Rows' tables that lack the prefix's whole pages, and own pages with something else in its last slots: neither is looked at, nor told."""
     a = call(shape, prefix, dtype)
@@ -59,7 +59,7 @@ def test_the_prefix_is_read_through_its_row(kvc_lib, shape, dtype, prefix):
 
 @ALL
 @BOTH
-@pytest.mark.parametrize("prefix,there", [(301, 300), (303, 301), (302, 300), (302, 299), (3, 2), (2, 0)])
+@pytest.mark.parametrize("prefix,there", [(301, 300), (303, 301), (259, 257), (513, 512), (302, 300), (302, 299), (3, 2), (2, 0)])
 def test_a_prefix_row_that_ends_a_little_early(kvc_lib, shape, dtype, prefix, there):
     """What it lacks is seen by nobody, whatever the rows' own pages have there, and is told."""
     a = call(shape, prefix, dtype)
